@@ -302,6 +302,139 @@ int spectrain_stage_read_stash(spectrain_stage_t st, int64_t mb_id, int32_t inde
  * Passing NULL returns EINVAL. */
 int spectrain_stage_destroy(spectrain_stage_t st);
 
+/* ---- Operators ----
+ *
+ * What a TRANSFORMER stage with positions, masks or an 8-bit stash
+ * (spectrain_stage_set_attention, spectrain_stage_set_stash) runs, for callers
+ * with tensors of their own. Each call checks its arguments on the host
+ * (EINVAL, nothing enqueued), enqueues its work on hip_stream (NULL = the null
+ * stream) of the current device, which has to be the tensors' device, and
+ * allocates and keeps nothing, so it can be captured in a HIP graph. Tensors
+ * are device memory; their last dimension is contiguous. A tensor with a
+ * dimension of 0 is allowed and makes the call write nothing (an attention
+ * with kv_len 0 has rows that see no key: see there).
+ * Workspace memory is the caller's: calls that may overlap need one each. */
+
+/* Strides, in elements, of a [batch, token, head, head_dim] tensor, each in
+ * [0, 2^40]. A written tensor may not overlap itself; a stride of 0 repeats an
+ * input. */
+typedef struct {
+  int64_t batch, token, head;
+} spectrain_strides;
+
+/* Rotary positions: the first rotary_dim values of every head, as rotary_dim/2
+ * pairs, are turned by angle position * frequency_i, frequency_i = base^(-2 i /
+ * rotary_dim) before scaling; the other values are copied. The angle is formed
+ * in float64, so far positions keep their phase. positions: int32 [batch,
+ * tokens], or NULL for first_position + token. inverse != 0 turns the other way
+ * (the gradient of the forward turn). out may be x itself (same strides);
+ * otherwise the two may not overlap. */
+typedef enum {
+  SPECTRAIN_ROTARY_HALF = 0,         /* pair i: values i and i + rotary_dim/2 */
+  SPECTRAIN_ROTARY_INTERLEAVED = 1   /* pair i: values 2i and 2i + 1 */
+} spectrain_rotary_layout;
+
+typedef enum {
+  SPECTRAIN_ROTARY_UNSCALED = 0,
+  SPECTRAIN_ROTARY_LINEAR = 1,       /* frequency_i / factor */
+  SPECTRAIN_ROTARY_NTK = 2,          /* base * factor^(rotary_dim / (rotary_dim - 2)); rotary_dim 2: unscaled */
+  SPECTRAIN_ROTARY_PARTS = 3         /* pairs of >= 32 turns within original_length keep their frequency, those of
+                                        <= 1 turn divide it by factor, linear in the turns between; every turned
+                                        value is multiplied by 0.1 ln(factor) + 1 */
+} spectrain_rotary_scaling;
+
+typedef struct {
+  uint32_t abi_version;      /* SPECTRAIN_ABI_VERSION */
+  int32_t dtype;             /* spectrain_dtype of x and out */
+  int32_t batch, tokens, heads, head_dim;   /* >= 0; batch * tokens < 2^24, heads < 2^16, head_dim 2 .. 256 */
+  int32_t rotary_dim;        /* even, 2 .. head_dim */
+  int32_t layout;            /* spectrain_rotary_layout */
+  int32_t scaling;           /* spectrain_rotary_scaling */
+  int32_t original_length;   /* PARTS: >= 1 */
+  int32_t first_position;
+  int32_t reserved;          /* 0 */
+  double base;               /* > 1 */
+  double factor;             /* scaled: >= 1 */
+  spectrain_strides x, out;
+} spectrain_rotary_desc;
+
+int spectrain_rotary(const spectrain_rotary_desc* desc, const void* x_dev, const int32_t* positions_dev,
+                     int32_t inverse, void* out_dev, void* hip_stream);
+
+/* Masked attention of bf16 heads. Query row i of sequence b stands at position
+ * p = q_offset + i among the kv_len keys; head h reads key/value head
+ * h * kv_heads / heads.
+ *   z = scale q.k          z = cap tanh(z / cap) if cap > 0
+ *   s = z - slopes[h] |p - j|                           (slopes given)
+ *   key j is visible if   j < kv_lengths[b]             (given)
+ *                  and    j and p lie in one document   (documents given)
+ *                  and    j <= p or j < prefix[b]       (causal; prefix may be NULL: 0)
+ *   out = softmax over the visible keys (s) V           lse = ln sum exp(s)
+ * A row without a visible key has out 0, lse -infinity and no gradient. Keys
+ * at or past kv_lengths[b] are not read. Scores, softmax statistics and sums
+ * are float32; probabilities and score gradients are rounded to bf16 for their
+ * products, results once to bf16. Results do not depend on timing: no atomics.
+ *   documents   int32 [batch, kv_len]: a document is a run of equal numbers
+ *               (needs 0 <= q_offset and q_offset + q_len <= kv_len)
+ *   prefix, kv_lengths  int32 [batch], taken into [0, kv_len]
+ *   slopes      float32 [heads]
+ *   lse         float32 [batch, heads, q_len], contiguous
+ * head_dim: a multiple of 8 up to 128; batch * heads * ceil(length / 32) below
+ * 2^23 for both lengths. Strides are multiples of 8 elements and
+ * tensors 16-byte aligned. out may not overlap q, k, v; the gradients may not
+ * overlap each other or an input, but all of them may be parts of one packed
+ * tensor. */
+typedef struct {
+  uint32_t abi_version;      /* SPECTRAIN_ABI_VERSION */
+  int32_t dtype;             /* SPECTRAIN_BF16 */
+  int32_t batch, heads, kv_heads, head_dim;   /* heads a multiple of kv_heads */
+  int32_t q_len, kv_len;
+  int32_t q_offset;          /* position of the first query row */
+  int32_t causal;            /* 0 or 1; prefix needs 1 */
+  float scale;               /* finite */
+  float cap;                 /* 0: none; > 0 */
+  spectrain_strides q, k, v, out;
+  spectrain_strides dout, dq, dk, dv;   /* backward only */
+} spectrain_attention_desc;
+
+typedef struct {
+  const int32_t* documents;
+  const int32_t* prefix;
+  const int32_t* kv_lengths;
+  const float* slopes;
+} spectrain_attention_masks;   /* device pointers, each may be NULL */
+
+/* Bytes of workspace a forward or a backward needs (any masks and strides);
+ * 256-byte aligned memory of that size is given to the calls. */
+int spectrain_attention_workspace(const spectrain_attention_desc* desc, int32_t backward, size_t* bytes);
+
+/* masks may be NULL (none). lse_dev may be NULL when no backward follows. */
+int spectrain_attention_forward(const spectrain_attention_desc* desc, const spectrain_attention_masks* masks,
+                                const void* q_dev, const void* k_dev, const void* v_dev, void* out_dev,
+                                float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Gradients of q, k and v (overwritten) from the forward's inputs, masks, out
+ * and lse, and dout = dL/d out. */
+int spectrain_attention_backward(const spectrain_attention_desc* desc, const spectrain_attention_masks* masks,
+                                 const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
+                                 const float* lse_dev, const void* dout_dev, void* dq_dev, void* dk_dev, void* dv_dev,
+                                 void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Activation checkpoints in 8 bits. Every 32 consecutive values of a row (the
+ * last group of a row may be shorter) share the scale 2^(byte - 127), the
+ * smallest power of two (at least 2^-117) with max |x| / scale <= 448; a value
+ * is kept as the nearest e4m3 number of x / scale, ties to even. A value that
+ * is not zero keeps a code that is not zero (so the sign mask of a ReLU
+ * survives), a value that is not finite becomes NaN, and nothing finite
+ * becomes infinite: the largest code is the last one whose value is finite.
+ * codes: uint8 [rows, cols]; scales: uint8 [rows, ceil(cols / 32)], both
+ * contiguous; x and out: rows `ld` >= cols elements apart. rows *
+ * ceil(cols / 32) and cols are below 2^30. */
+int spectrain_checkpoint_pack(int32_t dtype, int64_t rows, int64_t cols, const void* x_dev, int64_t ld,
+                              uint8_t* codes_dev, uint8_t* scales_dev, void* hip_stream);
+int spectrain_checkpoint_restore(int32_t dtype, int64_t rows, int64_t cols, const uint8_t* codes_dev,
+                                 const uint8_t* scales_dev, void* out_dev, int64_t ld, void* hip_stream);
+
 /* Message of the last failed call on this host thread ("" if none). */
 const char* spectrain_last_error(void);
 

@@ -3,6 +3,7 @@
 #include <new>
 #include <string>
 
+#include "operators.hpp"
 #include "stage.hpp"
 
 struct spectrain_stage {
@@ -19,12 +20,9 @@ int set_error(int code, const std::string& msg) {
 }
 
 template <typename F>
-int guarded(spectrain_stage_t st, F&& f, bool check_flag = true) {
-  if (!st || !st->impl) return set_error(SPECTRAIN_EINVAL, "stage handle is NULL");
+int guarded(F&& f) {
   try {
-    if (check_flag && st->impl->nonfinite())
-      return set_error(SPECTRAIN_ENONFINITE, "an update produced a non-finite weight or smoothed gradient");
-    f(*st->impl);
+    f();
     g_last_error.clear();
     return SPECTRAIN_OK;
   } catch (const spx::StageError& e) {
@@ -36,6 +34,16 @@ int guarded(spectrain_stage_t st, F&& f, bool check_flag = true) {
   } catch (...) {
     return set_error(SPECTRAIN_EINVAL, "unknown failure");
   }
+}
+
+template <typename F>
+int guarded(spectrain_stage_t st, F&& f, bool check_flag = true) {
+  if (!st || !st->impl) return set_error(SPECTRAIN_EINVAL, "stage handle is NULL");
+  return guarded([&]() {
+    if (check_flag && st->impl->nonfinite())
+      throw spx::StageError(SPECTRAIN_ENONFINITE, "an update produced a non-finite weight or smoothed gradient");
+    f(*st->impl);
+  });
 }
 
 }  // namespace
@@ -140,6 +148,53 @@ int spectrain_stage_destroy(spectrain_stage_t st) {
   delete st;
   g_last_error.clear();
   return SPECTRAIN_OK;
+}
+
+int spectrain_rotary(const spectrain_rotary_desc* desc, const void* x_dev, const int32_t* positions_dev,
+                     int32_t inverse, void* out_dev, void* hip_stream) {
+  return guarded([&]() {
+    spx::run_rotary(desc, x_dev, positions_dev, inverse, out_dev, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int spectrain_attention_workspace(const spectrain_attention_desc* desc, int32_t backward, size_t* bytes) {
+  if (!bytes) return set_error(SPECTRAIN_EINVAL, "bytes is NULL");
+  return guarded([&]() { *bytes = spx::attention_workspace(desc, backward != 0); });
+}
+
+int spectrain_attention_forward(const spectrain_attention_desc* desc, const spectrain_attention_masks* masks,
+                                const void* q_dev, const void* k_dev, const void* v_dev, void* out_dev,
+                                float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  return guarded([&]() {
+    spx::run_attention_forward(desc, masks, q_dev, k_dev, v_dev, out_dev, lse_dev, workspace_dev, workspace_bytes,
+                               static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int spectrain_attention_backward(const spectrain_attention_desc* desc, const spectrain_attention_masks* masks,
+                                 const void* q_dev, const void* k_dev, const void* v_dev, const void* out_dev,
+                                 const float* lse_dev, const void* dout_dev, void* dq_dev, void* dk_dev, void* dv_dev,
+                                 void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  return guarded([&]() {
+    spx::run_attention_backward(desc, masks, q_dev, k_dev, v_dev, out_dev, lse_dev, dout_dev, dq_dev, dk_dev, dv_dev,
+                                workspace_dev, workspace_bytes, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int spectrain_checkpoint_pack(int32_t dtype, int64_t rows, int64_t cols, const void* x_dev, int64_t ld,
+                              uint8_t* codes_dev, uint8_t* scales_dev, void* hip_stream) {
+  return guarded([&]() {
+    spx::run_checkpoint(dtype, rows, cols, x_dev, ld, codes_dev, scales_dev, nullptr,
+                        static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int spectrain_checkpoint_restore(int32_t dtype, int64_t rows, int64_t cols, const uint8_t* codes_dev,
+                                 const uint8_t* scales_dev, void* out_dev, int64_t ld, void* hip_stream) {
+  return guarded([&]() {
+    spx::run_checkpoint(dtype, rows, cols, nullptr, ld, const_cast<uint8_t*>(codes_dev),
+                        const_cast<uint8_t*>(scales_dev), out_dev, static_cast<hipStream_t>(hip_stream));
+  });
 }
 
 const char* spectrain_last_error(void) { return g_last_error.c_str(); }

@@ -1,0 +1,576 @@
+// Masked attention with shared key/value heads, forward and backward.
+//
+// Every mask the interface has (causal with a prefix, documents, valid lengths)
+// leaves a row one interval of keys [lo, hi), and both ends only grow with the
+// row's position. So a tile is classified from its first and last row: skipped,
+// whole, or cut (only cut tiles compare columns), and no mask tensor exists.
+//
+// Rows are the queries of every head that shares a key/value head (row r: query
+// r / group, head r % group of the group), so one staging of a key tile serves
+// the whole group.
+#include "attention_tiles.hpp"
+
+namespace spx {
+namespace {
+
+constexpr int NT = 256, ROWS = 128, KT = 64;   // threads, rows of a block, keys (rows) of a staged tile
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+struct Args : AttentionArgs {
+  const int2* doc = nullptr;      // [batch][kv_len]: first and past-the-last token of the token's document
+  float* delta = nullptr;         // [batch][heads][q_len]: out . dout (backward)
+  float c1 = 0.0f;                // uncapped: scale log2(e); capped: 2 scale / cap log2(e)
+  float c2 = 0.0f;                // capped: cap log2(e)
+  FastDiv by_group, by_bh, by_kv;
+  int tiles = 0;
+};
+
+struct Sequence {
+  int limit, prefix;              // valid keys; keys every row sees (causal)
+  const int2* doc;
+  __device__ __forceinline__ Sequence(const Args& a, int b)
+      : limit(a.kv_lengths ? min(max(a.kv_lengths[b], 0), a.kv_len) : a.kv_len),
+        prefix(a.prefix ? min(max(a.prefix[b], 0), a.kv_len) : 0),
+        doc(a.doc ? a.doc + static_cast<long>(b) * a.kv_len : nullptr) {}
+  // Keys [x, y) that the row at position p sees (none if y <= x).
+  __device__ __forceinline__ int2 keys(const Args& a, int p) const {
+    int lo = 0, hi = limit;
+    if (a.causal) hi = min(hi, max(p + 1, prefix));
+    if (doc) {
+      const int2 d = doc[p];
+      lo = d.x;
+      hi = min(hi, d.y);
+    }
+    return make_int2(lo, hi);
+  }
+};
+
+// Score of one product in units of log2: s * log2(e), and tanh(z / cap).
+template <bool CAP>
+__device__ __forceinline__ float score(const Args& a, float acc, float& t) {
+  if constexpr (CAP) {
+    t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(acc * a.c1));
+    return t * a.c2;
+  } else {
+    return acc * a.c1;
+  }
+}
+
+// A thread's share of a KT x DH tile of rows (zero past `limit` rows and past
+// `dim` columns), and its copy into an LDS tile [KT][DH + 8].
+template <int DH>
+struct Tile {
+  static constexpr int C = DH / 8, V = KT * C / NT;
+  static_assert(KT * C % NT == 0, "whole accesses");
+  uint4 v[V];
+  template <typename F>
+  __device__ __forceinline__ void load(int first, int limit, int dim, int tid, F&& address) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int e = tid + NT * i, row = first + e / C, col = (e % C) * 8;
+      v[i] = make_uint4(0, 0, 0, 0);
+      if (row < limit && col < dim) v[i] = *reinterpret_cast<const uint4*>(address(row) + col);
+    }
+  }
+  __device__ __forceinline__ void store(bf16_t* dst, int tid) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int e = tid + NT * i;
+      *reinterpret_cast<uint4*>(dst + (e / C) * (DH + 8) + (e % C) * 8) = v[i];
+    }
+  }
+};
+
+template <int DH>
+__device__ __forceinline__ void load_row(const bf16_t* row, int dim, int lane, bf16x8_t (&f)[DH / 16]) {
+#pragma unroll
+  for (int q = 0; q < DH / 16; ++q) {
+    const int col = 16 * q + 8 * (lane >> 5);
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (col < dim) u = *reinterpret_cast<const uint4*>(row + col);
+    f[q] = __builtin_bit_cast(bf16x8_t, u);
+  }
+}
+
+// The wave's 32 rows (fragments fr) against rows c0 .. c0 + 31 of an LDS tile.
+template <int DH>
+__device__ __forceinline__ f32x16_t product(const bf16x8_t (&fr)[DH / 16], const bf16_t* tile, int c0, int lane) {
+  f32x16_t acc;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
+#pragma unroll
+  for (int q = 0; q < DH / 16; ++q)
+    acc = mfma(frag_rows<DH + 8>(tile, c0 + (lane & 31), 16 * q + 8 * (lane >> 5)), fr[q], acc);
+  return acc;
+}
+
+// acc += the group's values, rounded to bf16, times rows c0 .. of a [k][DH] tile.
+template <int DH>
+__device__ __forceinline__ void accumulate(const f32x16_t& v, const bf16_t* tile, int c0, int lane,
+                                           f32x16_t (&acc)[DH / 32]) {
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const uint4 u = make_uint4(pack_bf16x2(v[8 * c], v[8 * c + 1]), pack_bf16x2(v[8 * c + 2], v[8 * c + 3]),
+                               pack_bf16x2(v[8 * c + 4], v[8 * c + 5]), pack_bf16x2(v[8 * c + 6], v[8 * c + 7]));
+    const bf16x8_t fa = __builtin_bit_cast(bf16x8_t, u);
+#pragma unroll
+    for (int jn = 0; jn < DH / 32; ++jn)
+      acc[jn] = mfma(frag_cols<DH + 8>(tile, 32 * jn, c0 + 16 * c, lane), fa, acc[jn]);
+  }
+}
+
+// Row lane % 32 of a wave's 32 x DH result, times alpha, as bf16.
+template <int DH>
+__device__ __forceinline__ void store_row(bf16_t* out, int dim, const f32x16_t (&acc)[DH / 32], float alpha, int lane) {
+#pragma unroll
+  for (int jn = 0; jn < DH / 32; ++jn)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int col = 32 * jn + col_of(4 * g, lane);
+      if (col < dim)
+        *reinterpret_cast<uint2*>(out + col) =
+            make_uint2(pack_bf16x2(acc[jn][4 * g] * alpha, acc[jn][4 * g + 1] * alpha),
+                       pack_bf16x2(acc[jn][4 * g + 2] * alpha, acc[jn][4 * g + 3] * alpha));
+    }
+}
+
+// Documents: each token's run of equal numbers. A block owns 1024 tokens; runs
+// that cross its ends are followed outwards, a block's width at a time.
+constexpr int DT = 1024;
+__global__ __launch_bounds__(DT) void document_runs_kernel(const int32_t* ids, int len, FastDiv chunks, int2* runs) {
+  __shared__ int scan[2][DT];
+  __shared__ int edge[2];
+  const int b = chunks.div(blockIdx.x);
+  const int tid = threadIdx.x, first = (blockIdx.x - b * chunks.d) * DT, j = first + tid;
+  const int last = min(first + DT, len) - 1;
+  ids += static_cast<long>(b) * len;
+  runs += static_cast<long>(b) * len;
+  const bool in = j < len;
+  const int id = in ? ids[j] : 0;
+  // start of the first token's run: the first of the tokens before it that are all equal
+  int start = first;
+  for (int to = first; to > 0;) {
+    const int w = min(DT, to), base = to - w;
+    if (tid == 0) edge[0] = -1;
+    __syncthreads();
+    if (tid < w && ids[base + tid] != ids[first]) atomicMax(&edge[0], base + tid);
+    __syncthreads();
+    const int found = edge[0];
+    __syncthreads();
+    start = found < 0 ? base : found + 1;
+    if (found >= 0) break;
+    to = base;
+  }
+  int end = last + 1;
+  for (int from = last + 1; from < len;) {
+    const int w = min(DT, len - from);
+    if (tid == 0) edge[1] = 0x7fffffff;
+    __syncthreads();
+    if (tid < w && ids[from + tid] != ids[last]) atomicMin(&edge[1], from + tid);
+    __syncthreads();
+    const int found = edge[1];
+    __syncthreads();
+    end = found == 0x7fffffff ? from + w : found;
+    if (found != 0x7fffffff) break;
+    from += w;
+  }
+  // inside the block: the last start at or before a token, the first end after it
+  scan[0][tid] = tid == 0 ? start : (in && ids[j - 1] != id ? j : -1);
+  scan[1][tid] = j == last ? end : (in && j < last && ids[j + 1] != id ? j + 1 : 0x7fffffff);
+  __syncthreads();
+  for (int step = 1; step < DT; step *= 2) {
+    const int s = tid >= step ? scan[0][tid - step] : -1;
+    const int e = tid + step < DT ? scan[1][tid + step] : 0x7fffffff;
+    __syncthreads();
+    scan[0][tid] = max(scan[0][tid], s);
+    scan[1][tid] = min(scan[1][tid], e);
+    __syncthreads();
+  }
+  if (in) runs[j] = make_int2(scan[0][tid], scan[1][tid]);
+}
+
+// One block's place: its (sequence, kv head) and tile. Consecutive blocks take
+// different kv heads (of one XCD each where their number is a multiple of 8),
+// and the last rows first: they see the most keys under a causal mask.
+struct Block {
+  int b, kh, tile;
+  __device__ __forceinline__ Block(const Args& a) {
+    const uint32_t x = blockIdx.x, t = a.by_bh.div(x), bh = x - t * a.by_bh.d;
+    b = a.by_kv.div(bh);
+    kh = bh - b * a.kv_heads;
+    tile = a.tiles - 1 - static_cast<int>(t);
+  }
+};
+
+template <int DH, bool CAP>
+__global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
+  __shared__ __attribute__((aligned(16))) bf16_t Ks[KT * (DH + 8)];
+  __shared__ __attribute__((aligned(16))) bf16_t Vs[KT * (DH + 8)];
+  const Block at(a);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Sequence seq(a, at.b);
+  const int row0 = at.tile * ROWS + 32 * wave, row = min(row0 + (lane & 31), a.rows - 1);
+  const int i = a.by_group.div(row), head = at.kh * a.group + row - i * a.group, p = a.q_offset + i;
+  const int2 mine = seq.keys(a, p);
+  const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
+  const int2 wfirst = seq.keys(a, position(row0)), wlast = seq.keys(a, position(row0 + 31));
+  const int begin = seq.keys(a, position(at.tile * ROWS)).x / KT * KT;
+  const int end = seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y;
+  const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
+  bf16x8_t fq[DH / 16];
+  load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq);
+  const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
+  const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
+  const auto krow = [&](int j) { return k + j * a.sk.t; };
+  const auto vrow = [&](int j) { return v + j * a.sv.t; };
+
+  f32x16_t o[DH / 32];
+  zero(o);
+  float m = -INFINITY, sum = 0.0f;
+  Tile<DH> kr, vr;
+  kr.load(begin, seq.limit, a.dim, tid, krow);
+  vr.load(begin, seq.limit, a.dim, tid, vrow);
+  for (int k0 = begin; k0 < end; k0 += KT) {
+    __syncthreads();
+    kr.store(Ks, tid);
+    vr.store(Vs, tid);
+    __syncthreads();
+    kr.load(k0 + KT, seq.limit, a.dim, tid, krow);
+    vr.load(k0 + KT, seq.limit, a.dim, tid, vrow);
+    if (k0 >= wlast.y || k0 + KT <= wfirst.x) continue;
+    const bool cut = k0 < wlast.x || k0 + KT > wfirst.y;
+    f32x16_t s[KT / 32];
+    float top = m, t;
+#pragma unroll
+    for (int n = 0; n < KT / 32; ++n) {
+      s[n] = product<DH>(fq, Ks, 32 * n, lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[n][r] = score<CAP>(a, s[n][r], t);
+    }
+    if (a.slopes) {
+#pragma unroll
+      for (int n = 0; n < KT / 32; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[n][r] -= slope * fabsf(static_cast<float>(p - (k0 + 32 * n + col_of(r, lane))));
+    }
+    if (cut) {
+#pragma unroll
+      for (int n = 0; n < KT / 32; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = k0 + 32 * n + col_of(r, lane);
+          if (j < mine.x || j >= mine.y) s[n][r] = -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < KT / 32; ++n)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float base = top == -INFINITY ? 0.0f : top;   // nothing seen so far weighs zero
+    const float shrink = __builtin_amdgcn_exp2f(m - base);
+    m = top;
+    sum *= shrink;
+#pragma unroll
+    for (int jn = 0; jn < DH / 32; ++jn)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[jn][r] *= shrink;
+#pragma unroll
+    for (int n = 0; n < KT / 32; ++n) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - base);
+        sum += s[n][r];
+      }
+      accumulate<DH>(s[n], Vs, 32 * n, lane, o);
+    }
+  }
+  sum += __shfl_xor(sum, 32);
+  if (row0 + (lane & 31) >= a.rows) return;
+  store_row<DH>(a.out + at.b * a.so.b + i * a.so.t + head * a.so.h, a.dim, o, sum == 0.0f ? 0.0f : 1.0f / sum, lane);
+  if (a.lse && lane < 32)
+    a.lse[(static_cast<long>(at.b) * a.heads + head) * a.q_len + i] =
+        sum == 0.0f ? -INFINITY : m * LN2 + logf(sum);
+}
+
+// delta = out . dout of every row, 16 lanes a row.
+__global__ __launch_bounds__(NT) void attention_delta_kernel(Args a, long rows, FastDiv by_heads, FastDiv by_len) {
+  const long r = static_cast<long>(blockIdx.x) * (NT / 16) + threadIdx.x / 16;
+  if (r >= rows) return;   // whole 16-lane groups leave
+  const uint32_t t = by_heads.div(static_cast<uint32_t>(r)), h = static_cast<uint32_t>(r) - t * by_heads.d;
+  const uint32_t b = by_len.div(t), i = t - b * by_len.d;
+  const int col = (threadIdx.x % 16) * 8;
+  float s = 0.0f;
+  if (col < a.dim) {
+    const u16x8_t o = *reinterpret_cast<const u16x8_t*>(a.out + b * a.so.b + i * a.so.t + h * a.so.h + col);
+    const u16x8_t d = *reinterpret_cast<const u16x8_t*>(a.dout + b * a.sdo.b + i * a.sdo.t + h * a.sdo.h + col);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf(bf16_to_f32(o[e]), bf16_to_f32(d[e]), s);
+  }
+#pragma unroll
+  for (int w = 8; w >= 1; w /= 2) s += __shfl_xor(s, w);
+  if (threadIdx.x % 16 == 0) a.delta[(static_cast<long>(b) * a.heads + h) * a.q_len + i] = s;
+}
+
+// A row's statistics for the backward: log2 of its sum (infinite where the row
+// has no weight, so every probability is zero) and delta.
+__device__ __forceinline__ float2 row_stats(const Args& a, int b, int head, int i) {
+  const long at = (static_cast<long>(b) * a.heads + head) * a.q_len + i;
+  const float l = a.lse[at];
+  return make_float2(l == -INFINITY ? INFINITY : l * LOG2E, a.delta[at]);
+}
+
+template <int DH, bool CAP>
+__global__ __launch_bounds__(NT, DH > 64 ? 1 : 2) void attention_masked_dq_kernel(Args a) {
+  __shared__ __attribute__((aligned(16))) bf16_t Ks[KT * (DH + 8)];
+  __shared__ __attribute__((aligned(16))) bf16_t Vs[KT * (DH + 8)];
+  const Block at(a);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Sequence seq(a, at.b);
+  const int row0 = at.tile * ROWS + 32 * wave, row = min(row0 + (lane & 31), a.rows - 1);
+  const int i = a.by_group.div(row), head = at.kh * a.group + row - i * a.group, p = a.q_offset + i;
+  const int2 mine = seq.keys(a, p);
+  const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
+  const int2 wfirst = seq.keys(a, position(row0)), wlast = seq.keys(a, position(row0 + 31));
+  const int begin = seq.keys(a, position(at.tile * ROWS)).x / KT * KT;
+  const int end = seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y;
+  const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
+  bf16x8_t fq[DH / 16], fo[DH / 16];
+  load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq);
+  load_row<DH>(a.dout + at.b * a.sdo.b + i * a.sdo.t + head * a.sdo.h, a.dim, lane, fo);
+  const float2 st = row_stats(a, at.b, head, i);
+  const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
+  const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
+  const auto krow = [&](int j) { return k + j * a.sk.t; };
+  const auto vrow = [&](int j) { return v + j * a.sv.t; };
+
+  f32x16_t o[DH / 32];
+  zero(o);
+  Tile<DH> kr, vr;
+  kr.load(begin, seq.limit, a.dim, tid, krow);
+  vr.load(begin, seq.limit, a.dim, tid, vrow);
+  for (int k0 = begin; k0 < end; k0 += KT) {
+    __syncthreads();
+    kr.store(Ks, tid);
+    vr.store(Vs, tid);
+    __syncthreads();
+    kr.load(k0 + KT, seq.limit, a.dim, tid, krow);
+    vr.load(k0 + KT, seq.limit, a.dim, tid, vrow);
+    if (k0 >= wlast.y || k0 + KT <= wfirst.x) continue;
+    const bool cut = k0 < wlast.x || k0 + KT > wfirst.y;
+#pragma unroll
+    for (int n = 0; n < KT / 32; ++n) {
+      f32x16_t s = product<DH>(fq, Ks, 32 * n, lane);
+      const f32x16_t dp = product<DH>(fo, Vs, 32 * n, lane);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int j = k0 + 32 * n + col_of(r, lane);
+        float t = 0.0f, x = score<CAP>(a, s[r], t);
+        if (a.slopes) x -= slope * fabsf(static_cast<float>(p - j));
+        float e = __builtin_amdgcn_exp2f(x - st.x) * (dp[r] - st.y);
+        if (CAP) e *= 1.0f - t * t;
+        if (cut && (j < mine.x || j >= mine.y)) e = 0.0f;
+        s[r] = e;
+      }
+      accumulate<DH>(s, Ks, 32 * n, lane, o);
+    }
+  }
+  if (row0 + (lane & 31) >= a.rows) return;
+  store_row<DH>(a.dq + at.b * a.sdq.b + i * a.sdq.t + head * a.sdq.h, a.dim, o, a.scale, lane);
+}
+
+// dK and dV of 128 keys: the wave's own 32 are keys, the walked columns rows.
+template <int DH, bool CAP>
+__global__ __launch_bounds__(NT, DH > 64 ? 1 : 2) void attention_masked_dkv_kernel(Args a) {
+  __shared__ __attribute__((aligned(16))) bf16_t Qs[KT * (DH + 8)];
+  __shared__ __attribute__((aligned(16))) bf16_t Os[KT * (DH + 8)];
+  __shared__ __attribute__((aligned(16))) float ls[KT], ds[KT], sl[KT];   // log2 sum, delta, slope of the staged rows
+  __shared__ __attribute__((aligned(16))) int lo[KT], hi[KT], ps[KT];     // their keys and positions
+  const Block at(a);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Sequence seq(a, at.b);
+  const int key0 = at.tile * ROWS, wkey0 = key0 + 32 * wave, key = wkey0 + (lane & 31);
+  const int kc = min(key, a.kv_len - 1), valid = min(seq.limit, key0 + ROWS);
+  const bf16_t* q = a.q + at.b * a.sq.b + at.kh * a.group * a.sq.h;
+  const bf16_t* dout = a.dout + at.b * a.sdo.b + at.kh * a.group * a.sdo.h;
+  bf16x8_t fk[DH / 16], fv[DH / 16];
+  load_row<DH>(a.k + at.b * a.sk.b + kc * a.sk.t + at.kh * a.sk.h, kc < seq.limit ? a.dim : 0, lane, fk);
+  load_row<DH>(a.v + at.b * a.sv.b + kc * a.sv.t + at.kh * a.sv.h, kc < seq.limit ? a.dim : 0, lane, fv);
+  f32x16_t dk[DH / 32], dv[DH / 32];
+  zero(dk);
+  zero(dv);
+  // rows that see one of the block's keys: positions [pa, pb)
+  int pa = -(1 << 30), pb = 0x7fffffff;
+  if (a.causal && key0 >= seq.prefix) pa = key0;
+  if (seq.doc && key0 < valid) {
+    pa = max(pa, seq.doc[key0].x);
+    pb = seq.doc[valid - 1].y;
+  }
+  const long first = max(0L, static_cast<long>(pa) - a.q_offset) * a.group;
+  const int begin = static_cast<int>(min(first, static_cast<long>(a.rows))) / KT * KT;
+  const int end = key0 < valid ? static_cast<int>(min(max(static_cast<long>(pb) - a.q_offset, 0L) * a.group,
+                                                      static_cast<long>(a.rows)))
+                               : 0;
+  const auto split = [&](int r, int& i, int& g) {
+    i = a.by_group.div(r);
+    g = r - i * a.group;
+  };
+  const auto qrow = [&](int r) {
+    int i, g;
+    split(r, i, g);
+    return q + i * a.sq.t + g * a.sq.h;
+  };
+  const auto orow = [&](int r) {
+    int i, g;
+    split(r, i, g);
+    return dout + i * a.sdo.t + g * a.sdo.h;
+  };
+  Tile<DH> qr, dor;
+  float sm = INFINITY, sd = 0.0f, ss = 0.0f;
+  int2 sk = make_int2(0, 0);
+  int sp = 0;
+  const auto fetch = [&](int r0) {
+    qr.load(r0, a.rows, a.dim, tid, qrow);
+    dor.load(r0, a.rows, a.dim, tid, orow);
+    sm = INFINITY, sd = 0.0f, ss = 0.0f, sk = make_int2(0, 0), sp = 0;
+    if (tid < KT && r0 + tid < a.rows) {
+      int i, g;
+      split(r0 + tid, i, g);
+      const int head = at.kh * a.group + g;
+      const float2 st = row_stats(a, at.b, head, i);
+      sm = st.x, sd = st.y, sp = a.q_offset + i;
+      sk = seq.keys(a, sp);
+      if (a.slopes) ss = a.slopes[head] * LOG2E;
+    }
+  };
+  fetch(begin);
+  for (int r0 = begin; r0 < end; r0 += KT) {
+    __syncthreads();
+    qr.store(Qs, tid);
+    dor.store(Os, tid);
+    if (tid < KT) {
+      ls[tid] = sm, ds[tid] = sd, sl[tid] = ss;
+      lo[tid] = sk.x, hi[tid] = sk.y, ps[tid] = sp;
+    }
+    __syncthreads();
+    fetch(r0 + KT);
+    if (wkey0 >= valid) continue;
+    // rows past the last are staged with an infinite sum: they weigh zero
+    const int tail = min(KT, a.rows - r0) - 1;
+    if (wkey0 >= hi[tail] || wkey0 + 32 <= lo[0]) continue;
+    const bool cut = wkey0 < lo[tail] || wkey0 + 32 > hi[0];
+#pragma unroll
+    for (int n = 0; n < KT / 32; ++n) {
+      f32x16_t s = product<DH>(fk, Qs, 32 * n, lane);
+      f32x16_t dp = product<DH>(fv, Os, 32 * n, lane);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int c = 32 * n + col_of(4 * g, lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * g + e;
+          float t = 0.0f, x = score<CAP>(a, s[r], t);
+          if (a.slopes) x -= sl[c + e] * fabsf(static_cast<float>(ps[c + e] - key));
+          float pr = __builtin_amdgcn_exp2f(x - ls[c + e]);
+          float z = pr * (dp[r] - ds[c + e]);
+          if (CAP) z *= 1.0f - t * t;
+          if (cut && (key < lo[c + e] || key >= hi[c + e])) pr = z = 0.0f;   // also where dP is not finite
+          s[r] = pr;
+          dp[r] = z;
+        }
+      }
+      accumulate<DH>(s, Os, 32 * n, lane, dv);
+      accumulate<DH>(dp, Qs, 32 * n, lane, dk);
+    }
+  }
+  if (key >= a.kv_len) return;
+  store_row<DH>(a.dk + at.b * a.sdk.b + key * a.sdk.t + at.kh * a.sdk.h, a.dim, dk, a.scale, lane);
+  store_row<DH>(a.dv + at.b * a.sdv.b + key * a.sdv.t + at.kh * a.sdv.h, a.dim, dv, 1.0f, lane);
+}
+
+size_t round256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
+size_t doc_bytes(const AttentionArgs& a) { return round256(static_cast<size_t>(a.batch) * a.kv_len * sizeof(int2)); }
+size_t delta_bytes(const AttentionArgs& a) {
+  return round256(static_cast<size_t>(a.batch) * a.heads * a.q_len * sizeof(float));
+}
+
+// Launch-independent values, and the document runs if there are documents.
+hipError_t prepare(const AttentionArgs& in, Args& a, hipStream_t s) {
+  static_cast<AttentionArgs&>(a) = in;
+  a.by_group = FastDiv(in.group);
+  a.by_bh = FastDiv(in.batch * in.kv_heads);
+  a.by_kv = FastDiv(in.kv_heads);
+  a.c1 = in.cap > 0.0f ? 2.0f * in.scale / in.cap * LOG2E : in.scale * LOG2E;
+  a.c2 = in.cap * LOG2E;
+  if (!in.documents || in.kv_len == 0) return hipSuccess;
+  int2* runs = reinterpret_cast<int2*>(in.ws);
+  a.doc = runs;
+  const unsigned chunks = (in.kv_len + DT - 1) / DT;
+  hipLaunchKernelGGL(document_runs_kernel, dim3(chunks * in.batch), dim3(DT), 0, s, in.documents, in.kv_len,
+                     FastDiv(chunks), runs);
+  return hipGetLastError();
+}
+
+// Calls f with the smallest compiled head width that holds dim, and the cap.
+template <typename F>
+void with_width(int dim, bool cap, F&& f) {
+  auto pick = [&](auto width) {
+    if (cap) f(width, std::true_type{});
+    else f(width, std::false_type{});
+  };
+  if (dim <= 32) pick(std::integral_constant<int, 32>{});
+  else if (dim <= 64) pick(std::integral_constant<int, 64>{});
+  else if (dim <= 96) pick(std::integral_constant<int, 96>{});
+  else pick(std::integral_constant<int, 128>{});
+}
+
+}  // namespace
+
+size_t attention_ws_bytes(const AttentionArgs& a, bool backward) {
+  return doc_bytes(a) + (backward ? delta_bytes(a) : 0);
+}
+
+hipError_t attention_masked_fwd(const AttentionArgs& in, hipStream_t s) {
+  if (in.batch == 0 || in.q_len == 0) return hipSuccess;
+  Args a;
+  hipError_t e = prepare(in, a, s);
+  if (e != hipSuccess) return e;
+  a.tiles = (a.rows + ROWS - 1) / ROWS;
+  with_width(a.dim, a.cap > 0.0f, [&](auto width, auto cap) {
+    hipLaunchKernelGGL((attention_masked_fwd_kernel<width(), cap()>),
+                       dim3(static_cast<unsigned>(a.tiles) * a.batch * a.kv_heads), dim3(NT), 0, s, a);
+    e = hipGetLastError();
+  });
+  return e;
+}
+
+hipError_t attention_masked_bwd(const AttentionArgs& in, hipStream_t s) {
+  if (in.batch == 0) return hipSuccess;
+  Args a;
+  hipError_t e = prepare(in, a, s);
+  if (e != hipSuccess) return e;
+  a.delta = reinterpret_cast<float*>(in.ws + doc_bytes(in));
+  if (a.q_len > 0) {
+    const long rows = static_cast<long>(a.batch) * a.q_len * a.heads;
+    hipLaunchKernelGGL(attention_delta_kernel, dim3(static_cast<unsigned>((rows + NT / 16 - 1) / (NT / 16))), dim3(NT),
+                       0, s, a, rows, FastDiv(a.heads), FastDiv(a.q_len));
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  with_width(a.dim, a.cap > 0.0f, [&](auto width, auto cap) {
+    if (a.q_len > 0) {
+      a.tiles = (a.rows + ROWS - 1) / ROWS;
+      hipLaunchKernelGGL((attention_masked_dq_kernel<width(), cap()>),
+                         dim3(static_cast<unsigned>(a.tiles) * a.batch * a.kv_heads), dim3(NT), 0, s, a);
+      if ((e = hipGetLastError()) != hipSuccess) return;
+    }
+    if (a.kv_len == 0) return;
+    a.tiles = (a.kv_len + ROWS - 1) / ROWS;
+    hipLaunchKernelGGL((attention_masked_dkv_kernel<width(), cap()>),
+                       dim3(static_cast<unsigned>(a.tiles) * a.batch * a.kv_heads), dim3(NT), 0, s, a);
+    e = hipGetLastError();
+  });
+  return e;
+}
+
+}  // namespace spx

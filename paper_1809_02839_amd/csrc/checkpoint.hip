@@ -1,0 +1,183 @@
+// Activation checkpoints in 8 bits: e4m3 codes with a power-of-two scale for
+// every 32 consecutive values of a row.
+//
+// Both directions are one pass bound by memory: 2 + 1 + 1/32 bytes a bf16 value.
+// Four lanes hold a group, eight values each, so a group's largest magnitude
+// takes two exchanges between lanes and no LDS. A power of two makes the scaling
+// itself exact: the only rounding is the code's (four significant bits, half a
+// step 2^-4 of the value).
+#include "kernels.hpp"
+
+namespace spx {
+namespace {
+
+constexpr int NT = 256, PER = 8, LANES = CHECKPOINT_GROUP / PER;
+
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+
+struct Place {
+  long row, col;   // first value of the lane's eight
+  int n;           // of them inside the row
+  bool live;
+};
+
+__device__ __forceinline__ Place place(long groups_total, FastDiv groups, long cols) {
+  const long unit = static_cast<long>(blockIdx.x) * NT + threadIdx.x, g = unit / LANES;
+  const bool live = g < groups_total;
+  const uint32_t gi = live ? static_cast<uint32_t>(g) : 0u, row = groups.div(gi);
+  Place p;
+  p.row = row;
+  p.col = static_cast<long>(gi - row * groups.d) * CHECKPOINT_GROUP + (threadIdx.x % LANES) * PER;
+  p.n = static_cast<int>(min(max(cols - p.col, 0L), static_cast<long>(PER)));
+  p.live = live;
+  return p;
+}
+
+template <typename T>
+__device__ __forceinline__ float to_float(T v) {
+  if constexpr (sizeof(T) == 2) return bf16_to_f32(v);
+  else return v;
+}
+
+// WIDE: every lane's eight values are whole and 16-byte aligned.
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(NT) void checkpoint_pack_kernel(CheckpointArgs a, long total, FastDiv groups) {
+  const Place p = place(total, groups, a.cols);
+  const T* x = static_cast<const T*>(a.x) + p.row * a.ld + p.col;
+  float v[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) v[i] = 0.0f;
+  if (WIDE) {
+    if (p.live && p.n) {
+      if constexpr (sizeof(T) == 2) {
+        const u16x8_t u = *reinterpret_cast<const u16x8_t*>(x);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = bf16_to_f32(u[i]);
+      } else {
+        const float4 u = *reinterpret_cast<const float4*>(x), w = *reinterpret_cast<const float4*>(x + 4);
+        v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w, v[4] = w.x, v[5] = w.y, v[6] = w.z, v[7] = w.w;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (p.live && i < p.n) v[i] = to_float(x[i]);
+  }
+  uint32_t top = 0;   // bits of the largest finite magnitude: ordered as the values
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu;
+    if (m < 0x7f800000u) top = max(top, m);
+  }
+  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
+  top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
+  // smallest e with top / 2^e <= 448 = 1.75 * 2^8
+  const int e = min(max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u), -117), 120);
+  const float inv = power_of_two(-e), limit = e == 120 ? 240.0f : 448.0f;   // 256 * 2^120 would be infinite
+  uint32_t word[2];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    float z[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float t = v[4 * w + i], y = fminf(fmaxf(t * inv, -limit), limit);
+      z[i] = (__float_as_uint(t) & 0x7fffffffu) < 0x7f800000u ? y : __uint_as_float(0x7fc00000u);
+    }
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], c, true);
+    uint32_t u = static_cast<uint32_t>(c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {   // what is not zero stays so
+      const bool lost = (u >> (8 * i) & 0x7fu) == 0 && (__float_as_uint(v[4 * w + i]) & 0x7fffffffu) != 0;
+      u |= lost ? 1u << (8 * i) : 0u;
+      u |= lost && v[4 * w + i] < 0.0f ? 0x80u << (8 * i) : 0u;
+    }
+    word[w] = u;
+  }
+  if (!p.live) return;
+  uint8_t* out = a.codes + p.row * a.cols + p.col;
+  if (WIDE) {
+    if (p.n) *reinterpret_cast<uint2*>(out) = make_uint2(word[0], word[1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (i < p.n) out[i] = static_cast<uint8_t>(word[i / 4] >> (8 * (i % 4)));
+  }
+  if (threadIdx.x % LANES == 0)
+    a.scales[p.row * groups.d + p.col / CHECKPOINT_GROUP] = static_cast<uint8_t>(e + 127);
+}
+
+template <typename T, bool WIDE>
+__global__ __launch_bounds__(NT) void checkpoint_restore_kernel(CheckpointArgs a, long total, FastDiv groups) {
+  const Place p = place(total, groups, a.cols);
+  if (!p.live || p.n == 0) return;
+  const uint8_t* codes = a.codes + p.row * a.cols + p.col;
+  const float scale =
+      __uint_as_float(static_cast<uint32_t>(a.scales[p.row * groups.d + p.col / CHECKPOINT_GROUP]) << 23);
+  uint32_t word[2] = {0u, 0u};
+  if (WIDE) {
+    const uint2 u = *reinterpret_cast<const uint2*>(codes);
+    word[0] = u.x, word[1] = u.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (i < p.n) word[i / 4] |= static_cast<uint32_t>(codes[i]) << (8 * (i % 4));
+  }
+  float v[PER];
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const f32x2_t lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(word[w]), false);
+    const f32x2_t hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(word[w]), true);
+    v[4 * w] = lo[0] * scale;
+    v[4 * w + 1] = lo[1] * scale;
+    v[4 * w + 2] = hi[0] * scale;
+    v[4 * w + 3] = hi[1] * scale;
+  }
+  T* out = static_cast<T*>(a.out) + p.row * a.ld + p.col;
+  if (WIDE) {
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                  pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    } else {
+      *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
+      *reinterpret_cast<float4*>(out + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (i >= p.n) continue;
+      if constexpr (sizeof(T) == 2) out[i] = f32_to_bf16(v[i]);
+      else out[i] = v[i];
+    }
+  }
+}
+
+bool wide(const CheckpointArgs& a, const void* t) {
+  return a.cols % PER == 0 && a.ld % PER == 0 && reinterpret_cast<uintptr_t>(t) % 16 == 0 &&
+         reinterpret_cast<uintptr_t>(a.codes) % 8 == 0;
+}
+
+template <typename K>
+hipError_t launch(K* kernel, const CheckpointArgs& a, hipStream_t s) {
+  const long groups = (a.cols + CHECKPOINT_GROUP - 1) / CHECKPOINT_GROUP, total = a.rows * groups;
+  const long blocks = (total * LANES + NT - 1) / NT;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(NT), 0, s, a, total,
+                     FastDiv(static_cast<uint32_t>(groups)));
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t checkpoint_pack(const CheckpointArgs& a, int dtype, hipStream_t s) {
+  const bool w = wide(a, a.x);
+  if (dtype) return launch(w ? checkpoint_pack_kernel<bf16_t, true> : checkpoint_pack_kernel<bf16_t, false>, a, s);
+  return launch(w ? checkpoint_pack_kernel<float, true> : checkpoint_pack_kernel<float, false>, a, s);
+}
+
+hipError_t checkpoint_restore(const CheckpointArgs& a, int dtype, hipStream_t s) {
+  const bool w = wide(a, a.out);
+  if (dtype) return launch(w ? checkpoint_restore_kernel<bf16_t, true> : checkpoint_restore_kernel<bf16_t, false>, a, s);
+  return launch(w ? checkpoint_restore_kernel<float, true> : checkpoint_restore_kernel<float, false>, a, s);
+}
+
+}  // namespace spx

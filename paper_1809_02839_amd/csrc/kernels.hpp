@@ -152,6 +152,54 @@ hipError_t attention_long_probs(const bf16_t* qkv, const float* stats, int batch
 hipError_t attention_long_bwd(const bf16_t* qkv, const bf16_t* dctx, const float* stats, int batch, int S, int heads,
                               int d, float scale, float* dots, bf16_t* dqkv, hipStream_t s);
 
+// Rotary positions (rotary.hip): the first `rot` of each head's `dim` values as
+// pairs, turned by position * turns[pair] of a full turn.
+struct RotaryArgs {
+  const void* x = nullptr;
+  void* out = nullptr;
+  const int32_t* positions = nullptr;   // [rows], or NULL: first + row % tokens
+  int first = 0, tokens = 0, rows = 0, heads = 0, dim = 0, rot = 0;   // rows = batch * tokens
+  long xb = 0, xt = 0, xh = 0, ob = 0, ot = 0, oh = 0;                // strides: sequence, token, head
+  int interleaved = 0;
+  float sign = 1.0f, magnitude = 1.0f;
+  double turns[128];
+};
+hipError_t rotary(const RotaryArgs& a, int dtype, hipStream_t s);
+
+// Masked attention (attention_masked.hip). Rows are query rows by the heads
+// that share a key/value head: row r of (sequence, kv head) is query r / group
+// of head kv_head * group + r % group.
+struct AttentionArgs {
+  struct Strides {
+    long b = 0, t = 0, h = 0;
+  };
+  const bf16_t *q = nullptr, *k = nullptr, *v = nullptr, *dout = nullptr;
+  bf16_t *out = nullptr, *dq = nullptr, *dk = nullptr, *dv = nullptr;
+  float* lse = nullptr;                 // [batch][heads][q_len]
+  char* ws = nullptr;
+  const int32_t *documents = nullptr, *prefix = nullptr, *kv_lengths = nullptr;
+  const float* slopes = nullptr;
+  Strides sq, sk, sv, so, sdo, sdq, sdk, sdv;
+  int batch = 0, heads = 0, kv_heads = 0, group = 1, dim = 0, q_len = 0, kv_len = 0, q_offset = 0;
+  int rows = 0;                         // q_len * group
+  int causal = 0;
+  float scale = 1.0f, cap = 0.0f;
+};
+size_t attention_ws_bytes(const AttentionArgs& a, bool backward);
+hipError_t attention_masked_fwd(const AttentionArgs& a, hipStream_t s);
+hipError_t attention_masked_bwd(const AttentionArgs& a, hipStream_t s);
+
+// 8-bit activation checkpoints (checkpoint.hip).
+constexpr int CHECKPOINT_GROUP = 32;    // values that share a scale
+struct CheckpointArgs {
+  const void* x = nullptr;              // pack
+  void* out = nullptr;                  // restore
+  uint8_t *codes = nullptr, *scales = nullptr;
+  long rows = 0, cols = 0, ld = 0;      // ld: elements between rows of x or out
+};
+hipError_t checkpoint_pack(const CheckpointArgs& a, int dtype, hipStream_t s);
+hipError_t checkpoint_restore(const CheckpointArgs& a, int dtype, hipStream_t s);
+
 // Row chunking of the two-pass column reductions (column sums, layer-norm
 // parameter gradients) and the float32 workspace each pass needs.
 constexpr int COLSUM_ROWS = 64;   // rows summed per block in the first pass

@@ -28,7 +28,12 @@ EXPORTED = ("spectrain_version_difference", "spectrain_stage_create", "spectrain
             "spectrain_stage_backward_noalloc", "spectrain_stage_forward_backward",
             "spectrain_stage_update", "spectrain_stage_get_state", "spectrain_stage_set_state",
             "spectrain_stage_get_predicted", "spectrain_stage_profile", "spectrain_stage_profile_read",
-            "spectrain_stage_read_stash", "spectrain_stage_destroy", "spectrain_last_error")
+            "spectrain_stage_read_stash", "spectrain_stage_destroy", "spectrain_rotary",
+            "spectrain_attention_workspace", "spectrain_attention_forward", "spectrain_attention_backward",
+            "spectrain_checkpoint_pack", "spectrain_checkpoint_restore", "spectrain_last_error")
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
+CHECKPOINT_GROUP = 32
 
 
 class StageDesc(ctypes.Structure):
@@ -42,6 +47,28 @@ class KernelStat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 48), ("launches", ctypes.c_int64), ("ms_total", ctypes.c_double),
                 ("flops_total", ctypes.c_double), ("bytes_total", ctypes.c_double),
                 ("extra_bytes_total", ctypes.c_double)]
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in (
+        "dtype", "batch", "tokens", "heads", "head_dim", "rotary_dim", "layout", "scaling", "original_length",
+        "first_position", "reserved")] + [("base", ctypes.c_double), ("factor", ctypes.c_double), ("x", Strides),
+                                          ("out", Strides)]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in (
+        "dtype", "batch", "heads", "kv_heads", "head_dim", "q_len", "kv_len", "q_offset", "causal")] + [
+        ("scale", ctypes.c_float), ("cap", ctypes.c_float)] + [
+        (n, Strides) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+
+
+class AttentionMasks(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("documents", "prefix", "kv_lengths", "slopes")]
 
 
 class SpecTrainError(RuntimeError):
@@ -80,6 +107,14 @@ def lib():
                                                             ctypes.POINTER(i32)]),
             "spectrain_stage_read_stash": (ctypes.c_int, [vp, i64, i32, vp, sz, ctypes.POINTER(sz)]),
             "spectrain_stage_destroy": (ctypes.c_int, [vp]),
+            "spectrain_rotary": (ctypes.c_int, [ctypes.POINTER(RotaryDesc), vp, vp, i32, vp, vp]),
+            "spectrain_attention_workspace": (ctypes.c_int, [ctypes.POINTER(AttentionDesc), i32, ctypes.POINTER(sz)]),
+            "spectrain_attention_forward": (ctypes.c_int, [ctypes.POINTER(AttentionDesc),
+                                                           ctypes.POINTER(AttentionMasks)] + [vp] * 6 + [sz, vp]),
+            "spectrain_attention_backward": (ctypes.c_int, [ctypes.POINTER(AttentionDesc),
+                                                            ctypes.POINTER(AttentionMasks)] + [vp] * 10 + [sz, vp]),
+            "spectrain_checkpoint_pack": (ctypes.c_int, [i32, i64, i64, vp, i64, vp, vp, vp]),
+            "spectrain_checkpoint_restore": (ctypes.c_int, [i32, i64, i64, vp, vp, vp, i64, vp]),
             "spectrain_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -252,3 +287,188 @@ class Stage:
             self.destroy()
         except Exception:
             pass
+
+
+# ---- operators ----
+
+def _dtype_code(t, what):
+    name = str(t.dtype)
+    if name == "torch.bfloat16":
+        return BF16
+    if name == "torch.float32":
+        return FP32
+    raise ValueError(f"{what} must be torch.bfloat16 or torch.float32, got {t.dtype}")
+
+
+def _on(device, stream, call):
+    """call(stream pointer) with `device` current, on `stream` (None: the device's current torch stream)."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError("operators take GPU tensors")
+    if device.index == torch.cuda.current_device():
+        raw = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+        _check(call(raw))
+        return
+    with torch.cuda.device(device):
+        raw = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+        _check(call(raw))
+
+
+def _heads4(t, shape, dtype, device, what):
+    """Pointer of a [batch, token, head, head_dim] tensor, after its checks."""
+    if t.device != device:
+        raise ValueError(f"{what} must be on {device}, got {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if shape[3] > 1 and t.stride(3) != 1:
+        raise ValueError(f"{what} must be contiguous in its last dimension")
+    return t.data_ptr()
+
+
+def _side(t, shape, dtype, device, what):
+    """Pointer of a contiguous side input (None: absent)."""
+    if t is None:
+        return None
+    if t.device != device or str(t.dtype) != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous {dtype} {tuple(shape)} on {device}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+class Rotary:
+    """Rotary positions of heads of one width (spectrain_rotary): layout "half"
+    or "interleaved"; scaling "none", "linear", "ntk" or "parts"."""
+
+    def __init__(self, head_dim, rotary_dim=None, layout="half", base=10000.0, scaling="none", factor=1.0,
+                 original_length=0):
+        d = RotaryDesc()
+        d.abi_version = ABI_VERSION
+        d.head_dim = head_dim
+        d.rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        d.layout, d.scaling = ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling]
+        d.base, d.factor, d.original_length = base, factor, original_length
+        self._d, self._layout = d, None
+
+    def apply(self, x, out=None, positions=None, first_position=0, inverse=False, stream=None):
+        """Turn x [batch, token, head, head_dim] into out (None: in place; any
+        strides with a contiguous last dimension). positions: int32 [batch,
+        token], else first_position + token. Returns out."""
+        out = x if out is None else out
+        if x.dim() != 4 or x.shape[3] != self._d.head_dim:
+            raise ValueError(f"x must be [batch, token, head, {self._d.head_dim}], got {tuple(x.shape)}")
+        xp = _heads4(x, x.shape, x.dtype, x.device, "x")
+        op = _heads4(out, x.shape, x.dtype, x.device, "out")
+        pp = _side(positions, x.shape[:2], "torch.int32", x.device, "positions")
+        d, layout = self._d, (x.shape, x.stride(), out.stride(), x.dtype)
+        if layout != self._layout:
+            d.dtype = _dtype_code(x, "x")
+            d.batch, d.tokens, d.heads = x.shape[:3]
+            d.x, d.out = Strides(*x.stride()[:3]), Strides(*out.stride()[:3])
+            self._layout = layout
+        d.first_position = first_position
+        _on(x.device, stream, lambda s: lib().spectrain_rotary(ctypes.byref(d), xp, pp, int(bool(inverse)), op, s))
+        return out
+
+
+class Attention:
+    """Masked attention of one shape (spectrain_attention_forward and
+    _backward). Tensors are [batch, token, head, head_dim] bf16 with any strides
+    whose last is 1; scale None is 1 / sqrt(head_dim). The masks (each may be
+    None) are documents int32 [batch, kv_len], prefix and kv_lengths int32
+    [batch], slopes float32 [heads]."""
+
+    def __init__(self, batch, heads, kv_heads, head_dim, q_len, kv_len, causal=False, q_offset=0, scale=None, cap=0.0):
+        d = AttentionDesc()
+        d.abi_version, d.dtype = ABI_VERSION, BF16
+        d.batch, d.heads, d.kv_heads, d.head_dim, d.q_len, d.kv_len = batch, heads, kv_heads, head_dim, q_len, kv_len
+        d.q_offset, d.causal = q_offset, int(bool(causal))
+        d.scale = head_dim ** -0.5 if scale is None else scale
+        d.cap = cap
+        self._d = d
+        self._layout = {}
+        self._qs, self._ks = (batch, q_len, heads, head_dim), (batch, kv_len, kv_heads, head_dim)
+
+    def workspace_bytes(self, backward=False):
+        n = ctypes.c_size_t()
+        _check(lib().spectrain_attention_workspace(ctypes.byref(self._d), int(bool(backward)), ctypes.byref(n)))
+        return n.value
+
+    def workspace(self, backward=False, device="cuda"):
+        """A workspace for this shape's calls: one for calls that follow each other on a stream."""
+        import torch
+        return torch.empty(max(256, self.workspace_bytes(backward)), dtype=torch.uint8, device=device)
+
+    def _tensor(self, name, t, shape, q):
+        import torch
+        p = _heads4(t, shape, torch.bfloat16, q.device, name)
+        st = t.stride()
+        if self._layout.get(name) != st:
+            setattr(self._d, name, Strides(*st[:3]))
+            self._layout[name] = st
+        return p
+
+    def _masks(self, device, documents, prefix, kv_lengths, slopes):
+        d = self._d
+        return AttentionMasks(_side(documents, (d.batch, d.kv_len), "torch.int32", device, "documents"),
+                              _side(prefix, (d.batch,), "torch.int32", device, "prefix"),
+                              _side(kv_lengths, (d.batch,), "torch.int32", device, "kv_lengths"),
+                              _side(slopes, (d.heads,), "torch.float32", device, "slopes"))
+
+    def _scratch(self, workspace, device):
+        if workspace.device != device or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be contiguous and on {device}")
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+    def forward(self, q, k, v, out, lse=None, *, workspace, documents=None, prefix=None, kv_lengths=None, slopes=None,
+                stream=None):
+        """out = attention(q, k, v); lse float32 [batch, heads, q_len] as the backward takes it (None: not wanted)."""
+        dev, d = q.device, self._d
+        ptr = [self._tensor(n, t, s, q) for n, t, s in (("q", q, self._qs), ("k", k, self._ks), ("v", v, self._ks),
+                                                        ("out", out, self._qs))]
+        lp = _side(lse, (d.batch, d.heads, d.q_len), "torch.float32", dev, "lse")
+        m = self._masks(dev, documents, prefix, kv_lengths, slopes)
+        wp, wn = self._scratch(workspace, dev)
+        _on(dev, stream, lambda s: lib().spectrain_attention_forward(ctypes.byref(d), ctypes.byref(m), *ptr, lp, wp, wn,
+                                                                     s))
+
+    def backward(self, q, k, v, out, lse, dout, dq, dk, dv, *, workspace, documents=None, prefix=None, kv_lengths=None,
+                 slopes=None, stream=None):
+        """dq, dk, dv (overwritten) from the forward's tensors and masks and dout."""
+        dev, d = q.device, self._d
+        qs, ks = self._qs, self._ks
+        ptr = {n: self._tensor(n, t, s, q) for n, t, s in (
+            ("q", q, qs), ("k", k, ks), ("v", v, ks), ("out", out, qs), ("dout", dout, qs), ("dq", dq, qs),
+            ("dk", dk, ks), ("dv", dv, ks))}
+        lp = _side(lse, (d.batch, d.heads, d.q_len), "torch.float32", dev, "lse")
+        m = self._masks(dev, documents, prefix, kv_lengths, slopes)
+        wp, wn = self._scratch(workspace, dev)
+        _on(dev, stream, lambda s: lib().spectrain_attention_backward(
+            ctypes.byref(d), ctypes.byref(m), ptr["q"], ptr["k"], ptr["v"], ptr["out"], lp, ptr["dout"], ptr["dq"],
+            ptr["dk"], ptr["dv"], wp, wn, s))
+
+
+def _checkpoint_args(t, codes, scales, what):
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what} must be [rows, cols] with a contiguous last dimension")
+    rows, cols = t.shape
+    cp = _side(codes, (rows, cols), "torch.uint8", t.device, "codes")
+    sp = _side(scales, (rows, -(-cols // CHECKPOINT_GROUP)), "torch.uint8", t.device, "scales")
+    if cp is None or sp is None:
+        raise ValueError("codes and scales must be given")
+    return _dtype_code(t, what), rows, cols, cp, sp, t.stride(0) if rows > 1 else max(cols, 1)
+
+
+def checkpoint_pack(x, codes, scales, stream=None):
+    """x [rows, cols] to 8-bit codes uint8 [rows, cols] and scales uint8 [rows, ceil(cols / 32)]."""
+    dt, rows, cols, cp, sp, ld = _checkpoint_args(x, codes, scales, "x")
+    xp = x.data_ptr()
+    _on(x.device, stream, lambda s: lib().spectrain_checkpoint_pack(dt, rows, cols, xp, ld, cp, sp, s))
+
+
+def checkpoint_restore(codes, scales, out, stream=None):
+    """The values that codes and scales stand for, into out [rows, cols]."""
+    dt, rows, cols, cp, sp, ld = _checkpoint_args(out, codes, scales, "out")
+    op = out.data_ptr()
+    _on(out.device, stream, lambda s: lib().spectrain_checkpoint_restore(dt, rows, cols, cp, sp, op, ld, s))

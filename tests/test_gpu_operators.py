@@ -1,0 +1,491 @@
+"""GPU: the stand-alone operators against plain implementations in 64 bits.
+
+Tolerances are bounds, not measured values. A bf16 rounding is off by at most
+2^-8 of the value, an e4m3 one is exact by definition here.
+  rotary      the turn's angle is a float in half turns: off by pi 2^-24, its
+              sine and cosine by two steps of 2^-24, and four float32 roundings:
+              below 8e-7 (|a| + |b|) a value.
+  attention   probabilities are rounded once: 2^-8 sum P |v|, then the result:
+              2^-8 |out|. Scores are float32 sums of `dim` products, so a
+              probability is off by a factor exp(+-2 E), E the bound on a score.
+  gradients   the same with dS = P (dP - delta): P by 2 E, delta by the
+              forward's bound on out times |dout|, one rounding of P and of dS,
+              one of the result.
+"""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+BF = 2.0 ** -8     # half a step of bf16, relative
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _randn(shape, g, dtype=torch.bfloat16, scale=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+# ------------------------------------------------------------------ rotary ----
+
+def _turned(x, pos, rot, layout, base, scaling, factor, original, inverse):
+    """Float64, pair by pair from the definition; also |a| + |b| of each value's pair."""
+    x = x.double()
+    i = torch.arange(rot // 2, device=x.device, dtype=torch.float64)
+    if scaling == "ntk" and rot > 2:
+        base = base * factor ** (rot / (rot - 2))
+    w = base ** (-2 * i / rot)
+    m = 1.0
+    if scaling == "linear":
+        w = w / factor
+    if scaling == "parts":
+        keep = ((original * w / (2 * math.pi) - 1) / 31).clamp(0, 1)
+        w = w * keep + w / factor * (1 - keep)
+        m = 0.1 * math.log(factor) + 1
+    t = pos.double()[:, :, None, None] * w * (-1 if inverse else 1)
+    first, second = (slice(0, rot // 2), slice(rot // 2, rot)) if layout == "half" else (slice(0, rot, 2),
+                                                                                          slice(1, rot, 2))
+    a, b = x[..., first], x[..., second]
+    out, size = x.clone(), torch.zeros_like(x)
+    out[..., first] = m * (a * t.cos() - b * t.sin())
+    out[..., second] = m * (a * t.sin() + b * t.cos())
+    size[..., first] = size[..., second] = m * (a.abs() + b.abs())
+    return out, size
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape,rot", [((1, 1, 1, 2), 2), ((3, 5, 7, 64), 64), ((2, 129, 3, 80), 48),
+                                       ((1, 33, 40, 128), 126), ((4, 17, 1, 256), 256), ((2, 9, 6, 32), 16),
+                                       ((1, 3, 33, 96), 96), ((1, 2, 600, 64), 32)])
+def test_rotary_matches_the_definition(shape, rot, dtype, layout):
+    from paper_1809_02839_amd import native
+    print(f"[rotary] {shape} rot {rot} {dtype} {layout}", flush=True)
+    g = _gen(sum(shape) + rot)
+    x = _randn(shape, g, dtype)
+    far = torch.randint(-5, 1 << 21, (shape[0], 1), generator=g, device="cuda")
+    pos = (far + torch.arange(shape[1], device="cuda")).to(torch.int32)
+    for scaling, factor, original in (("none", 1.0, 0), ("linear", 3.5, 0), ("ntk", 8.0, 0), ("parts", 16.0, 512)):
+        r = native.Rotary(shape[3], rot, layout, 10000.0, scaling, factor, original)
+        for inverse in (False, True):
+            want, size = _turned(x, pos, rot, layout, 10000.0, scaling, factor, original, inverse)
+            out = torch.full_like(x, float("nan"))
+            assert r.apply(x, out, positions=pos, inverse=inverse) is out
+            tol = 8e-7 * size + (BF * want.abs() if dtype == torch.bfloat16 else 0)
+            assert bool(((out.double() - want).abs() <= tol).all())
+            assert torch.equal(out[..., rot:], x[..., rot:])
+            again = x.clone()                   # in place gives the same bits
+            r.apply(again, positions=pos, inverse=inverse)
+            assert torch.equal(again, out)
+
+
+def test_rotary_strides_and_first_position():
+    from paper_1809_02839_amd import native
+    g = _gen(3)
+    room = _randn((2, 11, 9, 3, 64), g)          # heads 2 .. 7 of part 1 of a packed tensor
+    before = room.clone()
+    x = room[:, :, 2:8, 1]
+    want, size = _turned(x, torch.arange(100, 111, device="cuda").expand(2, 11), 64, "half", 500.0, "none", 1, 0, False)
+    native.Rotary(64, base=500.0).apply(x, first_position=100)
+    assert bool(((room[:, :, 2:8, 1].double() - want).abs() <= 8e-7 * size + BF * want.abs()).all())
+    room[:, :, 2:8, 1] = before[:, :, 2:8, 1]
+    assert torch.equal(room, before)             # nothing else was written
+    odd = _randn((2, 5, 3, 67), g)[..., 1:65]    # single-value accesses
+    want, size = _turned(odd, torch.arange(5, device="cuda").expand(2, 5), 64, "interleaved", 1e4, "none", 1, 0, True)
+    out = native.Rotary(64, layout="interleaved").apply(odd, torch.empty(2, 5, 3, 64, dtype=torch.bfloat16,
+                                                                         device="cuda"), inverse=True)
+    assert bool(((out.double() - want).abs() <= 8e-7 * size + BF * want.abs()).all())
+
+
+# --------------------------------------------------------------- attention ----
+
+def _visible(B, Sq, Sk, offset, causal, documents, prefix, kv_lengths):
+    p = torch.arange(Sq, device="cuda")[:, None] + offset
+    j = torch.arange(Sk, device="cuda")[None]
+    see = torch.ones(B, Sq, Sk, dtype=torch.bool, device="cuda")
+    for b in range(B):
+        if causal:
+            see[b] &= (j <= p) | (j < (int(prefix[b]) if prefix is not None else 0))
+        if documents is not None:
+            ids = documents[b].tolist()
+            run = [0]
+            for t in range(1, Sk):
+                run.append(run[-1] + (ids[t] != ids[t - 1]))
+            run = torch.tensor(run, device="cuda")
+            see[b] &= run[p] == run[j]
+        if kv_lengths is not None:
+            see[b] &= j < int(kv_lengths[b])
+    return see
+
+
+class Reference:
+    """Float64 attention, its gradients, and bounds on what the kernels may differ by."""
+
+    def __init__(self, q, k, v, scale, cap, slopes, see, offset, dout=None):
+        B, Sq, H, D = q.shape
+        Sk, Hk = k.shape[1], k.shape[2]
+        G = H // Hk
+        heads = lambda t: t.double().transpose(1, 2)
+        Q, K, V = heads(q), heads(k).repeat_interleave(G, 1), heads(v).repeat_interleave(G, 1)
+        T = lambda t: t.transpose(2, 3)
+        z = scale * Q @ T(K)
+        size = abs(scale) * Q.abs() @ T(K.abs())           # sum of the products' magnitudes
+        t = torch.tanh(z / cap) if cap else None
+        s = cap * t if cap else z
+        if slopes is not None:
+            far = (torch.arange(Sq, device="cuda")[:, None] + offset - torch.arange(Sk, device="cuda")[None]).abs()
+            s = s - slopes.double()[None, :, None, None] * far
+        s = s.masked_fill(~see[:, None], -math.inf)
+        empty = (s == -math.inf).all(3, keepdim=True) if Sk else torch.ones(B, H, Sq, 1, dtype=bool, device="cuda")
+        lse = torch.logsumexp(s, 3, keepdim=True) if Sk else torch.full((B, H, Sq, 1), -math.inf, device="cuda").double()
+        P = torch.exp(s - lse.masked_fill(empty, 0.0)).masked_fill(empty, 0.0)
+        out = P @ V
+        # a score: `dim` float32 additions, the scaling, the cap's tanh, the bias, the change to base 2
+        E = (D + 8) * 2.0 ** -24 * size.masked_fill(~see[:, None], 0.0).amax((1, 2, 3), keepdim=True) if Sk else 0.0
+        E = E + 2.0 ** -21 * (1 + s.masked_fill(s == -math.inf, 0.0).abs().amax() if Sk else 1.0) + (
+            cap * 2.0 ** -21 if cap else 0.0)
+        self.E = E
+        pv = P @ V.abs()
+        out_tol = (BF + 2 * E) * pv * (1 + 2 * BF) + BF * out.abs()
+        back = lambda t: t.transpose(1, 2)
+        self.out, self.out_tol = back(out), back(out_tol)
+        self.lse, self.lse_tol = lse[..., 0], (E + 2.0 ** -22 * lse.abs().masked_fill(empty, 0.0))[..., 0]
+        self.empty = empty[..., 0]
+        if dout is None:
+            return
+        dO = heads(dout)
+        dP = dO @ T(V)
+        delta = (out * dO).sum(3, keepdim=True)
+        dS = P * (dP - delta)
+        one = 1 - t * t if cap else torch.ones_like(P)
+        dZ = dS * one * scale
+        delta_tol = (out_tol * dO.abs()).sum(3, keepdim=True) + (D + 8) * 2.0 ** -24 * (out.abs() * dO.abs()).sum(
+            3, keepdim=True)
+        dP_tol = (D + 8) * 2.0 ** -24 * dO.abs() @ T(V.abs())
+        dS_tol = P * (delta_tol + dP_tol) + (BF + 2 * E + (E + 2.0 ** -20 if cap else 0)) * P * (dP.abs() + delta.abs())
+        dS_tol = dS_tol * abs(scale) * (1 + 2 * BF)
+        group = lambda t: back(t.reshape(B, Hk, G, Sk, D).sum(2))
+        self.dq, self.dk, self.dv = back(dZ @ K), group(T(dZ) @ Q), group(T(P) @ dO)
+        self.dq_tol = back(dS_tol @ K.abs()) + BF * self.dq.abs()
+        self.dk_tol = group(T(dS_tol) @ Q.abs()) + BF * self.dk.abs()
+        self.dv_tol = group(T(P) @ dO.abs()) * (BF + 2 * E) * (1 + 2 * BF) + BF * self.dv.abs()
+        self.dO, self.z_size = dO, size
+
+
+def _close(got, want, tol, what):
+    bad = ~((got.double() - want).abs() <= tol + 1e-30)
+    assert not bool(bad.any()), (what, int(bad.sum()), float((got.double() - want).abs().max()), float(tol.max()))
+
+
+CASES = [
+    # B, H, Hk, D, Sq, Sk, offset, causal, masks, cap, slopes
+    (1, 1, 1, 8, 1, 1, 0, True, "", 0.0, False),
+    (2, 4, 2, 64, 1, 65, 64, True, "len", 0.0, False),
+    (3, 8, 1, 128, 1, 777, 776, True, "len", 20.0, True),
+    (2, 6, 6, 32, 2, 300, 298, True, "", 0.0, True),
+    (1, 16, 2, 80, 5, 1000, 995, True, "len", 0.0, False),
+    (2, 2, 2, 64, 63, 63, 0, True, "doc", 0.0, False),
+    (2, 4, 2, 64, 64, 64, 0, True, "doc prefix", 15.0, False),
+    (1, 4, 4, 96, 65, 65, 0, False, "doc", 0.0, True),
+    (2, 3, 1, 128, 129, 129, 0, True, "prefix len", 0.0, False),
+    (1, 2, 1, 40, 200, 200, 0, True, "doc len", 8.0, True),
+    (2, 5, 5, 64, 127, 190, 63, True, "prefix", 0.0, False),
+    (1, 8, 2, 128, 97, 411, 314, True, "", 30.0, True),
+    (1, 12, 4, 64, 130, 130, 0, False, "len", 0.0, False),
+    (1, 2, 2, 64, 40, 20, -30, True, "", 0.0, False),          # rows before the first key see nothing
+    (2, 2, 1, 32, 17, 0, 0, False, "", 0.0, False),            # no keys at all
+    (2, 4, 1, 64, 33, 70, 100, True, "len zero", 0.0, True),   # positions past every key, one empty sequence
+    (1, 1, 1, 128, 520, 520, 0, True, "doc", 0.0, False),
+    (1, 7, 7, 16, 300, 300, 0, True, "every", 0.0, False),     # every token its own document
+    (1, 3, 3, 24, 2100, 2100, 0, True, "doc", 0.0, False),     # runs over several blocks of the run search
+    (1, 64, 1, 64, 6, 6, 0, True, "", 0.0, False),
+]
+
+
+def _masks(kind, B, Sk, H, slopes, g):
+    m = {}
+    if "doc" in kind:
+        m["documents"] = (torch.rand(B, Sk, generator=g, device="cuda") < 4 / max(Sk, 1)).int().cumsum(1).int() % 3
+    if "every" in kind:
+        m["documents"] = torch.arange(Sk, device="cuda", dtype=torch.int32).expand(B, Sk).contiguous()
+    if "prefix" in kind:
+        m["prefix"] = torch.randint(0, Sk + 20, (B,), generator=g, device="cuda", dtype=torch.int32)
+    if "len" in kind:
+        m["kv_lengths"] = torch.randint(1, Sk + 5, (B,), generator=g, device="cuda", dtype=torch.int32)
+    if "zero" in kind:
+        m["kv_lengths"][0] = 0
+    if slopes:
+        m["slopes"] = torch.rand(H, generator=g, device="cuda") * 0.3
+    return m
+
+
+def _case(c, seed=0):
+    B, H, Hk, D, Sq, Sk, offset, causal, kind, cap, slopes = c
+    g = _gen(seed + B + 3 * H + 5 * D + 7 * Sq + 11 * Sk)
+    q, k, v = _randn((B, Sq, H, D), g, scale=1.5), _randn((B, Sk, Hk, D), g), _randn((B, Sk, Hk, D), g)
+    return q, k, v, _randn((B, Sq, H, D), g), _masks(kind, B, Sk, H, slopes, g)
+
+
+def _see(c, m):
+    B, H, Hk, D, Sq, Sk, offset, causal, kind, cap, slopes = c
+    return _visible(B, Sq, Sk, offset, causal, m.get("documents"), m.get("prefix"), m.get("kv_lengths"))
+
+
+def _attention(c):
+    from paper_1809_02839_amd import native
+    B, H, Hk, D, Sq, Sk, offset, causal, kind, cap, slopes = c
+    return native.Attention(B, H, Hk, D, Sq, Sk, causal=causal, q_offset=offset, cap=cap)
+
+
+def _nan(t):
+    return torch.full_like(t, float("nan"))
+
+
+def _run(a, q, k, v, dout, m, ws=None, stream=None):
+    ws = a.workspace(backward=True) if ws is None else ws
+    out, lse = _nan(q), torch.full((q.shape[0], q.shape[2], q.shape[1]), float("nan"), device="cuda")
+    dq, dk, dv = _nan(q), _nan(k), _nan(v)
+    a.forward(q, k, v, out, lse, workspace=ws, stream=stream, **m)
+    a.backward(q, k, v, out, lse, dout, dq, dk, dv, workspace=ws, stream=stream, **m)
+    return out, lse, dq, dk, dv
+
+
+@pytest.mark.parametrize("c", CASES, ids=lambda c: "-".join(str(v) for v in c).replace(" ", "+"))
+def test_attention_and_gradients_match_the_definition(c):
+    print(f"[attention] {c}", flush=True)
+    q, k, v, dout, m = _case(c)
+    r = Reference(q, k, v, c[3] ** -0.5, c[9], m.get("slopes"), _see(c, m), c[6], dout)
+    out, lse, dq, dk, dv = _run(_attention(c), q, k, v, dout, m)
+    _close(out, r.out, r.out_tol, "out")
+    assert torch.equal(lse == -math.inf, r.empty)
+    _close(lse.masked_fill(r.empty, 0.0), r.lse.masked_fill(r.empty, 0.0), r.lse_tol, "lse")
+    assert not bool(out.transpose(1, 2)[r.empty].any()) and not bool(dq.transpose(1, 2)[r.empty].any())
+    for got, name in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+        _close(got, getattr(r, name), getattr(r, name + "_tol"), name)
+    if "kv_lengths" in m:
+        for b, n in enumerate(m["kv_lengths"].tolist()):
+            assert not bool(dk[b, n:].any()) and not bool(dv[b, n:].any())
+
+
+def test_attention_gradients_match_differences():
+    """The kernels' gradients along a direction against central differences of the float64 definition."""
+    c = (2, 4, 2, 64, 70, 70, 0, True, "doc", 10.0, True)
+    q, k, v, dout, m = _case(c)
+    see = _see(c, m)
+    _, _, *grads = _run(_attention(c), q, k, v, dout, m)
+    g = _gen(77)
+    base = [t.double() for t in (q, k, v)]
+    r = Reference(q, k, v, 0.125, 10.0, m["slopes"], see, 0, dout)
+    for n, name in enumerate(("dq", "dk", "dv")):
+        d = torch.randn(base[n].shape, generator=g, device="cuda").double()
+        step, values = 1e-5, []
+        for sign in (1, -1):
+            moved = list(base)
+            moved[n] = base[n] + sign * step * d
+            values.append(float((Reference(*moved, 0.125, 10.0, m["slopes"], see, 0).out * dout.double()).sum()))
+        slope = (values[0] - values[1]) / (2 * step)
+        # the bound of every value, and 1e-6 for the differences' own error
+        tol = float((getattr(r, name + "_tol") * d.abs()).sum()) + 1e-6 * (1 + abs(slope))
+        assert abs(float((grads[n].double() * d).sum()) - slope) <= tol, name
+
+
+def test_attention_scale_and_large_scores():
+    """Scores of thousands, a negative and a zero scale."""
+    from paper_1809_02839_amd import native
+    g = _gen(5)
+    q, k, v, dout = (_randn((1, 100, 2, 64), g, scale=s) for s in (8.0, 8.0, 1.0, 1.0))
+    see = _visible(1, 100, 100, 0, True, None, None, None)
+    for scale in (1.0, -0.5, 0.0):
+        a = native.Attention(1, 2, 2, 64, 100, 100, causal=True, scale=scale)
+        r = Reference(q, k, v, scale, 0.0, None, see, 0, dout)
+        got = _run(a, q, k, v, dout, {})
+        _close(got[0], r.out, r.out_tol, "out")
+        for x, name in zip(got[2:], ("dq", "dk", "dv")):
+            _close(x, getattr(r, name), getattr(r, name + "_tol"), name)
+
+
+def test_attention_strides_and_packed_gradients():
+    """q, k, v and their gradients as parts of packed tensors; out and dout of other orders."""
+    c = (2, 4, 2, 64, 90, 90, 0, True, "doc", 0.0, False)
+    q, k, v, dout, m = _case(c)
+    r = Reference(q, k, v, 0.125, 0.0, None, _see(c, m), 0, dout)
+    packed = torch.zeros(90, 2, 9, 64, dtype=torch.bfloat16, device="cuda")      # token, batch, (q q q q k k v v -)
+    parts = lambda t: [t[:, :, a:b].transpose(0, 1) for a, b in ((0, 4), (4, 6), (6, 8))]
+    pq, pk, pv = parts(packed)
+    pq.copy_(q), pk.copy_(k), pv.copy_(v)
+    grads = torch.full_like(packed, 7.0)
+    dq, dk, dv = parts(grads)
+    out = torch.empty(2, 4, 90, 64, dtype=torch.bfloat16, device="cuda").transpose(1, 2)
+    d2 = torch.empty(90, 4, 2, 64, dtype=torch.bfloat16, device="cuda").permute(2, 0, 1, 3)
+    d2.copy_(dout)
+    lse = torch.empty(2, 4, 90, device="cuda")
+    a = _attention(c)
+    ws = a.workspace(backward=True)
+    a.forward(pq, pk, pv, out, lse, workspace=ws, **m)
+    a.backward(pq, pk, pv, out, lse, d2, dq, dk, dv, workspace=ws, **m)
+    _close(out, r.out, r.out_tol, "out")
+    for x, name in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+        _close(x, getattr(r, name), getattr(r, name + "_tol"), name)
+    assert bool((grads[:, :, 8] == 7.0).all())
+    # a key shared by the batch through a stride of 0
+    k1, v1 = k[:1].expand(2, -1, -1, -1), v[:1].expand(2, -1, -1, -1)
+    r = Reference(q, k1, v1, 0.125, 0.0, None, _see(c, m), 0)
+    a.forward(q, k1, v1, out, None, workspace=ws, **m)
+    _close(out, r.out, r.out_tol, "out")
+
+
+@pytest.mark.parametrize("Sq", [1, 50])
+def test_attention_ignores_what_no_row_sees(Sq):
+    """NaN and infinities past kv_lengths, and huge finite values behind the causal mask, change nothing."""
+    c = (2, 4, 2, 64, Sq, 200, 120, True, "len", 0.0, False)
+    q, k, v, dout, m = _case(c)
+    m["kv_lengths"] = torch.tensor([131, 0], dtype=torch.int32, device="cuda")
+    a = _attention(c)
+    clean = _run(a, q, k, v, dout, m)
+    k2, v2 = k.clone(), v.clone()
+    for b, n in ((0, 131), (1, 0)):
+        k2[b, n:], v2[b, n:] = float("nan"), float("inf")
+    for x, y in zip(clean, _run(a, q, k2, v2, dout, m)):
+        assert torch.equal(x, y)
+    m = {}
+    k2, v2 = k.clone(), v.clone()
+    k2[:, 120 + Sq:], v2[:, 120 + Sq:] = -3e38, 3e38
+    clean, got = _run(a, q, k, v, dout, m), _run(a, q, k2, v2, dout, m)
+    for x, y in zip(clean, got):
+        assert torch.equal(x, y)
+
+
+def test_attention_passes_on_nan_and_infinity_of_seen_values():
+    c = (1, 2, 2, 64, 40, 40, 0, True, "", 0.0, False)
+    q, k, v, dout, m = _case(c)
+    q[0, 7, 1, 3] = float("nan")
+    out, lse, *_ = _run(_attention(c), q, k, v, dout, m)
+    assert bool(out[0, 7, 1].isnan().all()) and bool(lse[0, 1, 7].isnan())
+    assert not bool(out[0, :, 0].isnan().any()) and int(lse.isnan().sum()) == 1
+
+
+def test_attention_offsets_past_32_bits():
+    """A cache whose last keys lie beyond 2^32 elements, for one token and for many."""
+    step, Sk = 1 << 20, 4200
+    store = torch.empty(step * Sk, dtype=torch.bfloat16, device="cuda")
+    k = store.as_strided((1, Sk, 2, 64), (8, step, 64, 1))
+    v = store.as_strided((1, Sk, 2, 64), (8, step, 64, 1), 256)
+    g = _gen(11)
+    k.copy_(_randn(k.shape, g)), v.copy_(_randn(v.shape, g))
+    for Sq in (1, 150):
+        c = (1, 4, 2, 64, Sq, Sk, Sk - Sq, True, "", 0.0, False)
+        q = _randn((1, Sq, 4, 64), g)
+        a = _attention(c)
+        out = torch.empty_like(q)
+        a.forward(q, k, v, out, workspace=a.workspace())
+        r = Reference(q, k, v, 0.125, 0.0, None, _see(c, {}), Sk - Sq)
+        _close(out, r.out, r.out_tol, "out")
+
+
+@pytest.mark.parametrize("c", [CASES[2], CASES[9]], ids=["token", "documents"])
+def test_attention_repeats_bitwise_on_another_stream_and_in_a_graph(c):
+    q, k, v, dout, m = _case(c)
+    a = _attention(c)
+    want = _run(a, q, k, v, dout, m)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    got = _run(a, q, k, v, dout, m, stream=stream)
+    torch.cuda.synchronize()
+    for x, y in zip(want, got):
+        assert torch.equal(x, y)
+    ws = a.workspace(backward=True)
+    outs = [torch.empty_like(t) for t in want]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        a.forward(q, k, v, outs[0], outs[1], workspace=ws, **m)
+        a.backward(q, k, v, outs[0], outs[1], dout, *outs[2:], workspace=ws, **m)
+    for replay in range(3):
+        for t in outs:
+            t.zero_()
+        ws.fill_(255)                            # what the workspace held does not matter
+        fresh = _case(c, seed=replay)[0]
+        q.copy_(fresh)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(outs, _run(a, q, k, v, dout, m)):
+            assert torch.equal(x, y)
+
+
+# -------------------------------------------------------------- checkpoint ----
+
+def _packed(x):
+    """Float64 definition, group by group: values, and scale bytes."""
+    R, C = x.shape
+    x = x.double()
+    out, byte = torch.empty_like(x), torch.empty(R, -(-C // 32), dtype=torch.uint8, device=x.device)
+    for n in range(byte.shape[1]):
+        y = x[:, 32 * n:32 * n + 32]
+        top = torch.where(y.isfinite(), y.abs(), torch.zeros_like(y)).amax(1)
+        e = torch.full_like(top, -117.0)
+        for s in range(-116, 121):               # the smallest power that holds the largest
+            e = torch.where(top > 448 * 2.0 ** (s - 1), torch.full_like(e, s), e)
+        byte[:, n] = (e + 127).to(torch.uint8)
+        z = y * torch.exp2(-e)[:, None]
+        step = torch.exp2(torch.floor(torch.log2(z.abs().clamp(min=2.0 ** -6))) - 3)
+        near = torch.round(z / step) * step
+        near = torch.where((near == 0) & (z != 0), torch.sign(z) * 2.0 ** -9, near)
+        near = near.clamp(min=torch.where(e == 120, -240.0, -448.0)[:, None],
+                          max=torch.where(e == 120, 240.0, 448.0)[:, None])
+        out[:, 32 * n:32 * n + 32] = torch.where(y.isfinite(), near * torch.exp2(e)[:, None],
+                                                 torch.full_like(near, float("nan")))
+    return out, byte
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape", [(1, 1), (1, 32), (3, 33), (7, 95), (130, 256), (5, 8), (2, 1000), (257, 72),
+                                   (1, 4096)])
+def test_checkpoint_matches_the_definition(shape, dtype):
+    from paper_1809_02839_amd import native
+    print(f"[checkpoint] {shape} {dtype}", flush=True)
+    g = _gen(shape[0] + shape[1])
+    R, C = shape
+    big = torch.exp2(torch.randint(-140, 125, (R, 1), generator=g, device="cuda").float())   # rows over the whole range
+    for scale in (1.0, big):
+        x = (torch.randn(shape, generator=g, device="cuda") * scale * 4.0 ** torch.randint(
+            -9, 1, shape, generator=g, device="cuda").float()).to(dtype)
+        x[torch.rand(shape, generator=g, device="cuda") < 0.1] = 0.0
+        want, byte = _packed(x)
+        codes = torch.empty(shape, dtype=torch.uint8, device="cuda")
+        scales = torch.empty(R, -(-C // 32), dtype=torch.uint8, device="cuda")
+        native.checkpoint_pack(x, codes, scales)
+        assert torch.equal(scales, byte)
+        for back in (torch.bfloat16, torch.float32):
+            out = torch.empty(shape, dtype=back, device="cuda")
+            native.checkpoint_restore(codes, scales, out)
+            assert torch.equal(out.double(), want)
+        assert torch.equal(codes & 0x7f != 0, x != 0) and torch.equal(out > 0, x > 0)
+
+
+def test_checkpoint_special_values_and_strides():
+    from paper_1809_02839_amd import native
+    for dtype in (torch.bfloat16, torch.float32):
+        top = torch.finfo(dtype).max
+        inf, nan = float("inf"), float("nan")
+        x = torch.zeros(4, 64, dtype=dtype, device="cuda")
+        x[0, :4] = torch.tensor([top, -top, top * 0.5, 1.0])           # the largest: no infinity comes back
+        x[1, :5] = torch.tensor([inf, -inf, nan, 3.0, -448.0])         # not finite: NaN, and no part of the scale
+        x[2, :3] = torch.tensor([1e-38, -1e-38, -0.0])
+        x[3, :4] = torch.tensor([448.0, 1e-6, -1e-6, 9.0])             # far below the group's largest: not zero
+        want, byte = _packed(x)
+        room = torch.full((4, 80), 5.0, dtype=dtype, device="cuda")
+        view = room[:, 8:72]
+        view.copy_(x)
+        codes = torch.empty(4, 64, dtype=torch.uint8, device="cuda")
+        scales = torch.empty(4, 2, dtype=torch.uint8, device="cuda")
+        native.checkpoint_pack(view, codes, scales)
+        room.fill_(5.0)
+        native.checkpoint_restore(codes, scales, view)
+        assert torch.equal(scales, byte)
+        assert torch.equal(view.double().nan_to_num(nan=12345.0), want.nan_to_num(nan=12345.0))
+        assert bool((room[:, :8] == 5.0).all()) and bool((room[:, 72:] == 5.0).all())
+        assert bool(view[0].isfinite().all()) and bool(view[1, :3].isnan().all())
