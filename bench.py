@@ -116,6 +116,7 @@ class StageLoop:
         dev = torch.device("cuda")
         dt = torch.bfloat16 if spec.dtype == "bf16" else torch.float32
         self.st = native.Stage(native.desc_from_spec(spec), synth.initial_params(spec), stream)
+        self.st.configure(spec)
         k, N = spec.stage_index, spec.num_stages
         self.sf, self.sb = native.policy_versions(spec.policy, k, N)
         self.depth = N - k
@@ -204,6 +205,7 @@ class PipeLoop:
         self.st, self.sf, self.sb = [], [], []
         for spec in self.specs:
             st = native.Stage(native.desc_from_spec(spec), synth.initial_params(spec), stream)
+            st.configure(spec)
             sf, sb = native.policy_versions(spec.policy, spec.stage_index, spec.num_stages)
             self.st.append(st)
             self.sf.append(sf)

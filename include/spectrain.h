@@ -298,10 +298,6 @@ int spectrain_stage_profile_read(spectrain_stage_t st, spectrain_kernel_stat* ou
 int spectrain_stage_read_stash(spectrain_stage_t st, int64_t mb_id, int32_t index, void* host_out, size_t capacity,
                                size_t* size);
 
-/* Release every device buffer of the stage. Synchronises the stream.
- * Passing NULL returns EINVAL. */
-int spectrain_stage_destroy(spectrain_stage_t st);
-
 /* ---- Operators ----
  *
  * What a TRANSFORMER stage with positions, masks or an 8-bit stash
@@ -434,6 +430,62 @@ int spectrain_checkpoint_pack(int32_t dtype, int64_t rows, int64_t cols, const v
                               uint8_t* codes_dev, uint8_t* scales_dev, void* hip_stream);
 int spectrain_checkpoint_restore(int32_t dtype, int64_t rows, int64_t cols, const uint8_t* codes_dev,
                                  const uint8_t* scales_dev, void* out_dev, int64_t ld, void* hip_stream);
+
+/* ---- A transformer stage's use of them ---- */
+
+/* Positions and masks of a TRANSFORMER stage. By default its attention has
+ * neither; with this call its layers turn the query and key heads by rotary
+ * positions (token index; rotary_dim 0: none) and run spectrain_attention_*
+ * (causal, cap, bias by distance; scale 1/sqrt(head dimension)). slopes_host:
+ * `heads` float32 values, copied, or NULL. attn NULL: back to the default. The
+ * stash keeps the turned qkv, and lse (float32 [B, heads, S]) as buffer 13l+1;
+ * buffer 13l+2 is unused. EINVAL for another kind of stage, a head dimension
+ * above 128 (or whatever spectrain_rotary refuses); ESTATE while a mini-batch
+ * is in flight. The stage's buffers are made anew (ENOMEM leaves the stage as
+ * it was), so graphs captured before the call must not be replayed.
+ * Synchronises the stream. */
+typedef struct {
+  uint32_t abi_version;      /* SPECTRAIN_ABI_VERSION */
+  int32_t causal;            /* 0 or 1 */
+  float cap;                 /* 0: none; > 0 */
+  int32_t rotary_dim;        /* 0: no positions */
+  int32_t rotary_layout;     /* as in spectrain_rotary_desc */
+  int32_t rotary_scaling;
+  int32_t rotary_original_length;
+  int32_t reserved;          /* 0 */
+  double rotary_base;
+  double rotary_factor;
+} spectrain_stage_attention;
+
+int spectrain_stage_set_attention(spectrain_stage_t st, const spectrain_stage_attention* attn,
+                                  const float* slopes_host);
+
+/* Masks of mini-batch mb_id, for its coming forward and its backward: documents
+ * int32 [B, S], prefix (causal stages) and kv_lengths int32 [B], each may be
+ * NULL; slopes has to be NULL (the stage has its own). The device arrays are
+ * kept by reference until the backward returns. ESTATE without
+ * spectrain_stage_set_attention, or when mb_id is already in flight; a second
+ * call before the forward replaces the first. */
+int spectrain_stage_set_masks(spectrain_stage_t st, int64_t mb_id, const spectrain_attention_masks* masks);
+
+/* How a TRANSFORMER stage keeps the activations of mini-batches in flight:
+ * BF16 (the default), or E4M3: buffers 4, 7, 8, 9 and 12 of every layer (r1, h,
+ * f1, r2 and the layer output) as 8-bit checkpoints (spectrain_checkpoint_pack),
+ * restored layer by layer in the backward; qkv and ctx, from which the attention
+ * gradient is formed again, stay in 16 bits. The forward's results do not
+ * change; the backward reads the restored values (its layer norms with the row
+ * statistics of the original ones), and
+ * spectrain_stage_read_stash hands out those. A slot then takes 16.3 in place
+ * of 24 units of T * d bytes a layer at ffn = 4 d; the workspace grows by one
+ * layer's activations. EINVAL, ESTATE and buffers as for
+ * spectrain_stage_set_attention. */
+typedef enum { SPECTRAIN_STASH_BF16 = 0, SPECTRAIN_STASH_E4M3 = 1 } spectrain_stash_format;
+
+int spectrain_stage_set_stash(spectrain_stage_t st, int32_t format);
+
+/* Release every device buffer of the stage. Synchronises the stream.
+ * Passing NULL returns EINVAL. */
+int spectrain_stage_destroy(spectrain_stage_t st);
 
 /* Message of the last failed call on this host thread ("" if none). */
 const char* spectrain_last_error(void);

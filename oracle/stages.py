@@ -21,6 +21,7 @@ import numpy as np
 
 import synth
 
+from . import attention as At
 from . import layers as Lr
 from .numerics import identity, to_bf16
 
@@ -56,21 +57,26 @@ def pack(spec, tensors: Dict[str, np.ndarray]) -> np.ndarray:
 
 # ============================================================== forward ====
 
-def forward(spec, P, x, labels=None, exact=False):
+def forward(spec, P, x, labels=None, exact=False, masks=None):
     """Returns (y, loss, stash). y is the stage output (logits for a CE head),
-    loss is the mean cross-entropy for a CE head and None otherwise."""
+    loss is the mean cross-entropy for a CE head and None otherwise. masks: the
+    mini-batch's attention masks (a stage whose spec has an attention)."""
     q = rounder(spec, exact)
+    if spec.kind == "transformer":
+        return _tfm_fwd(spec, P, np.asarray(x, np.float64), labels, q, masks)
     fn = {"fc": _fc_fwd, "conv3x3": _conv_fwd, "bottleneck": _bneck_fwd,
-          "transformer": _tfm_fwd, "reslstm": _lstm_fwd}[spec.kind]
+          "reslstm": _lstm_fwd}[spec.kind]
     return fn(spec, P, np.asarray(x, np.float64), labels, q)
 
 
-def backward(spec, P, stash, dy=None, exact=False):
+def backward(spec, P, stash, dy=None, exact=False, masks=None):
     """Returns (dx, grads) with grads keyed like the parameter layout.
     For a CE head dy is ignored (the head's dlogits is in the stash)."""
     q = rounder(spec, exact)
+    if spec.kind == "transformer":
+        return _tfm_bwd(spec, P, stash, None if dy is None else np.asarray(dy, np.float64), q, masks)
     fn = {"fc": _fc_bwd, "conv3x3": _conv_bwd, "bottleneck": _bneck_bwd,
-          "transformer": _tfm_bwd, "reslstm": _lstm_bwd}[spec.kind]
+          "reslstm": _lstm_bwd}[spec.kind]
     return fn(spec, P, stash, None if dy is None else np.asarray(dy, np.float64), q)
 
 
@@ -202,11 +208,12 @@ def _bneck_bwd(spec, P, st, dy, q):
 
 # ----------------------------------------------------------- transformer ----
 
-def _tfm_fwd(spec, P, x, labels, q):
+def _tfm_fwd(spec, P, x, labels, q, masks=None):
     """Post-LN encoder layer: h = LN1(x + W_o MHA(x) + b_o),
     y = LN2(h + W_2 relu(W_1 h + b_1) + b_2); softmax scale 1/sqrt(d_head),
-    no mask, no dropout. A CE head projects every token to the vocabulary and
-    averages the per-token loss (the target-token head of the last stage)."""
+    no dropout; no mask and no positions unless the spec has an attention (then
+    the stashed qkv holds the turned heads). A CE head projects every token to
+    the vocabulary and averages the per-token loss (the target-token head of the last stage)."""
     dm, H, _, S = spec.dims[:4]
     B = spec.batch
     a = x.reshape(B * S, dm)
@@ -214,10 +221,15 @@ def _tfm_fwd(spec, P, x, labels, q):
     for l in range(spec.num_layers):
         p = f"layer{l}."
         qkv = q(Lr.linear(a, P[p + "attn.qkv.weight"], P[p + "attn.qkv.bias"]))
+        if spec.attention is not None:
+            qkv = q(At.turn_heads(spec.attention, qkv, B, S, H))
         Q = Lr.split_heads(qkv[:, :dm], B, S, H)
         K = Lr.split_heads(qkv[:, dm:2 * dm], B, S, H)
         V = Lr.split_heads(qkv[:, 2 * dm:], B, S, H)
-        Pr = q(Lr.attention_probs(Q, K))
+        if spec.attention is None:
+            Pr = q(Lr.attention_probs(Q, K))
+        else:
+            Pr = q(At.probs(spec.attention, Q, K, masks)[0])
         ctx = q(Lr.merge_heads(Pr @ V))
         r1 = q(a + Lr.linear(ctx, P[p + "attn.out.weight"], P[p + "attn.out.bias"]))
         h, _, _ = Lr.layernorm_forward(r1, P[p + "ln1.weight"], P[p + "ln1.bias"], LN_EPS)
@@ -254,7 +266,18 @@ def _attention_backward(dctx, qkv, B, S, H, q):
     return np.concatenate([Lr.merge_heads(dQ), Lr.merge_heads(dK), Lr.merge_heads(dV)], axis=1)
 
 
-def _tfm_bwd(spec, P, st, dy, q):
+def _normalised(c, ln, r, P, p):
+    """Normalised rows and 1/std of a residual sum: of the stored sum itself, or,
+    where the stash holds a rounded copy of it (an 8-bit stash), with the row
+    statistics of the original, which are stashed beside it."""
+    if ln in c:
+        mean, rstd = c[ln]
+        return (c[r] - mean) * rstd, rstd
+    _, xhat, rstd = Lr.layernorm_forward(c[r], P[p + ln + ".weight"], P[p + ln + ".bias"], LN_EPS)
+    return xhat, rstd
+
+
+def _tfm_bwd(spec, P, st, dy, q, masks=None):
     dm, H, _, S = spec.dims[:4]
     B = spec.batch
     grads = {}
@@ -268,7 +291,7 @@ def _tfm_bwd(spec, P, st, dy, q):
     for l in range(spec.num_layers - 1, -1, -1):
         p = f"layer{l}."
         c = st["layers"][l]
-        _, xh2, rs2 = Lr.layernorm_forward(c["r2"], P[p + "ln2.weight"], P[p + "ln2.bias"], LN_EPS)
+        xh2, rs2 = _normalised(c, "ln2", "r2", P, p)
         dr2, grads[p + "ln2.weight"], grads[p + "ln2.bias"] = Lr.layernorm_backward(g, xh2, rs2, P[p + "ln2.weight"])
         dr2 = q(dr2)
         grads[p + "ffn2.weight"] = dr2.T @ c["f1"]
@@ -277,13 +300,16 @@ def _tfm_bwd(spec, P, st, dy, q):
         grads[p + "ffn1.weight"] = df1.T @ c["h"]
         grads[p + "ffn1.bias"] = df1.sum(axis=0)
         dh = q(df1 @ P[p + "ffn1.weight"] + dr2)
-        _, xh1, rs1 = Lr.layernorm_forward(c["r1"], P[p + "ln1.weight"], P[p + "ln1.bias"], LN_EPS)
+        xh1, rs1 = _normalised(c, "ln1", "r1", P, p)
         dr1, grads[p + "ln1.weight"], grads[p + "ln1.bias"] = Lr.layernorm_backward(dh, xh1, rs1, P[p + "ln1.weight"])
         dr1 = q(dr1)
         grads[p + "attn.out.weight"] = dr1.T @ c["ctx"]
         grads[p + "attn.out.bias"] = dr1.sum(axis=0)
         dctx = q(dr1 @ P[p + "attn.out.weight"])
-        dqkv = _attention_backward(dctx, c["qkv"], B, S, H, q)
+        if spec.attention is None:
+            dqkv = _attention_backward(dctx, c["qkv"], B, S, H, q)
+        else:
+            dqkv = At.backward(spec.attention, dctx, c["qkv"], B, S, H, masks, q)
         grads[p + "attn.qkv.weight"] = dqkv.T @ c["a"]
         grads[p + "attn.qkv.bias"] = dqkv.sum(axis=0)
         g = q(dqkv @ P[p + "attn.qkv.weight"] + dr1)

@@ -150,6 +150,19 @@ int spectrain_stage_destroy(spectrain_stage_t st) {
   return SPECTRAIN_OK;
 }
 
+int spectrain_stage_set_attention(spectrain_stage_t st, const spectrain_stage_attention* attn,
+                                  const float* slopes_host) {
+  return guarded(st, [&](spx::Stage& x) { x.set_attention(attn, slopes_host); }, false);
+}
+
+int spectrain_stage_set_masks(spectrain_stage_t st, int64_t mb_id, const spectrain_attention_masks* masks) {
+  return guarded(st, [&](spx::Stage& x) { x.set_masks(mb_id, masks); }, false);
+}
+
+int spectrain_stage_set_stash(spectrain_stage_t st, int32_t format) {
+  return guarded(st, [&](spx::Stage& x) { x.set_stash(format); }, false);
+}
+
 int spectrain_rotary(const spectrain_rotary_desc* desc, const void* x_dev, const int32_t* positions_dev,
                      int32_t inverse, void* out_dev, void* hip_stream) {
   return guarded([&]() {

@@ -21,14 +21,31 @@ struct Place {
   bool live;
 };
 
-__device__ __forceinline__ Place place(long groups_total, FastDiv groups, long cols) {
-  const long unit = static_cast<long>(blockIdx.x) * NT + threadIdx.x, g = unit / LANES;
-  const bool live = g < groups_total;
-  const uint32_t gi = live ? static_cast<uint32_t>(g) : 0u, row = groups.div(gi);
+struct Job : CheckpointArgs {
+  long total = 0;          // groups of the tensor
+  FastDiv groups;          // of a row
+  unsigned first = 0;      // its first block
+};
+struct Jobs {
+  Job job[CHECKPOINT_MAX];
+  int n = 0;
+};
+
+// The block's tensor: blocks are dealt to the tensors in order.
+__device__ __forceinline__ const Job& my_job(const Jobs& jobs) {
+  int j = 0;
+  while (j + 1 < jobs.n && blockIdx.x >= jobs.job[j + 1].first) ++j;
+  return jobs.job[j];
+}
+
+__device__ __forceinline__ Place place(const Job& a) {
+  const long unit = static_cast<long>(blockIdx.x - a.first) * NT + threadIdx.x, g = unit / LANES;
+  const bool live = g < a.total;
+  const uint32_t gi = live ? static_cast<uint32_t>(g) : 0u, row = a.groups.div(gi);
   Place p;
   p.row = row;
-  p.col = static_cast<long>(gi - row * groups.d) * CHECKPOINT_GROUP + (threadIdx.x % LANES) * PER;
-  p.n = static_cast<int>(min(max(cols - p.col, 0L), static_cast<long>(PER)));
+  p.col = static_cast<long>(gi - row * a.groups.d) * CHECKPOINT_GROUP + (threadIdx.x % LANES) * PER;
+  p.n = static_cast<int>(min(max(a.cols - p.col, 0L), static_cast<long>(PER)));
   p.live = live;
   return p;
 }
@@ -41,8 +58,9 @@ __device__ __forceinline__ float to_float(T v) {
 
 // WIDE: every lane's eight values are whole and 16-byte aligned.
 template <typename T, bool WIDE>
-__global__ __launch_bounds__(NT) void checkpoint_pack_kernel(CheckpointArgs a, long total, FastDiv groups) {
-  const Place p = place(total, groups, a.cols);
+__global__ __launch_bounds__(NT) void checkpoint_pack_kernel(Jobs jobs) {
+  const Job& a = my_job(jobs);
+  const Place p = place(a);
   const T* x = static_cast<const T*>(a.x) + p.row * a.ld + p.col;
   float v[PER];
 #pragma unroll
@@ -104,16 +122,17 @@ __global__ __launch_bounds__(NT) void checkpoint_pack_kernel(CheckpointArgs a, l
       if (i < p.n) out[i] = static_cast<uint8_t>(word[i / 4] >> (8 * (i % 4)));
   }
   if (threadIdx.x % LANES == 0)
-    a.scales[p.row * groups.d + p.col / CHECKPOINT_GROUP] = static_cast<uint8_t>(e + 127);
+    a.scales[p.row * a.groups.d + p.col / CHECKPOINT_GROUP] = static_cast<uint8_t>(e + 127);
 }
 
 template <typename T, bool WIDE>
-__global__ __launch_bounds__(NT) void checkpoint_restore_kernel(CheckpointArgs a, long total, FastDiv groups) {
-  const Place p = place(total, groups, a.cols);
+__global__ __launch_bounds__(NT) void checkpoint_restore_kernel(Jobs jobs) {
+  const Job& a = my_job(jobs);
+  const Place p = place(a);
   if (!p.live || p.n == 0) return;
   const uint8_t* codes = a.codes + p.row * a.cols + p.col;
   const float scale =
-      __uint_as_float(static_cast<uint32_t>(a.scales[p.row * groups.d + p.col / CHECKPOINT_GROUP]) << 23);
+      __uint_as_float(static_cast<uint32_t>(a.scales[p.row * a.groups.d + p.col / CHECKPOINT_GROUP]) << 23);
   uint32_t word[2] = {0u, 0u};
   if (WIDE) {
     const uint2 u = *reinterpret_cast<const uint2*>(codes);
@@ -157,27 +176,38 @@ bool wide(const CheckpointArgs& a, const void* t) {
          reinterpret_cast<uintptr_t>(a.codes) % 8 == 0;
 }
 
+// WIDE only where every tensor allows it.
 template <typename K>
-hipError_t launch(K* kernel, const CheckpointArgs& a, hipStream_t s) {
-  const long groups = (a.cols + CHECKPOINT_GROUP - 1) / CHECKPOINT_GROUP, total = a.rows * groups;
-  const long blocks = (total * LANES + NT - 1) / NT;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(blocks)), dim3(NT), 0, s, a, total,
-                     FastDiv(static_cast<uint32_t>(groups)));
+hipError_t launch(K* wide_kernel, K* plain_kernel, const CheckpointArgs* a, int n, hipStream_t s) {
+  if (n < 1 || n > CHECKPOINT_MAX) return hipErrorInvalidValue;
+  Jobs jobs;
+  jobs.n = n;
+  long blocks = 0;
+  bool w = true;
+  for (int i = 0; i < n; ++i) {
+    Job& j = jobs.job[i];
+    static_cast<CheckpointArgs&>(j) = a[i];
+    j.groups = FastDiv(static_cast<uint32_t>((a[i].cols + CHECKPOINT_GROUP - 1) / CHECKPOINT_GROUP));
+    j.total = a[i].rows * j.groups.d;
+    j.first = static_cast<unsigned>(blocks);
+    blocks += (j.total * LANES + NT - 1) / NT;
+    w = w && wide(a[i], a[i].x ? a[i].x : a[i].out);
+  }
+  if (blocks >= 1L << 24) return hipErrorInvalidValue;   // grids of up to 2^32 - 1 threads
+  hipLaunchKernelGGL(w ? wide_kernel : plain_kernel, dim3(static_cast<unsigned>(blocks)), dim3(NT), 0, s, jobs);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t checkpoint_pack(const CheckpointArgs& a, int dtype, hipStream_t s) {
-  const bool w = wide(a, a.x);
-  if (dtype) return launch(w ? checkpoint_pack_kernel<bf16_t, true> : checkpoint_pack_kernel<bf16_t, false>, a, s);
-  return launch(w ? checkpoint_pack_kernel<float, true> : checkpoint_pack_kernel<float, false>, a, s);
+hipError_t checkpoint_pack(const CheckpointArgs* a, int n, int dtype, hipStream_t s) {
+  if (dtype) return launch(checkpoint_pack_kernel<bf16_t, true>, checkpoint_pack_kernel<bf16_t, false>, a, n, s);
+  return launch(checkpoint_pack_kernel<float, true>, checkpoint_pack_kernel<float, false>, a, n, s);
 }
 
-hipError_t checkpoint_restore(const CheckpointArgs& a, int dtype, hipStream_t s) {
-  const bool w = wide(a, a.out);
-  if (dtype) return launch(w ? checkpoint_restore_kernel<bf16_t, true> : checkpoint_restore_kernel<bf16_t, false>, a, s);
-  return launch(w ? checkpoint_restore_kernel<float, true> : checkpoint_restore_kernel<float, false>, a, s);
+hipError_t checkpoint_restore(const CheckpointArgs* a, int n, int dtype, hipStream_t s) {
+  if (dtype) return launch(checkpoint_restore_kernel<bf16_t, true>, checkpoint_restore_kernel<bf16_t, false>, a, n, s);
+  return launch(checkpoint_restore_kernel<float, true>, checkpoint_restore_kernel<float, false>, a, n, s);
 }
 
 }  // namespace spx

@@ -197,8 +197,13 @@ struct CheckpointArgs {
   uint8_t *codes = nullptr, *scales = nullptr;
   long rows = 0, cols = 0, ld = 0;      // ld: elements between rows of x or out
 };
-hipError_t checkpoint_pack(const CheckpointArgs& a, int dtype, hipStream_t s);
-hipError_t checkpoint_restore(const CheckpointArgs& a, int dtype, hipStream_t s);
+inline size_t checkpoint_scale_count(long rows, long cols) {
+  return static_cast<size_t>(rows) * ((cols + CHECKPOINT_GROUP - 1) / CHECKPOINT_GROUP);
+}
+// Up to CHECKPOINT_MAX tensors of one dtype in one launch.
+constexpr int CHECKPOINT_MAX = 5;
+hipError_t checkpoint_pack(const CheckpointArgs* a, int n, int dtype, hipStream_t s);
+hipError_t checkpoint_restore(const CheckpointArgs* a, int n, int dtype, hipStream_t s);
 
 // Row chunking of the two-pass column reductions (column sums, layer-norm
 // parameter gradients) and the float32 workspace each pass needs.

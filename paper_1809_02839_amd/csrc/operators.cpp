@@ -276,7 +276,7 @@ void run_checkpoint(int dtype, int64_t rows, int64_t cols, const void* x, int64_
   a.rows = rows;
   a.cols = cols;
   a.ld = ld;
-  hip_check(x ? checkpoint_pack(a, dtype, s) : checkpoint_restore(a, dtype, s), x ? "checkpoint_pack"
+  hip_check(x ? checkpoint_pack(&a, 1, dtype, s) : checkpoint_restore(&a, 1, dtype, s), x ? "checkpoint_pack"
                                                                                   : "checkpoint_restore");
 }
 

@@ -6,7 +6,7 @@
 // convolutions, ResNet bottlenecks, a post-LN Transformer encoder, a residual
 // LSTM, and fully-connected layers), with the forward pass reading predicted
 // slot 0 and the backward pass reading slot 1 (Section 3.2, Eq. 5 and Eq. 6).
-#include "stage.hpp"
+#include "operators.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -558,14 +558,21 @@ void Stage::plan_buffers() {
       const Attention core = attention();
       // the fused cores keep only softmax row statistics; the GEMM path P (f32, bf16) and the scores
       const long BHSS = core == Attention::kGemm ? B * H * S * S : 0;
+      const long row_floats = core == Attention::kMasked ? 1 : 2;   // lse, or maximum and 1 / sum
+      // an activation kept for the backward: bf16, or codes followed by scales
+      auto kept = [&](long cols) -> size_t {
+        return opt_.packed ? static_cast<size_t>(T * cols) + checkpoint_scale_count(T, cols)
+                           : static_cast<size_t>(T * cols * 2);
+      };
       for (int l = 0; l < L; ++l) {
-        size_t s[13] = {static_cast<size_t>(T * 3 * d * 2), static_cast<size_t>(BHSS ? BHSS * 4 : B * H * S * 2 * 4),
+        size_t s[13] = {static_cast<size_t>(T * 3 * d * 2),
+                        static_cast<size_t>(BHSS ? BHSS * 4 : B * H * S * row_floats * 4),
                         static_cast<size_t>(BHSS * 2),      static_cast<size_t>(T * d * 2),
-                        static_cast<size_t>(T * d * 2),     static_cast<size_t>(T * 4),
-                        static_cast<size_t>(T * 4),         static_cast<size_t>(T * d * 2),
-                        static_cast<size_t>(T * F * 2),     static_cast<size_t>(T * d * 2),
+                        kept(d),                            static_cast<size_t>(T * 4),
+                        static_cast<size_t>(T * 4),         kept(d),
+                        kept(F),                            kept(d),
                         static_cast<size_t>(T * 4),         static_cast<size_t>(T * 4),
-                        static_cast<size_t>(l < L - 1 || ce ? T * d * 2 : 0)};
+                        l < L - 1 || ce ? kept(d) : 0};
         st.insert(st.end(), s, s + 13);
       }
       st.push_back(ce ? T * V * 2 : 0);   // dlogits (bf16) at id 13 L
@@ -574,6 +581,12 @@ void Stage::plan_buffers() {
             static_cast<size_t>(T * d * 2), static_cast<size_t>(T * d * 2), static_cast<size_t>(T * d * 2),
             static_cast<size_t>(T * 3 * d * 2), static_cast<size_t>(ce ? T * V * 4 : 0),
             static_cast<size_t>(ce ? T * 4 : 0)};
+      if (opt_.masked || opt_.packed) {   // ids 12: masked attention, 13 .. 17: a layer's restored activations
+        const spectrain_attention_desc ad = masked_desc(opt_);
+        ws.push_back(opt_.masked ? attention_workspace(&ad, true) : 0);
+        const long widest = std::max(F, d);
+        for (long cols : {widest, d, d, d, d}) ws.push_back(opt_.packed ? static_cast<size_t>(T * cols * 2) : 0);
+      }
       partial = std::max(partial_floats(T, 3 * d), partial_floats(T, F));
       if (ce) partial = std::max(partial, partial_floats(T, V));
       partial = std::max(partial, layernorm_bwd_ws_floats(T, d));
@@ -620,6 +633,12 @@ void Stage::plan_buffers() {
       stash_bytes_[13 * l + 1] = scores * 4;
       stash_bytes_[13 * l + 2] = scores * 2;
     }
+  }
+  if (opt_.packed) {   // read_stash hands out restored values
+    const size_t T = static_cast<size_t>(B) * dm[3];
+    for (int l = 0; l < L; ++l)
+      for (int j : {4, 7, 8, 9, 12})
+        if (st[13 * l + j]) stash_bytes_[13 * l + j] = T * (j == 8 ? dm[2] : dm[0]) * 2;
   }
   for (size_t b : st) stash_off_.push_back(probe.add(std::max<size_t>(b, 1)));
   for (size_t b : ws) ws_off_.push_back(ws_block_.add(std::max<size_t>(b, 1)));
@@ -854,6 +873,16 @@ size_t Stage::read_stash(int64_t mb, int index, void* host, size_t capacity) {
     }
     return n;
   }
+  if (opt_.packed && index < 13 * d_.num_layers) {
+    const int j = index % 13;
+    if (j == 4 || (j >= 7 && j <= 9) || j == 12) {   // through the workspace: no pass is using it
+      const DeviceGuard on(device_);
+      checkpoint(slot, {{index, ws<bf16_t>(13), j == 8 ? d_.dims[2] : d_.dims[0]}}, false);
+      sync();
+      hip_check(hipMemcpy(host, ws<char>(13), n, hipMemcpyDeviceToHost), "copy stash");
+      return n;
+    }
+  }
   hip_check(hipMemcpy(host, slot_blocks_[slot].at<char>(stash_off_[index]), n, hipMemcpyDeviceToHost), "copy stash");
   return n;
 }
@@ -903,6 +932,8 @@ void Stage::forward(int64_t mb, const void* x, void* y, const int32_t* labels, f
     hip_check(hipMemcpyAsync(wstash_.at<char>(wstash_off_[free_slot]), what_[0], n_arena_ * esz_,
                              hipMemcpyDeviceToDevice, ls_),
               "stash weights");
+  const auto masks = next_masks_.find(mb);
+  slots_[free_slot].masks = masks == next_masks_.end() ? spectrain_attention_masks{} : masks->second;
   switch (d_.kind) {
     case SPECTRAIN_KIND_FC: fwd_fc(free_slot, x, y, labels, loss); break;
     case SPECTRAIN_KIND_CONV3X3: fwd_conv(free_slot, x, y, labels, loss); break;
@@ -910,7 +941,8 @@ void Stage::forward(int64_t mb, const void* x, void* y, const int32_t* labels, f
     case SPECTRAIN_KIND_TRANSFORMER: fwd_tfm(free_slot, x, y, labels, loss); break;
     case SPECTRAIN_KIND_RESLSTM: fwd_lstm(free_slot, x, y, labels, loss); break;
   }
-  slots_[free_slot] = Slot{true, mb, x, y};
+  slots_[free_slot] = Slot{true, mb, x, y, slots_[free_slot].masks};
+  if (masks != next_masks_.end()) next_masks_.erase(masks);
 }
 
 void Stage::backward(int64_t mb, const void* dy, void* dx) {
@@ -1265,9 +1297,194 @@ void Stage::bwd_bneck(int slot, const void* dy, void* dx) {
   }
 }
 
+// ------------------------------------------------------- stage options ----
+void Stage::release_buffers() {
+  slots_.clear();
+  slot_blocks_.clear();
+  stash_off_.clear();
+  stash_bytes_.clear();
+  ws_off_.clear();
+  ws_block_.reset();
+  ws_block_f_.reset();
+  slopes_block_.reset();
+}
+
+// Other options mean other buffers: what the stage holds for passes is freed
+// and planned again.
+void Stage::reconfigure(Options next) {
+  if (d_.kind != SPECTRAIN_KIND_TRANSFORMER) fail("only transformer stages take positions, masks and an 8-bit stash");
+  for (const Slot& sl : slots_)
+    if (sl.used) throw StageError(SPECTRAIN_ESTATE, "a mini-batch is in flight");
+  const DeviceGuard on(device_);
+  sync();
+  hip_check(hipStreamSynchronize(s2_), "hipStreamSynchronize");
+  hip_check(hipStreamSynchronize(s3_), "hipStreamSynchronize");
+  const auto plan = [&](const Options& o) {
+    opt_ = o;
+    release_buffers();
+    const size_t at = slopes_block_.add(o.slopes.size() * sizeof(float));
+    slopes_block_.allocate();
+    if (!o.slopes.empty())
+      hip_check(hipMemcpy(slopes_block_.at<float>(at), o.slopes.data(), o.slopes.size() * sizeof(float),
+                          hipMemcpyHostToDevice),
+                "copy slopes");
+    plan_buffers();
+  };
+  const Options before = opt_;
+  try {
+    plan(next);
+  } catch (...) {
+    try {
+      plan(before);
+    } catch (...) {
+      release_buffers();   // no slots: every later pass is refused
+    }
+    throw;
+  }
+  if (!opt_.masked) next_masks_.clear();
+}
+
+spectrain_attention_desc Stage::masked_desc(const Options& o) const {
+  const int d = d_.dims[0], S = d_.dims[3];
+  spectrain_attention_desc a{};
+  a.abi_version = SPECTRAIN_ABI_VERSION;
+  a.dtype = SPECTRAIN_BF16;
+  a.batch = d_.batch;
+  a.heads = a.kv_heads = d_.dims[1];
+  a.head_dim = d / d_.dims[1];
+  a.q_len = a.kv_len = S;
+  a.causal = o.attn.causal;
+  a.scale = 1.0f / std::sqrt(static_cast<float>(a.head_dim));
+  a.cap = o.attn.cap;
+  a.q = a.k = a.v = a.dq = a.dk = a.dv = {static_cast<int64_t>(S) * 3 * d, 3 * d, a.head_dim};
+  a.out = a.dout = {static_cast<int64_t>(S) * d, d, a.head_dim};
+  return a;
+}
+
+spectrain_rotary_desc Stage::rotary_desc(const Options& o) const {
+  const int d = d_.dims[0], S = d_.dims[3];
+  spectrain_rotary_desc r{};
+  r.abi_version = SPECTRAIN_ABI_VERSION;
+  r.dtype = SPECTRAIN_BF16;
+  r.batch = d_.batch;
+  r.tokens = S;
+  r.heads = 2 * d_.dims[1];   // queries and keys lie side by side
+  r.head_dim = d / d_.dims[1];
+  r.rotary_dim = o.attn.rotary_dim;
+  r.layout = o.attn.rotary_layout;
+  r.scaling = o.attn.rotary_scaling;
+  r.original_length = o.attn.rotary_original_length;
+  r.base = o.attn.rotary_base;
+  r.factor = o.attn.rotary_factor;
+  r.x = r.out = {static_cast<int64_t>(S) * 3 * d, 3 * d, r.head_dim};
+  return r;
+}
+
+void Stage::set_attention(const spectrain_stage_attention* attn, const float* slopes) {
+  if (d_.kind != SPECTRAIN_KIND_TRANSFORMER) fail("only transformer stages take positions, masks and an 8-bit stash");
+  Options next = opt_;
+  next.masked = attn != nullptr;
+  next.attn = attn ? *attn : spectrain_stage_attention{};
+  next.slopes.clear();
+  if (!attn && slopes) fail("slopes need an attention");
+  if (attn) {
+    if (attn->abi_version != SPECTRAIN_ABI_VERSION) fail("abi_version mismatch");
+    if (attn->reserved != 0) fail("reserved must be 0");
+    if (attn->rotary_dim < 0) fail("rotary_dim must be >= 0");
+    const spectrain_attention_desc a = masked_desc(next);
+    (void)attention_workspace(&a, true);   // its checks
+    if (attn->rotary_dim) {
+      spectrain_rotary_desc r = rotary_desc(next);
+      if (static_cast<int64_t>(r.batch) * r.tokens >= 1 << 24) fail("batch * seq must be below 2^24");
+      r.batch = 0;                         // its checks, nothing enqueued
+      run_rotary(&r, nullptr, nullptr, 0, nullptr, s_);
+    }
+    if (slopes) {
+      next.slopes.assign(slopes, slopes + d_.dims[1]);
+      for (float v : next.slopes)
+        if (!std::isfinite(v)) fail("slopes must be finite");
+    }
+  }
+  reconfigure(std::move(next));
+}
+
+void Stage::set_stash(int format) {
+  if (format != SPECTRAIN_STASH_BF16 && format != SPECTRAIN_STASH_E4M3) fail("unknown stash format");
+  Options next = opt_;
+  next.packed = format == SPECTRAIN_STASH_E4M3;
+  const int64_t T = static_cast<int64_t>(d_.batch) * d_.dims[3], widest = std::max(d_.dims[0], d_.dims[2]);
+  if (next.packed && d_.kind == SPECTRAIN_KIND_TRANSFORMER && T * ((widest + 31) / 32) >= int64_t{1} << 27)
+    fail("batch * seq * features / 32 must be below 2^27 for an 8-bit stash");   // a layer's tensors share a launch
+  reconfigure(std::move(next));
+}
+
+void Stage::set_masks(int64_t mb, const spectrain_attention_masks* masks) {
+  if (!opt_.masked) throw StageError(SPECTRAIN_ESTATE, "masks need spectrain_stage_set_attention");
+  if (!masks) fail("masks is NULL");
+  if (masks->slopes) fail("slopes belong to the stage's attention");
+  if (masks->prefix && !opt_.attn.causal) fail("prefix needs a causal attention");
+  for (const int32_t* p : {masks->documents, masks->prefix, masks->kv_lengths})
+    if (reinterpret_cast<uintptr_t>(p) % 4) fail("a mask is not 4-byte aligned");
+  for (const Slot& sl : slots_)
+    if (sl.used && sl.mb == mb) throw StageError(SPECTRAIN_ESTATE, "mini-batch already in flight");
+  next_masks_[mb] = *masks;
+}
+
 // ======================================================= TRANSFORMER ====
+// Positions and masked attention of one layer; the workspace (id 12) is the
+// pass's own.
+void Stage::turn_heads(bf16_t* qkv, bool inverse) {
+  const spectrain_rotary_desc r = rotary_desc(opt_);
+  LAUNCH("rotary", 3.0 * r.batch * r.tokens * r.heads * r.rotary_dim, 4.0 * r.batch * r.tokens * r.heads * r.rotary_dim,
+         (run_rotary(&r, qkv, nullptr, inverse, qkv, ls_), hipSuccess));
+}
+
+void Stage::masked_fwd(int slot, const bf16_t* qkv, float* lse, bf16_t* ctx) {
+  const spectrain_attention_desc a = masked_desc(opt_);
+  spectrain_attention_masks m = slots_[slot].masks;
+  m.slopes = opt_.slopes.empty() ? nullptr : slopes_block_.at<float>(0);
+  const int d = d_.dims[0];
+  const double rows = static_cast<double>(a.batch) * a.heads * a.q_len, pairs = a.causal ? (a.q_len + 1) / 2.0 : a.q_len;
+  LAUNCH("attention_masked", 4.0 * rows * pairs * a.head_dim, 2.0 * a.batch * a.q_len * 4 * d + 4.0 * rows,
+         (run_attention_forward(&a, &m, qkv, qkv + d, qkv + 2 * d, ctx, lse, ws<void>(12), attention_workspace(&a, true),
+                                ls_),
+          hipSuccess));
+}
+
+void Stage::masked_bwd(int slot, const bf16_t* qkv, const bf16_t* ctx, const float* lse, const bf16_t* dctx,
+                       bf16_t* dqkv) {
+  const spectrain_attention_desc a = masked_desc(opt_);
+  spectrain_attention_masks m = slots_[slot].masks;
+  m.slopes = opt_.slopes.empty() ? nullptr : slopes_block_.at<float>(0);
+  const int d = d_.dims[0];
+  const double rows = static_cast<double>(a.batch) * a.heads * a.q_len, pairs = a.causal ? (a.q_len + 1) / 2.0 : a.q_len;
+  LAUNCH("attention_masked_bwd", 10.0 * rows * pairs * a.head_dim, 2.0 * a.batch * a.q_len * 8 * d + 4.0 * rows,
+         (run_attention_backward(&a, &m, qkv, qkv + d, qkv + 2 * d, ctx, lse, dctx, dqkv, dqkv + d, dqkv + 2 * d,
+                                 ws<void>(12), attention_workspace(&a, true), s_),
+          hipSuccess));
+}
+
+void Stage::checkpoint(int slot, std::initializer_list<Packed> bufs, bool pack) {
+  CheckpointArgs a[CHECKPOINT_MAX];
+  int n = 0;
+  double values = 0.0;
+  for (const Packed& b : bufs) {
+    CheckpointArgs& c = a[n++];
+    if (pack) c.x = b.values;
+    else c.out = b.values;
+    c.rows = static_cast<long>(d_.batch) * d_.dims[3];
+    c.cols = c.ld = b.cols;
+    c.codes = stash<uint8_t>(slot, b.id);
+    c.scales = c.codes + c.rows * c.cols;
+    values += static_cast<double>(c.rows) * c.cols;
+  }
+  if (pack) LAUNCH("checkpoint_pack", 0, values * (3 + 1.0 / 32), checkpoint_pack(a, n, 1, ls_));
+  else LAUNCH("checkpoint_restore", 0, values * (3 + 1.0 / 32), checkpoint_restore(a, n, 1, s_));
+}
+
 Stage::Attention Stage::attention() const {
   const int B = d_.batch, d = d_.dims[0], Hh = d_.dims[1], S = d_.dims[3];
+  if (opt_.masked) return Attention::kMasked;
   if (attention_fused_supported(S, d / Hh, d)) return Attention::kBlock;
   return attention_long_supported(B, Hh, d / Hh) && attention_long_preferred(B, S, Hh) ? Attention::kTiles
                                                                                        : Attention::kGemm;
@@ -1307,18 +1524,24 @@ void Stage::fwd_tfm(int slot, const void* x, void* y, const int32_t* labels, flo
     bf16_t* qkv = stash<bf16_t>(slot, q);
     float* P = stash<float>(slot, q + 1);
     bf16_t* Pb = stash<bf16_t>(slot, q + 2);
-    bf16_t* ctx = stash<bf16_t>(slot, q + 3);
-    bf16_t* r1 = stash<bf16_t>(slot, q + 4);
-    bf16_t* h = stash<bf16_t>(slot, q + 7);
-    bf16_t* f1 = stash<bf16_t>(slot, q + 8);
-    bf16_t* r2 = stash<bf16_t>(slot, q + 9);
-    void* out = l == L - 1 && !ce ? y : stash<void>(slot, q + 12);
+    // what is kept in 8 bits is computed in the workspace and packed at the layer's end
+    auto act = [&](int j, int w) { return opt_.packed ? ws<bf16_t>(w) : stash<bf16_t>(slot, q + j); };
+    bf16_t* ctx = stash<bf16_t>(slot, q + 3);   // 16 bits always: the attention gradient's row sums come from it
+    bf16_t* r1 = act(4, 7);
+    bf16_t* h = act(7, 6);
+    bf16_t* f1 = act(8, 5);
+    bf16_t* r2 = act(9, 4);
+    const bool keep_out = l < L - 1 || ce;
+    void* out = keep_out ? act(12, 2 + l % 2) : y;
 
     GemmDesc g = gd(T, 3 * d, d, opK(a, d), opK(wf(p), d), 3 * d);
     g.epi.bias_bf16 = static_cast<const bf16_t*>(wf(p + 1));
     g.epi.out_bf16 = qkv;
     gemm(g);
-    if (core == Attention::kTiles) {
+    if (core == Attention::kMasked) {
+      if (opt_.attn.rotary_dim) turn_heads(qkv, false);
+      masked_fwd(slot, qkv, P, ctx);
+    } else if (core == Attention::kTiles) {
       LAUNCH("attention_long", 4.0 * B * Hh * S * S * dh, 2.0 * T * 4 * d + 8.0 * B * Hh * S,
              attention_long_fwd(qkv, B, S, Hh, d, scale, P, ctx, ls_));
     } else if (core == Attention::kBlock) {
@@ -1360,6 +1583,12 @@ void Stage::fwd_tfm(int slot, const void* x, void* y, const int32_t* labels, flo
     LAUNCH("layernorm", 0, ln_bytes(T, d), layernorm_fwd(r2, static_cast<const bf16_t*>(wf(p + 10)), static_cast<const bf16_t*>(wf(p + 11)), T, d,
                             LN_EPS, static_cast<bf16_t*>(out), stash<float>(slot, q + 10), stash<float>(slot, q + 11),
                             ls_));
+    if (opt_.packed) {
+      if (keep_out)
+        checkpoint(slot, {{q + 4, r1, d}, {q + 7, h, d}, {q + 8, f1, F}, {q + 9, r2, d}, {q + 12, static_cast<bf16_t*>(out), d}}, true);
+      else
+        checkpoint(slot, {{q + 4, r1, d}, {q + 7, h, d}, {q + 8, f1, F}, {q + 9, r2, d}}, true);
+    }
     a = out;
   }
   if (ce) {   // logits of every token (float32), mean token cross-entropy, dlogits (bf16) for the backward
@@ -1375,7 +1604,8 @@ void Stage::fwd_tfm(int slot, const void* x, void* y, const int32_t* labels, flo
 
 // workspace ids: 0 scores/dP (f32; kTiles: row sums of P dP), 1 dS, 2/3 layer-output gradient ping-pong,
 // 4 dr2, 5 df1, 6 dh, 7 dr1, 8 dctx, 9 dqkv, 10 logits (f32, CE head),
-// 11 per-token losses (CE head), 12 column-sum partials
+// 11 per-token losses (CE head); with positions, masks or an 8-bit stash 12 masked attention, 13 f1, 14 r1, 15 h,
+// 16 r2 and 17 the layer input, restored; then column-sum partials
 void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
   const int L = d_.num_layers, B = d_.batch, d = d_.dims[0], Hh = d_.dims[1], F = d_.dims[2], S = d_.dims[3];
   const int T = B * S, dh = d / Hh;
@@ -1389,7 +1619,8 @@ void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
   if (d_.head == SPECTRAIN_HEAD_CE) {   // vocabulary head: its gradients and dY of the last layer
     const int V = d_.dims[4];
     const bf16_t* dl = stash<bf16_t>(slot, 13 * L);
-    const void* yL = stash<void>(slot, 13 * (L - 1) + 12);
+    const void* yL = opt_.packed ? ws<void>(17) : stash<void>(slot, 13 * (L - 1) + 12);
+    if (opt_.packed) checkpoint(slot, {{13 * (L - 1) + 12, ws<bf16_t>(17), d}}, false);
     GemmDesc gw = gd(V, d, T, opR(dl, V), opR(yL, d), d);
     gw.epi.out_f32 = grad(12 * L);
     gemm(gw);
@@ -1402,21 +1633,32 @@ void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
   }
   for (int l = L - 1; l >= 0; --l) {
     const int p = 12 * l, q = 13 * l;
-    const void* a = l == 0 ? sl.x : stash<void>(slot, 13 * (l - 1) + 12);
+    auto act = [&](int id, int w) { return opt_.packed ? ws<bf16_t>(w) : stash<bf16_t>(slot, id); };
+    const void* a = l == 0 ? sl.x : act(q - 1, 17);
     const bf16_t* qkv = stash<bf16_t>(slot, q);
     const float* P = stash<float>(slot, q + 1);
     const bf16_t* Pb = stash<bf16_t>(slot, q + 2);
     const bf16_t* ctx = stash<bf16_t>(slot, q + 3);
-    const bf16_t* r1 = stash<bf16_t>(slot, q + 4);
-    const bf16_t* h = stash<bf16_t>(slot, q + 7);
-    const bf16_t* f1 = stash<bf16_t>(slot, q + 8);
-    const bf16_t* r2 = stash<bf16_t>(slot, q + 9);
+    const bf16_t* r1 = act(q + 4, 14);
+    const bf16_t* h = act(q + 7, 15);
+    const bf16_t* f1 = act(q + 8, 13);
+    const bf16_t* r2 = act(q + 9, 16);
     bf16_t* dr2 = ws<bf16_t>(4);
     bf16_t* df1 = ws<bf16_t>(5);
     bf16_t* dhh = ws<bf16_t>(6);
     bf16_t* dr1 = ws<bf16_t>(7);
     bf16_t* dctx = ws<bf16_t>(8);
     bf16_t* dqkv = ws<bf16_t>(9);
+
+    if (opt_.packed) {   // this layer's activations, over those of the layer above
+      for (int w : {13, 15, 17}) protect(ws<void>(w));
+      if (l > 0)
+        checkpoint(slot, {{q + 4, ws<bf16_t>(14), d}, {q + 7, ws<bf16_t>(15), d}, {q + 8, ws<bf16_t>(13), F},
+                          {q + 9, ws<bf16_t>(16), d}, {q - 1, ws<bf16_t>(17), d}}, false);
+      else
+        checkpoint(slot, {{q + 4, ws<bf16_t>(14), d}, {q + 7, ws<bf16_t>(15), d}, {q + 8, ws<bf16_t>(13), F},
+                          {q + 9, ws<bf16_t>(16), d}}, false);
+    }
 
     // layer-norm backward rows on the stage stream; its parameter gradients
     // (and the FFN output bias gradient: column sums of dr2) reduced from the
@@ -1432,7 +1674,7 @@ void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
     });
     GemmDesc w2 = gd(d, F, T, opR(dr2, d), opR(f1, F), F);
     w2.epi.out_f32 = grad(p + 8);
-    side_gemm(w2, {dr2});
+    side_gemm(w2, {dr2, f1});
     GemmDesc x2 = gd(T, F, d, opK(dr2, d), opR(wb(p + 8), F), F);
     x2.epi.mask = f1;
     x2.epi.out_bf16 = df1;
@@ -1440,7 +1682,7 @@ void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
     gemm(x2);
     GemmDesc w1 = gd(F, d, T, opR(df1, F), opR(h, d), d);
     w1.epi.out_f32 = grad(p + 6);
-    side_gemm(w1, {df1});
+    side_gemm(w1, {df1, h});
     on_side({df1}, [&]() {
       LAUNCH("bias_grad", 0, colsum_bytes(T, F, 2), column_sum(df1, 1, T, F, F, grad(p + 7), 0, part2, ls_));
     });
@@ -1466,7 +1708,10 @@ void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
 
     // attention backward: fused, or batched GEMMs over (b, h)
     protect(dqkv);
-    if (core == Attention::kTiles) {
+    if (core == Attention::kMasked) {
+      masked_bwd(slot, qkv, ctx, P, dctx, dqkv);
+      if (opt_.attn.rotary_dim) turn_heads(dqkv, true);
+    } else if (core == Attention::kTiles) {
       LAUNCH("attention_long_bwd", 10.0 * B * Hh * S * S * dh, 2.0 * T * 7 * d + 8.0 * B * Hh * S,
              attention_long_bwd(qkv, dctx, P, B, S, Hh, d, scale, ws<float>(0), dqkv, s_));
     } else if (core == Attention::kBlock) {

@@ -47,6 +47,10 @@ class DeviceBlock {
   size_t add(size_t bytes);  // returns an offset; call before allocate()
   void allocate();
   void release();
+  void reset() {   // empty again: add() starts over
+    release();
+    total_ = 0;
+  }
   template <typename T>
   T* at(size_t off) const { return reinterpret_cast<T*>(base_ + off); }
   size_t bytes() const { return total_; }
@@ -147,6 +151,9 @@ class Stage {
   void set_state(const float* W, const float* v);
   void get_predicted(int slot, float* out);
   size_t read_stash(int64_t mb, int index, void* host, size_t capacity);
+  void set_attention(const spectrain_stage_attention* attn, const float* slopes);
+  void set_masks(int64_t mb, const spectrain_attention_masks* masks);
+  void set_stash(int format);
   bool nonfinite() const { return *reinterpret_cast<volatile int*>(flag_.host()) != 0; }
   void sync();
   // serial: every launch on the stage stream (forward_backward's forward and
@@ -160,6 +167,14 @@ class Stage {
     int64_t mb = -1;
     const void* x = nullptr;
     void* y = nullptr;
+    spectrain_attention_masks masks{};
+  };
+  // What a transformer stage's attention and stash add to its descriptor.
+  struct Options {
+    bool masked = false;               // attention with positions and masks
+    spectrain_stage_attention attn{};
+    std::vector<float> slopes;         // per head, or empty
+    bool packed = false;               // activations in flight as 8-bit checkpoints
   };
 
   // ---- layout and buffers
@@ -258,8 +273,23 @@ class Stage {
   void bwd_bneck(int slot, const void* dy, void* dx);
   // Which attention core the stage's shape takes: one block per head (S = 128),
   // tiles recomputed on chip, or batched GEMMs with stored probabilities.
-  enum class Attention { kBlock, kTiles, kGemm };
+  // With positions or masks it is the masked operator, whatever the shape.
+  enum class Attention { kBlock, kTiles, kGemm, kMasked };
   Attention attention() const;
+  void reconfigure(Options next);
+  void release_buffers();
+  spectrain_attention_desc masked_desc(const Options& o) const;
+  spectrain_rotary_desc rotary_desc(const Options& o) const;
+  void turn_heads(bf16_t* qkv, bool inverse);   // rotary positions of the query and key heads, in place
+  void masked_fwd(int slot, const bf16_t* qkv, float* lse, bf16_t* ctx);
+  void masked_bwd(int slot, const bf16_t* qkv, const bf16_t* ctx, const float* lse, const bf16_t* dctx, bf16_t* dqkv);
+  // Stash buffers of a packed stage: bf16 [T, cols] <-> stash buffer id.
+  struct Packed {
+    int id;
+    bf16_t* values;
+    long cols;
+  };
+  void checkpoint(int slot, std::initializer_list<Packed> bufs, bool pack);
   // Softmax probabilities of every head from a layer's qkv by the batched
   // GEMM: scores (workspace, float32) -> P and bf16(P).
   void attention_probs(const bf16_t* qkv, float* scores, float* P, bf16_t* Pb);
@@ -286,6 +316,10 @@ class Stage {
   const void* bwd_weights_ = nullptr;    // base of the weights the current backward reads
   HostCopy host_copy_;
   PinnedInts flag_;   // set by the update kernel on a non-finite value
+
+  Options opt_;
+  DeviceBlock slopes_block_;
+  std::map<int64_t, spectrain_attention_masks> next_masks_;   // of mini-batches whose forward is to come
 
   std::vector<Slot> slots_;
   std::vector<DeviceBlock> slot_blocks_;

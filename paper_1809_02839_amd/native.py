@@ -28,12 +28,14 @@ EXPORTED = ("spectrain_version_difference", "spectrain_stage_create", "spectrain
             "spectrain_stage_backward_noalloc", "spectrain_stage_forward_backward",
             "spectrain_stage_update", "spectrain_stage_get_state", "spectrain_stage_set_state",
             "spectrain_stage_get_predicted", "spectrain_stage_profile", "spectrain_stage_profile_read",
-            "spectrain_stage_read_stash", "spectrain_stage_destroy", "spectrain_rotary",
+            "spectrain_stage_read_stash", "spectrain_stage_destroy", "spectrain_stage_set_attention",
+            "spectrain_stage_set_masks", "spectrain_stage_set_stash", "spectrain_rotary",
             "spectrain_attention_workspace", "spectrain_attention_forward", "spectrain_attention_backward",
             "spectrain_checkpoint_pack", "spectrain_checkpoint_restore", "spectrain_last_error")
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
 CHECKPOINT_GROUP = 32
+STASH_FORMATS = {"bf16": 0, "e4m3": 1}
 
 
 class StageDesc(ctypes.Structure):
@@ -69,6 +71,13 @@ class AttentionDesc(ctypes.Structure):
 
 class AttentionMasks(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("documents", "prefix", "kv_lengths", "slopes")]
+
+
+class StageAttention(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_uint32), ("causal", ctypes.c_int32), ("cap", ctypes.c_float)] + [
+        (n, ctypes.c_int32) for n in ("rotary_dim", "rotary_layout", "rotary_scaling", "rotary_original_length",
+                                      "reserved")] + [("rotary_base", ctypes.c_double),
+                                                      ("rotary_factor", ctypes.c_double)]
 
 
 class SpecTrainError(RuntimeError):
@@ -107,6 +116,9 @@ def lib():
                                                             ctypes.POINTER(i32)]),
             "spectrain_stage_read_stash": (ctypes.c_int, [vp, i64, i32, vp, sz, ctypes.POINTER(sz)]),
             "spectrain_stage_destroy": (ctypes.c_int, [vp]),
+            "spectrain_stage_set_attention": (ctypes.c_int, [vp, ctypes.POINTER(StageAttention), fp]),
+            "spectrain_stage_set_masks": (ctypes.c_int, [vp, i64, ctypes.POINTER(AttentionMasks)]),
+            "spectrain_stage_set_stash": (ctypes.c_int, [vp, i32]),
             "spectrain_rotary": (ctypes.c_int, [ctypes.POINTER(RotaryDesc), vp, vp, i32, vp, vp]),
             "spectrain_attention_workspace": (ctypes.c_int, [ctypes.POINTER(AttentionDesc), i32, ctypes.POINTER(sz)]),
             "spectrain_attention_forward": (ctypes.c_int, [ctypes.POINTER(AttentionDesc),
@@ -261,6 +273,47 @@ class Stage:
             _check(lib().spectrain_stage_read_stash(self.h, mb, index, ctypes.c_void_p(out.ctypes.data), out.size,
                                                     ctypes.byref(n)))
         return out
+
+    def set_attention(self, causal=False, cap=0.0, slopes=None, rotary_dim=0, rotary_layout="half",
+                      rotary_base=10000.0, rotary_scaling="none", rotary_factor=1.0, rotary_original_length=0):
+        """Positions and masks of a transformer stage (slopes: `heads` values on the host)."""
+        a = StageAttention(ABI_VERSION, int(bool(causal)), cap, rotary_dim, ROTARY_LAYOUTS[rotary_layout],
+                           ROTARY_SCALINGS[rotary_scaling], rotary_original_length, 0, rotary_base, rotary_factor)
+        s = None if slopes is None else np.ascontiguousarray(slopes, dtype=np.float32)
+        if s is not None and s.shape != (self.desc.dims[1],):
+            raise ValueError(f"slopes must have {self.desc.dims[1]} values")
+        _check(lib().spectrain_stage_set_attention(self.h, ctypes.byref(a), _fptr(s)))
+
+    def clear_attention(self):
+        """Back to attention without positions and masks."""
+        _check(lib().spectrain_stage_set_attention(self.h, None, None))
+
+    def set_masks(self, mb: int, documents=None, prefix=None, kv_lengths=None):
+        """Masks of mini-batch mb for its coming forward and its backward; int32
+        device tensors, kept alive by the caller until the backward."""
+        B, S = self.desc.batch, self.desc.dims[3]
+        for t, shape, what in ((documents, (B, S), "documents"), (prefix, (B,), "prefix"),
+                               (kv_lengths, (B,), "kv_lengths")):
+            if t is not None and tuple(t.shape) != shape:
+                raise ValueError(f"{what} must have shape {shape}")
+        i32 = "torch.int32"
+        m = AttentionMasks(_dptr(documents, i32, "documents"), _dptr(prefix, i32, "prefix"),
+                           _dptr(kv_lengths, i32, "kv_lengths"), None)
+        _check(lib().spectrain_stage_set_masks(self.h, mb, ctypes.byref(m)))
+
+    def set_stash(self, format: str):
+        """How activations of mini-batches in flight are kept: "bf16" or "e4m3"."""
+        _check(lib().spectrain_stage_set_stash(self.h, STASH_FORMATS[format]))
+
+    def configure(self, spec):
+        """The attention and stash of a spec that names them (synth.StageSpec)."""
+        attention = getattr(spec, "attention", None)
+        if attention is not None:
+            o = dict(vars(attention))
+            o["slopes"] = attention.slope_values(spec.dims[1]) if o.pop("slopes") else None
+            self.set_attention(**o)
+        if getattr(spec, "stash", "bf16") != "bf16":
+            self.set_stash(spec.stash)
 
     def profile(self, enable: bool, serial: bool = False):
         """Time every launch (serial: each on the stage stream, one at a time)."""

@@ -99,6 +99,7 @@ class Pipeline:
         self.spec_of: Dict[int, object] = {}
         for spec, W0 in zip(self.specs, W0s):
             st = native.Stage(native.desc_from_spec(spec), W0, self.stream)
+            st.configure(spec)
             self.stages[spec.stage_index] = st
             self.spec_of[spec.stage_index] = spec
         if v0s is not None:
@@ -120,8 +121,11 @@ class Pipeline:
         return [(k, kind, m) for kind, m in stage_task_order(k, self.N, M)]
 
     def run(self, M: int, inputs: Callable, on_update: Optional[Callable] = None, keep_io: bool = False,
-            s_override: Optional[Tuple[int, int]] = None, on_forward: Optional[Callable] = None):
-        """Run M mini-batches. on_update(k, count, stage) is called after each
+            s_override: Optional[Tuple[int, int]] = None, on_forward: Optional[Callable] = None,
+            masks: Optional[Callable] = None):
+        """Run M mini-batches. masks(spec, m), where given, returns the attention
+        masks of mini-batch m at a stage as a dict of device tensors (see
+        native.Stage.set_masks), or None. on_update(k, count, stage) is called after each
         update, on_forward(k, m, stage) after each forward (synchronise inside
         them if device state is read). Returns
         {"loss": {m: device scalar}, "y": {(k, m): tensor}, "dx": {(k, m): tensor}}."""
@@ -130,6 +134,7 @@ class Pipeline:
         held_dy: Dict[Tuple[int, int], torch.Tensor] = {}
         dx_out: Dict[Tuple[int, int], torch.Tensor] = {}
         labels: Dict[Tuple[int, int], torch.Tensor] = {}
+        held_masks: Dict[Tuple[int, int], dict] = {}
         out = {"loss": {}, "y": {}, "dx": {}}
         counts = {k: 0 for k in self.stages}
         with torch.cuda.stream(self.stream):
@@ -147,6 +152,10 @@ class Pipeline:
                     dy = to_device(dy, spec, self.device)
                     lab = to_device(lab, spec, self.device, integer=True)
                     held_x[(k, m)] = x
+                    mk = masks(spec, m) if masks is not None else None
+                    if mk:
+                        held_masks[(k, m)] = mk
+                        st.set_masks(m, **mk)
                     if spec.head == "ce":
                         loss = torch.empty(1, dtype=torch.float32, device=self.device)
                         labels[(k, m)] = lab
@@ -179,6 +188,7 @@ class Pipeline:
                         if keep_io:
                             out["dx"][(k, m)] = dx
                     labels.pop((k, m), None)
+                    held_masks.pop((k, m), None)
                     # the stage no longer references its stash for m; upstream
                     # (k+1) has already run its backward, so y and x can go
                     held_x.pop((k, m), None)

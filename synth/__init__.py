@@ -17,13 +17,31 @@ so both sides see identical input bits.
 from __future__ import annotations
 
 import dataclasses
-from typing import Dict, List, Tuple
+from typing import Dict, List, Optional, Tuple
 
 import numpy as np
 
 KINDS = ("fc", "conv3x3", "bottleneck", "transformer", "reslstm")
 INIT_SEED = 1809
 DATA_SEED = 2839
+
+
+@dataclasses.dataclass(frozen=True)
+class AttentionSpec:
+    """Positions and masks of a transformer stage's attention."""
+
+    causal: bool = False
+    cap: float = 0.0               # 0: scores are not capped
+    slopes: bool = False           # bias by distance, slope 2^(-8 (h + 1) / heads) for head h
+    rotary_dim: int = 0            # 0: no rotary positions
+    rotary_layout: str = "half"    # or "interleaved"
+    rotary_base: float = 10000.0
+    rotary_scaling: str = "none"   # or "linear", "ntk", "parts"
+    rotary_factor: float = 1.0
+    rotary_original_length: int = 0
+
+    def slope_values(self, heads: int) -> np.ndarray:
+        return np.exp2(-8.0 * np.arange(1, heads + 1) / heads).astype(np.float32)
 
 
 @dataclasses.dataclass(frozen=True)
@@ -56,6 +74,10 @@ class StageSpec:
     # bottleneck: start every block's last convolution at zero, so each block
     # is the identity at initialisation (whole stacks without normalisation)
     zero_residual: bool = False
+    # transformer: positions and masks (None: neither), and how activations of
+    # mini-batches in flight are kept ("bf16", or "e4m3": 8-bit checkpoints)
+    attention: Optional[AttentionSpec] = None
+    stash: str = "bf16"
 
     # ----- shapes -------------------------------------------------------
     def fc_widths(self) -> List[int]:
