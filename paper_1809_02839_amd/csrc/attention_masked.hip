@@ -56,28 +56,77 @@ __device__ __forceinline__ float score(const Args& a, float acc, float& t) {
   }
 }
 
-// A thread's share of a KT x DH tile of rows (zero past `limit` rows and past
-// `dim` columns), and its copy into an LDS tile [KT][DH + 8].
+// A staged tile: KT rows of C 16-byte chunks in LDS, chunk c of row r in place
+// c ^ swizzle(r). The places are chosen so that the 32 rows of a row fragment
+// and the 4 x 2 rows of a transposing read each spread over all banks.
 template <int DH>
 struct Tile {
-  static constexpr int C = DH / 8, V = KT * C / NT;
+  static constexpr int C = DH <= 32 ? 4 : DH <= 64 ? 8 : 16, V = KT * C / NT, BYTES = KT * C * 16;
   static_assert(KT * C % NT == 0, "whole accesses");
-  uint4 v[V];
-  template <typename F>
-  __device__ __forceinline__ void load(int first, int limit, int dim, int tid, F&& address) {
+  static __device__ __forceinline__ int swizzle(int r) {
+    if (C == 16) return ((r & 3) << 2) | ((r >> 2) & 3);
+    if (C == 8) return ((r & 2) << 1) | ((r >> 2) & 3);
+    return (r >> 2) & 3;
+  }
+};
+
+__device__ uint4 zero16;   // what rows and columns outside a tensor are staged from
+
+// Direct load into LDS: the 16 bytes at lane l's address land at LDS byte
+// address lds + 16 l (lds wave-uniform, passed in M0). Issued through inline
+// assembly so that the compiler, which cannot tell the two buffers apart, does
+// not wait for the next tile before each read of this one; landed() waits for
+// the wave's own loads, and the barrier after it for the others'.
+__device__ __forceinline__ void direct16(const void* g, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(g) : "memory", "m0");
+}
+__device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
+}
+
+// Starts the copy of rows first .. first + KT - 1 (zero from `limit` on and from
+// column `dim` on); address(row) is a row's first element.
+template <int DH, typename F>
+__device__ __forceinline__ void stage(uint32_t lds, int first, int limit, int dim, int tid, F&& address) {
+  using T = Tile<DH>;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = tid + NT * i, row = first + e / C, col = (e % C) * 8;
-      v[i] = make_uint4(0, 0, 0, 0);
-      if (row < limit && col < dim) v[i] = *reinterpret_cast<const uint4*>(address(row) + col);
+  for (int i = 0; i < T::V; ++i) {
+    const int e = tid + NT * i, r = e / T::C, row = first + r, col = ((e % T::C) ^ T::swizzle(r)) * 8;
+    const void* g = &zero16;
+    if (row < limit && col < dim) g = address(row) + col;
+    direct16(g, lds + 16 * (64 * wave + NT * i));
+  }
+}
+
+// Byte offsets of a lane's fragments in a tile: rows c0 + lane % 32, columns
+// 16 q + 8 (lane / 32) .. at rows ^ (q << 5) + c0 * pitch; and, transposed (see
+// frag_cols), rows k0 .. + 15, columns 32 j .. at cols[half] ^ (j << 6) + k0 * pitch.
+template <int DH>
+struct Lane {
+  static constexpr int PITCH = Tile<DH>::C * 16;
+  uint32_t rows, cols[2];
+  __device__ __forceinline__ explicit Lane(int lane) {
+    const int r = lane & 31, g = lane >> 4, i = lane & 15;
+    rows = r * PITCH + (((lane >> 5) ^ Tile<DH>::swizzle(r)) << 4);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = 4 * (g >> 1) + (i >> 2) + 8 * h, chunk = 2 * (g & 1) + ((i & 3) >> 1);
+      cols[h] = k * PITCH + ((chunk ^ Tile<DH>::swizzle(k)) << 4) + 8 * (i & 1);
     }
   }
-  __device__ __forceinline__ void store(bf16_t* dst, int tid) const {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = tid + NT * i;
-      *reinterpret_cast<uint4*>(dst + (e / C) * (DH + 8) + (e % C) * 8) = v[i];
-    }
+  __device__ __forceinline__ bf16x8_t row_frag(const char* tile, int c0, int q) const {
+    return gld8(reinterpret_cast<const bf16_t*>(tile + c0 * PITCH + (rows ^ (q << 5))));
+  }
+  __device__ __forceinline__ bf16x8_t col_frag(const char* tile, int k0, int j) const {
+    const char* t = tile + k0 * PITCH;
+    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(t + (cols[0] ^ (j << 6))));
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(t + (cols[1] ^ (j << 6))));
+    const u16x8_t v = {static_cast<uint16_t>(lo[0]), static_cast<uint16_t>(lo[1]), static_cast<uint16_t>(lo[2]),
+                       static_cast<uint16_t>(lo[3]), static_cast<uint16_t>(hi[0]), static_cast<uint16_t>(hi[1]),
+                       static_cast<uint16_t>(hi[2]), static_cast<uint16_t>(hi[3])};
+    return __builtin_bit_cast(bf16x8_t, v);
   }
 };
 
@@ -92,21 +141,21 @@ __device__ __forceinline__ void load_row(const bf16_t* row, int dim, int lane, b
   }
 }
 
-// The wave's 32 rows (fragments fr) against rows c0 .. c0 + 31 of an LDS tile.
+// The wave's 32 rows (fragments fr) against rows c0 .. c0 + 31 of a tile.
 template <int DH>
-__device__ __forceinline__ f32x16_t product(const bf16x8_t (&fr)[DH / 16], const bf16_t* tile, int c0, int lane) {
+__device__ __forceinline__ f32x16_t product(const bf16x8_t (&fr)[DH / 16], const char* tile, int c0,
+                                            const Lane<DH>& at) {
   f32x16_t acc;
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = 0.0f;
 #pragma unroll
-  for (int q = 0; q < DH / 16; ++q)
-    acc = mfma(frag_rows<DH + 8>(tile, c0 + (lane & 31), 16 * q + 8 * (lane >> 5)), fr[q], acc);
+  for (int q = 0; q < DH / 16; ++q) acc = mfma(at.row_frag(tile, c0, q), fr[q], acc);
   return acc;
 }
 
-// acc += the group's values, rounded to bf16, times rows c0 .. of a [k][DH] tile.
+// acc += the group's values, rounded to bf16, times rows c0 .. of a tile.
 template <int DH>
-__device__ __forceinline__ void accumulate(const f32x16_t& v, const bf16_t* tile, int c0, int lane,
+__device__ __forceinline__ void accumulate(const f32x16_t& v, const char* tile, int c0, const Lane<DH>& at,
                                            f32x16_t (&acc)[DH / 32]) {
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
@@ -114,8 +163,7 @@ __device__ __forceinline__ void accumulate(const f32x16_t& v, const bf16_t* tile
                                pack_bf16x2(v[8 * c + 4], v[8 * c + 5]), pack_bf16x2(v[8 * c + 6], v[8 * c + 7]));
     const bf16x8_t fa = __builtin_bit_cast(bf16x8_t, u);
 #pragma unroll
-    for (int jn = 0; jn < DH / 32; ++jn)
-      acc[jn] = mfma(frag_cols<DH + 8>(tile, 32 * jn, c0 + 16 * c, lane), fa, acc[jn]);
+    for (int j = 0; j < DH / 32; ++j) acc[j] = mfma(at.col_frag(tile, c0 + 16 * c, j), fa, acc[j]);
   }
 }
 
@@ -191,23 +239,30 @@ __global__ __launch_bounds__(DT) void document_runs_kernel(const int32_t* ids, i
 
 // One block's place: its (sequence, kv head) and tile. Consecutive blocks take
 // different kv heads (of one XCD each where their number is a multiple of 8),
-// and the last rows first: they see the most keys under a causal mask.
+// and the tiles with the most work under a causal mask first: the last rows,
+// the first keys.
 struct Block {
   int b, kh, tile;
-  __device__ __forceinline__ Block(const Args& a) {
+  __device__ __forceinline__ Block(const Args& a, bool last_first) {
     const uint32_t x = blockIdx.x, t = a.by_bh.div(x), bh = x - t * a.by_bh.d;
     b = a.by_kv.div(bh);
     kh = bh - b * a.kv_heads;
-    tile = a.tiles - 1 - static_cast<int>(t);
+    tile = last_first ? a.tiles - 1 - static_cast<int>(t) : static_cast<int>(t);
   }
 };
 
+// How far (in powers of two) a score may pass the running maximum before the
+// sums are scaled anew: probabilities stay below 2^8, in float32 as exact as
+// below 1, and most tiles skip the pass over the result's registers.
+constexpr float SLACK = 8.0f;
+
 template <int DH, bool CAP>
 __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
-  __shared__ __attribute__((aligned(16))) bf16_t Ks[KT * (DH + 8)];
-  __shared__ __attribute__((aligned(16))) bf16_t Vs[KT * (DH + 8)];
-  const Block at(a);
+  using T = Tile<DH>;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, K or V
+  const Block at(a, true);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Lane<DH> frag(lane);
   const Sequence seq(a, at.b);
   const int row0 = at.tile * ROWS + 32 * wave, row = min(row0 + (lane & 31), a.rows - 1);
   const int i = a.by_group.div(row), head = at.kh * a.group + row - i * a.group, p = a.q_offset + i;
@@ -216,34 +271,32 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   const int2 wfirst = seq.keys(a, position(row0)), wlast = seq.keys(a, position(row0 + 31));
   const int begin = seq.keys(a, position(at.tile * ROWS)).x / KT * KT;
   const int end = seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y;
+  const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
+  const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
+  const auto fetch = [&](int k0, int buf) {
+    stage<DH>(lds_address(lds[buf][0]), k0, seq.limit, a.dim, tid, [&](int j) { return k + j * a.sk.t; });
+    stage<DH>(lds_address(lds[buf][1]), k0, seq.limit, a.dim, tid, [&](int j) { return v + j * a.sv.t; });
+  };
+  if (begin < end) fetch(begin, 0);
   const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
   bf16x8_t fq[DH / 16];
   load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq);
-  const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
-  const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
-  const auto krow = [&](int j) { return k + j * a.sk.t; };
-  const auto vrow = [&](int j) { return v + j * a.sv.t; };
 
   f32x16_t o[DH / 32];
   zero(o);
   float m = -INFINITY, sum = 0.0f;
-  Tile<DH> kr, vr;
-  kr.load(begin, seq.limit, a.dim, tid, krow);
-  vr.load(begin, seq.limit, a.dim, tid, vrow);
-  for (int k0 = begin; k0 < end; k0 += KT) {
+  int buf = 0;
+  for (int k0 = begin; k0 < end; k0 += KT, buf ^= 1) {
+    landed();
     __syncthreads();
-    kr.store(Ks, tid);
-    vr.store(Vs, tid);
-    __syncthreads();
-    kr.load(k0 + KT, seq.limit, a.dim, tid, krow);
-    vr.load(k0 + KT, seq.limit, a.dim, tid, vrow);
+    if (k0 + KT < end) fetch(k0 + KT, buf ^ 1);
     if (k0 >= wlast.y || k0 + KT <= wfirst.x) continue;
-    const bool cut = k0 < wlast.x || k0 + KT > wfirst.y;
+    const char *Ks = lds[buf][0], *Vs = lds[buf][1];
     f32x16_t s[KT / 32];
-    float top = m, t;
+    float t;
 #pragma unroll
     for (int n = 0; n < KT / 32; ++n) {
-      s[n] = product<DH>(fq, Ks, 32 * n, lane);
+      s[n] = product<DH>(fq, Ks, 32 * n, frag);
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[n][r] = score<CAP>(a, s[n][r], t);
     }
@@ -254,7 +307,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
         for (int r = 0; r < 16; ++r)
           s[n][r] -= slope * fabsf(static_cast<float>(p - (k0 + 32 * n + col_of(r, lane))));
     }
-    if (cut) {
+    if (k0 < wlast.x || k0 + KT > wfirst.y) {
 #pragma unroll
       for (int n = 0; n < KT / 32; ++n)
 #pragma unroll
@@ -263,19 +316,22 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
           if (j < mine.x || j >= mine.y) s[n][r] = -INFINITY;
         }
     }
+    float top = s[0][0];
 #pragma unroll
     for (int n = 0; n < KT / 32; ++n)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
     top = fmaxf(top, __shfl_xor(top, 32));
-    const float base = top == -INFINITY ? 0.0f : top;   // nothing seen so far weighs zero
-    const float shrink = __builtin_amdgcn_exp2f(m - base);
-    m = top;
-    sum *= shrink;
+    if (__any(top > m + SLACK)) {
+      const float next = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.0f : next));
+      m = next;
+      sum *= shrink;
 #pragma unroll
-    for (int jn = 0; jn < DH / 32; ++jn)
+      for (int j = 0; j < DH / 32; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[jn][r] *= shrink;
+        for (int r = 0; r < 16; ++r) o[j][r] *= shrink;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;   // nothing seen so far weighs zero
 #pragma unroll
     for (int n = 0; n < KT / 32; ++n) {
 #pragma unroll
@@ -283,7 +339,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
         s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - base);
         sum += s[n][r];
       }
-      accumulate<DH>(s[n], Vs, 32 * n, lane, o);
+      accumulate<DH>(s[n], Vs, 32 * n, frag, o);
     }
   }
   sum += __shfl_xor(sum, 32);
@@ -322,11 +378,12 @@ __device__ __forceinline__ float2 row_stats(const Args& a, int b, int head, int 
 }
 
 template <int DH, bool CAP>
-__global__ __launch_bounds__(NT, DH > 64 ? 1 : 2) void attention_masked_dq_kernel(Args a) {
-  __shared__ __attribute__((aligned(16))) bf16_t Ks[KT * (DH + 8)];
-  __shared__ __attribute__((aligned(16))) bf16_t Vs[KT * (DH + 8)];
-  const Block at(a);
+__global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
+  using T = Tile<DH>;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, K or V
+  const Block at(a, true);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Lane<DH> frag(lane);
   const Sequence seq(a, at.b);
   const int row0 = at.tile * ROWS + 32 * wave, row = min(row0 + (lane & 31), a.rows - 1);
   const int i = a.by_group.div(row), head = at.kh * a.group + row - i * a.group, p = a.q_offset + i;
@@ -335,71 +392,85 @@ __global__ __launch_bounds__(NT, DH > 64 ? 1 : 2) void attention_masked_dq_kerne
   const int2 wfirst = seq.keys(a, position(row0)), wlast = seq.keys(a, position(row0 + 31));
   const int begin = seq.keys(a, position(at.tile * ROWS)).x / KT * KT;
   const int end = seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y;
+  const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
+  const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
+  const auto fetch = [&](int k0, int buf) {
+    stage<DH>(lds_address(lds[buf][0]), k0, seq.limit, a.dim, tid, [&](int j) { return k + j * a.sk.t; });
+    stage<DH>(lds_address(lds[buf][1]), k0, seq.limit, a.dim, tid, [&](int j) { return v + j * a.sv.t; });
+  };
+  if (begin < end) fetch(begin, 0);
   const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
   bf16x8_t fq[DH / 16], fo[DH / 16];
   load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq);
   load_row<DH>(a.dout + at.b * a.sdo.b + i * a.sdo.t + head * a.sdo.h, a.dim, lane, fo);
   const float2 st = row_stats(a, at.b, head, i);
-  const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
-  const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
-  const auto krow = [&](int j) { return k + j * a.sk.t; };
-  const auto vrow = [&](int j) { return v + j * a.sv.t; };
 
   f32x16_t o[DH / 32];
   zero(o);
-  Tile<DH> kr, vr;
-  kr.load(begin, seq.limit, a.dim, tid, krow);
-  vr.load(begin, seq.limit, a.dim, tid, vrow);
-  for (int k0 = begin; k0 < end; k0 += KT) {
+  int buf = 0;
+  for (int k0 = begin; k0 < end; k0 += KT, buf ^= 1) {
+    landed();
     __syncthreads();
-    kr.store(Ks, tid);
-    vr.store(Vs, tid);
-    __syncthreads();
-    kr.load(k0 + KT, seq.limit, a.dim, tid, krow);
-    vr.load(k0 + KT, seq.limit, a.dim, tid, vrow);
+    if (k0 + KT < end) fetch(k0 + KT, buf ^ 1);
     if (k0 >= wlast.y || k0 + KT <= wfirst.x) continue;
+    const char *Ks = lds[buf][0], *Vs = lds[buf][1];
     const bool cut = k0 < wlast.x || k0 + KT > wfirst.y;
 #pragma unroll
     for (int n = 0; n < KT / 32; ++n) {
-      f32x16_t s = product<DH>(fq, Ks, 32 * n, lane);
-      const f32x16_t dp = product<DH>(fo, Vs, 32 * n, lane);
+      f32x16_t s = product<DH>(fq, Ks, 32 * n, frag);
+      const f32x16_t dp = product<DH>(fo, Vs, 32 * n, frag);
+      f32x16_t t;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int j = k0 + 32 * n + col_of(r, lane);
-        float t = 0.0f, x = score<CAP>(a, s[r], t);
-        if (a.slopes) x -= slope * fabsf(static_cast<float>(p - j));
-        float e = __builtin_amdgcn_exp2f(x - st.x) * (dp[r] - st.y);
-        if (CAP) e *= 1.0f - t * t;
-        if (cut && (j < mine.x || j >= mine.y)) e = 0.0f;
-        s[r] = e;
+        float tr;
+        s[r] = score<CAP>(a, s[r], tr);
+        if (CAP) t[r] = tr;
       }
-      accumulate<DH>(s, Ks, 32 * n, lane, o);
+      if (a.slopes) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[r] -= slope * fabsf(static_cast<float>(p - (k0 + 32 * n + col_of(r, lane))));
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(s[r] - st.x) * (dp[r] - st.y);
+        if (CAP) s[r] *= 1.0f - t[r] * t[r];
+      }
+      if (cut) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = k0 + 32 * n + col_of(r, lane);
+          if (j < mine.x || j >= mine.y) s[r] = 0.0f;
+        }
+      }
+      accumulate<DH>(s, Ks, 32 * n, frag, o);
     }
   }
   if (row0 + (lane & 31) >= a.rows) return;
   store_row<DH>(a.dq + at.b * a.sdq.b + i * a.sdq.t + head * a.sdq.h, a.dim, o, a.scale, lane);
 }
 
+// What dK and dV need of a staged row: log2 of its sum, delta, slope, position
+// and keys.
+struct RowInfo {
+  float sum[KT], delta[KT], slope[KT];
+  int position[KT], lo[KT], hi[KT];
+};
+
 // dK and dV of 128 keys: the wave's own 32 are keys, the walked columns rows.
 template <int DH, bool CAP>
-__global__ __launch_bounds__(NT, DH > 64 ? 1 : 2) void attention_masked_dkv_kernel(Args a) {
-  __shared__ __attribute__((aligned(16))) bf16_t Qs[KT * (DH + 8)];
-  __shared__ __attribute__((aligned(16))) bf16_t Os[KT * (DH + 8)];
-  __shared__ __attribute__((aligned(16))) float ls[KT], ds[KT], sl[KT];   // log2 sum, delta, slope of the staged rows
-  __shared__ __attribute__((aligned(16))) int lo[KT], hi[KT], ps[KT];     // their keys and positions
-  const Block at(a);
+__global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
+  using T = Tile<DH>;
+  __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, Q or dO
+  __shared__ __attribute__((aligned(16))) RowInfo info[2];
+  const Block at(a, false);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const Lane<DH> frag(lane);
   const Sequence seq(a, at.b);
   const int key0 = at.tile * ROWS, wkey0 = key0 + 32 * wave, key = wkey0 + (lane & 31);
   const int kc = min(key, a.kv_len - 1), valid = min(seq.limit, key0 + ROWS);
   const bf16_t* q = a.q + at.b * a.sq.b + at.kh * a.group * a.sq.h;
   const bf16_t* dout = a.dout + at.b * a.sdo.b + at.kh * a.group * a.sdo.h;
-  bf16x8_t fk[DH / 16], fv[DH / 16];
-  load_row<DH>(a.k + at.b * a.sk.b + kc * a.sk.t + at.kh * a.sk.h, kc < seq.limit ? a.dim : 0, lane, fk);
-  load_row<DH>(a.v + at.b * a.sv.b + kc * a.sv.t + at.kh * a.sv.h, kc < seq.limit ? a.dim : 0, lane, fv);
-  f32x16_t dk[DH / 32], dv[DH / 32];
-  zero(dk);
-  zero(dv);
   // rows that see one of the block's keys: positions [pa, pb)
   int pa = -(1 << 30), pb = 0x7fffffff;
   if (a.causal && key0 >= seq.prefix) pa = key0;
@@ -412,77 +483,106 @@ __global__ __launch_bounds__(NT, DH > 64 ? 1 : 2) void attention_masked_dkv_kern
   const int end = key0 < valid ? static_cast<int>(min(max(static_cast<long>(pb) - a.q_offset, 0L) * a.group,
                                                       static_cast<long>(a.rows)))
                                : 0;
-  const auto split = [&](int r, int& i, int& g) {
-    i = a.by_group.div(r);
-    g = r - i * a.group;
+  const auto fetch = [&](int r0, int buf) {
+    stage<DH>(lds_address(lds[buf][0]), r0, a.rows, a.dim, tid, [&](int r) {
+      const int i = a.by_group.div(r);
+      return q + i * a.sq.t + (r - i * a.group) * a.sq.h;
+    });
+    stage<DH>(lds_address(lds[buf][1]), r0, a.rows, a.dim, tid, [&](int r) {
+      const int i = a.by_group.div(r);
+      return dout + i * a.sdo.t + (r - i * a.group) * a.sdo.h;
+    });
   };
-  const auto qrow = [&](int r) {
-    int i, g;
-    split(r, i, g);
-    return q + i * a.sq.t + g * a.sq.h;
-  };
-  const auto orow = [&](int r) {
-    int i, g;
-    split(r, i, g);
-    return dout + i * a.sdo.t + g * a.sdo.h;
-  };
-  Tile<DH> qr, dor;
+  // rows past the last have an infinite sum: they weigh zero
   float sm = INFINITY, sd = 0.0f, ss = 0.0f;
   int2 sk = make_int2(0, 0);
   int sp = 0;
-  const auto fetch = [&](int r0) {
-    qr.load(r0, a.rows, a.dim, tid, qrow);
-    dor.load(r0, a.rows, a.dim, tid, orow);
+  const auto look = [&](int r0) {
     sm = INFINITY, sd = 0.0f, ss = 0.0f, sk = make_int2(0, 0), sp = 0;
     if (tid < KT && r0 + tid < a.rows) {
-      int i, g;
-      split(r0 + tid, i, g);
-      const int head = at.kh * a.group + g;
+      const int i = a.by_group.div(r0 + tid), head = at.kh * a.group + r0 + tid - i * a.group;
       const float2 st = row_stats(a, at.b, head, i);
       sm = st.x, sd = st.y, sp = a.q_offset + i;
       sk = seq.keys(a, sp);
       if (a.slopes) ss = a.slopes[head] * LOG2E;
     }
   };
-  fetch(begin);
-  for (int r0 = begin; r0 < end; r0 += KT) {
-    __syncthreads();
-    qr.store(Qs, tid);
-    dor.store(Os, tid);
+  const auto note = [&](int buf) {
     if (tid < KT) {
-      ls[tid] = sm, ds[tid] = sd, sl[tid] = ss;
-      lo[tid] = sk.x, hi[tid] = sk.y, ps[tid] = sp;
+      RowInfo& w = info[buf];
+      w.sum[tid] = sm, w.delta[tid] = sd, w.slope[tid] = ss;
+      w.position[tid] = sp, w.lo[tid] = sk.x, w.hi[tid] = sk.y;
     }
+  };
+  if (begin < end) {
+    fetch(begin, 0);
+    look(begin);
+    note(0);
+  }
+  bf16x8_t fk[DH / 16], fv[DH / 16];
+  load_row<DH>(a.k + at.b * a.sk.b + kc * a.sk.t + at.kh * a.sk.h, kc < seq.limit ? a.dim : 0, lane, fk);
+  load_row<DH>(a.v + at.b * a.sv.b + kc * a.sv.t + at.kh * a.sv.h, kc < seq.limit ? a.dim : 0, lane, fv);
+  f32x16_t dk[DH / 32], dv[DH / 32];
+  zero(dk);
+  zero(dv);
+  int buf = 0;
+  for (int r0 = begin; r0 < end; r0 += KT, buf ^= 1) {
+    landed();
     __syncthreads();
-    fetch(r0 + KT);
-    if (wkey0 >= valid) continue;
-    // rows past the last are staged with an infinite sum: they weigh zero
-    const int tail = min(KT, a.rows - r0) - 1;
-    if (wkey0 >= hi[tail] || wkey0 + 32 <= lo[0]) continue;
-    const bool cut = wkey0 < lo[tail] || wkey0 + 32 > hi[0];
-#pragma unroll
-    for (int n = 0; n < KT / 32; ++n) {
-      f32x16_t s = product<DH>(fk, Qs, 32 * n, lane);
-      f32x16_t dp = product<DH>(fv, Os, 32 * n, lane);
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int c = 32 * n + col_of(4 * g, lane);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * g + e;
-          float t = 0.0f, x = score<CAP>(a, s[r], t);
-          if (a.slopes) x -= sl[c + e] * fabsf(static_cast<float>(ps[c + e] - key));
-          float pr = __builtin_amdgcn_exp2f(x - ls[c + e]);
-          float z = pr * (dp[r] - ds[c + e]);
-          if (CAP) z *= 1.0f - t * t;
-          if (cut && (key < lo[c + e] || key >= hi[c + e])) pr = z = 0.0f;   // also where dP is not finite
-          s[r] = pr;
-          dp[r] = z;
-        }
-      }
-      accumulate<DH>(s, Os, 32 * n, lane, dv);
-      accumulate<DH>(dp, Qs, 32 * n, lane, dk);
+    const bool more = r0 + KT < end;
+    if (more) {
+      fetch(r0 + KT, buf ^ 1);
+      look(r0 + KT);
     }
+    const RowInfo& w = info[buf];
+    const int tail = min(KT, a.rows - r0) - 1;
+    if (wkey0 < valid && wkey0 < w.hi[tail] && wkey0 + 32 > w.lo[0]) {
+      const char *Qs = lds[buf][0], *Os = lds[buf][1];
+      const bool cut = wkey0 < w.lo[tail] || wkey0 + 32 > w.hi[0];
+#pragma unroll
+      for (int n = 0; n < KT / 32; ++n) {
+        f32x16_t s = product<DH>(fk, Qs, 32 * n, frag);
+        f32x16_t dp = product<DH>(fv, Os, 32 * n, frag);
+        f32x16_t t;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float tr;
+          s[r] = score<CAP>(a, s[r], tr);
+          if (CAP) t[r] = tr;
+        }
+        if (a.slopes) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int c = 32 * n + col_of(r, lane);
+            s[r] -= w.slope[c] * fabsf(static_cast<float>(w.position[c] - key));
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int c = 32 * n + col_of(4 * g, lane);
+          const float4 su = *reinterpret_cast<const float4*>(w.sum + c);
+          const float4 de = *reinterpret_cast<const float4*>(w.delta + c);
+          const float sus[4] = {su.x, su.y, su.z, su.w}, des[4] = {de.x, de.y, de.z, de.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * g + e;
+            s[r] = __builtin_amdgcn_exp2f(s[r] - sus[e]);
+            dp[r] = s[r] * (dp[r] - des[e]);
+            if (CAP) dp[r] *= 1.0f - t[r] * t[r];
+          }
+        }
+        if (cut) {   // both, also where dP is not finite
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int c = 32 * n + col_of(r, lane);
+            if (key < w.lo[c] || key >= w.hi[c]) s[r] = dp[r] = 0.0f;
+          }
+        }
+        accumulate<DH>(s, Os, 32 * n, frag, dv);
+        accumulate<DH>(dp, Qs, 32 * n, frag, dk);
+      }
+    }
+    if (more) note(buf ^ 1);
   }
   if (key >= a.kv_len) return;
   store_row<DH>(a.dk + at.b * a.sdk.b + key * a.sdk.t + at.kh * a.sdk.h, a.dim, dk, a.scale, lane);
