@@ -400,8 +400,9 @@ typedef struct {
   const float* slopes;
 } spectrain_attention_masks;   /* device pointers, each may be NULL */
 
-/* Bytes of workspace a forward or a backward needs (any masks and strides);
- * 256-byte aligned memory of that size is given to the calls. */
+/* Bytes of workspace a forward, or a backward (then enough for either), needs
+ * with any masks and strides; 256-byte aligned memory of that size is given to
+ * the calls. */
 int spectrain_attention_workspace(const spectrain_attention_desc* desc, int32_t backward, size_t* bytes);
 
 /* masks may be NULL (none). lse_dev may be NULL when no backward follows. */
