@@ -376,7 +376,8 @@ int spectrain_rotary(const spectrain_rotary_desc* desc, const void* x_dev, const
  *   slopes      float32 [heads]
  *   lse         float32 [batch, heads, q_len], contiguous
  * head_dim: a multiple of 8 up to 128; batch * heads * ceil(length / 32) below
- * 2^23 for both lengths. Strides are multiples of 8 elements and
+ * 2^23 for both lengths. 64 tokens of k and v, and 64 / group tokens by the
+ * heads of a group of q and dout, span at most 2^29 elements. Strides are multiples of 8 elements and
  * tensors 16-byte aligned. out may not overlap q, k, v; the gradients may not
  * overlap each other or an input, but all of them may be parts of one packed
  * tensor. */

@@ -9,6 +9,7 @@
 // r / group, head r % group of the group), so one staging of a key tile serves
 // the whole group.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "attention_tiles.hpp"
@@ -22,8 +23,9 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 struct Args : AttentionArgs {
   const int2* doc = nullptr;      // [batch][kv_len]: first and past-the-last token of the token's document
   float* delta = nullptr;         // [batch][heads][q_len]: out . dout (backward)
-  float c1 = 0.0f;                // uncapped: scale log2(e); capped: 2 scale / cap log2(e)
+  float c1 = 0.0f;                // uncapped: |scale| log2(e); capped: 2 |scale| / cap log2(e)
   float c2 = 0.0f;                // capped: cap log2(e)
+  int flip = 0;                   // scale < 0: one operand of the scores changes sign instead
   FastDiv by_group, by_bh, by_kv, by_pieces;
   int tiles = 0;
   int pieces = 1;                 // blocks that share a tile's walk, each writing a partial result
@@ -62,15 +64,12 @@ struct Sequence {
   }
 };
 
-// Score of one product in units of log2: s * log2(e), and tanh(z / cap).
-template <bool CAP>
+// Score of one product in units of log2: s log2(e), and tanh(z / cap) where
+// capped. PLAIN scores are the product times c1.
 __device__ __forceinline__ float score(const Args& a, float acc, float& t) {
-  if constexpr (CAP) {
-    t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(acc * a.c1));
-    return t * a.c2;
-  } else {
-    return acc * a.c1;
-  }
+  if (a.c2 == 0.0f) return acc * a.c1;
+  t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(acc * a.c1));
+  return t * a.c2;
 }
 
 // A staged tile: KT rows of C 16-byte chunks in LDS, chunk c of row r in place
@@ -87,35 +86,62 @@ struct Tile {
   }
 };
 
-__device__ uint4 zero16;   // what rows and columns outside a tensor are staged from
-
-// Direct load into LDS: the 16 bytes at lane l's address land at LDS byte
-// address lds + 16 l (lds wave-uniform, passed in M0). Issued through inline
-// assembly so that the compiler, which cannot tell the two buffers apart, does
-// not wait for the next tile before each read of this one; landed() waits for
-// the wave's own loads, and the barrier after it for the others'.
-__device__ __forceinline__ void direct16(const void* g, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(g) : "memory", "m0");
+// Direct load into LDS: the 16 bytes at lane l's byte offset from the resource's
+// base land at LDS byte address lds + 16 l (lds wave-uniform, passed in M0); an
+// offset past the resource writes zeros. Issued through inline assembly so that
+// the compiler, which cannot tell the two buffers apart, does not wait for the
+// next tile before each read of this one; landed() waits for the wave's own
+// loads, and the barrier after it for the others'. The statement declares M0
+// clobbered; nothing else in these kernels keeps a value in M0 (a host test
+// checks the assembly for it).
+__device__ __forceinline__ void direct16(__amdgpu_buffer_rsrc_t r, uint32_t lds, int off) {
+  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
+               : "memory", "m0");
 }
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const bf16_t* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(p), static_cast<short>(0), 0x7fffffe0, 0x00020000);
+}
+constexpr int OUTSIDE = 0x7ffffff0;   // past every resource
 __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
 }
 
-// Starts the copy of rows first .. first + KT - 1 (zero from `limit` on and from
-// column `dim` on); address(row) is a row's first element.
-template <int DH, typename F>
-__device__ __forceinline__ void stage(uint32_t lds, int first, int limit, int dim, int tid, F&& address) {
+// A thread's part of the copy of tiles of N rows by THREADS threads: its byte
+// offsets from the tile's first row, the same for every tile, so that a whole
+// tile costs no address arithmetic (with 64-bit addresses formed for each access
+// it was half of all vector instructions).
+template <int DH, int N, int THREADS>
+struct Loader {
   using T = Tile<DH>;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  static constexpr int V = N * T::C / THREADS;
+  int off[V];
+  // row(r): element offset of the tile's row r.
+  template <typename F>
+  __device__ __forceinline__ void init(int t, int dim, F&& row) {
 #pragma unroll
-  for (int i = 0; i < T::V; ++i) {
-    const int e = tid + NT * i, r = e / T::C, row = first + r, col = ((e % T::C) ^ T::swizzle(r)) * 8;
-    const void* g = &zero16;
-    if (row < limit && col < dim) g = address(row) + col;
-    direct16(g, lds + 16 * (64 * wave + NT * i));
+    for (int i = 0; i < V; ++i) {
+      const int e = t + THREADS * i, r = e / T::C, col = ((e % T::C) ^ T::swizzle(r)) * 8;
+      off[i] = col < dim ? static_cast<int>(2 * (row(r) + col)) : OUTSIDE;
+    }
   }
-}
+  // Starts the copy of rows first .. (zero from `limit` on) into LDS.
+  __device__ __forceinline__ void start(const bf16_t* base, uint32_t lds, int first, int limit, int t) const {
+    const __amdgpu_buffer_rsrc_t r = resource(base);
+    const uint32_t to = lds + (THREADS > 64 ? 1024 * __builtin_amdgcn_readfirstlane(t >> 6) : 0);
+    if (first + N <= limit) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) direct16(r, to + 16 * THREADS * i, off[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        direct16(r, to + 16 * THREADS * i, first + (t + THREADS * i) / T::C < limit ? off[i] : OUTSIDE);
+    }
+  }
+};
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int2 uniform(int2 v) { return make_int2(uniform(v.x), uniform(v.y)); }
 
 // Byte offsets of a lane's fragments in a tile: rows c0 + lane % 32, columns
 // 16 q + 8 (lane / 32) .. at rows ^ (q << 5) + c0 * pitch; and, transposed (see
@@ -155,12 +181,14 @@ struct Lane {
 };
 
 template <int DH>
-__device__ __forceinline__ void load_row(const bf16_t* row, int dim, int lane, bf16x8_t (&f)[DH / 16]) {
+__device__ __forceinline__ void load_row(const bf16_t* row, int dim, int lane, bf16x8_t (&f)[DH / 16], int flip = 0) {
+  const uint32_t sign = flip ? 0x80008000u : 0u;
 #pragma unroll
   for (int q = 0; q < DH / 16; ++q) {
     const int col = 16 * q + 8 * (lane >> 5);
     uint4 u = make_uint4(0, 0, 0, 0);
     if (col < dim) u = *reinterpret_cast<const uint4*>(row + col);
+    u.x ^= sign, u.y ^= sign, u.z ^= sign, u.w ^= sign;
     f[q] = __builtin_bit_cast(bf16x8_t, u);
   }
 }
@@ -225,59 +253,69 @@ __device__ __forceinline__ void store_part(float* out, int dim, const f32x16_t (
     }
 }
 
-// Documents: each token's run of equal numbers. A block owns 1024 tokens; runs
-// that cross its ends are followed outwards, a block's width at a time.
-constexpr int DT = 1024;
-__global__ __launch_bounds__(DT) void document_runs_kernel(const int32_t* ids, int len, FastDiv chunks, int2* runs) {
-  __shared__ int scan[2][DT];
-  __shared__ int edge[2];
-  const int b = chunks.div(blockIdx.x);
-  const int tid = threadIdx.x, first = (blockIdx.x - b * chunks.d) * DT, j = first + tid;
-  const int last = min(first + DT, len) - 1;
+// Documents: each token's run of equal numbers. A block owns a chunk of tokens,
+// one a thread; where a run crosses its ends it is followed outwards, four
+// chunks at a time.
+__global__ __launch_bounds__(1024) void document_runs_kernel(const int32_t* ids, int len, FastDiv chunks, int2* runs) {
+  __shared__ unsigned long long starts[16], ends[16];   // by wave: tokens that start, or end, a run
+  __shared__ int edge;
+  const int n = blockDim.x, b = chunks.div(blockIdx.x);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int first = (blockIdx.x - b * chunks.d) * n, j = first + tid, last = min(first + n, len) - 1;
   ids += static_cast<long>(b) * len;
   runs += static_cast<long>(b) * len;
   const bool in = j < len;
-  const int id = in ? ids[j] : 0;
-  // start of the first token's run: the first of the tokens before it that are all equal
-  int start = first;
-  for (int to = first; to > 0;) {
-    const int w = min(DT, to), base = to - w;
-    if (tid == 0) edge[0] = -1;
-    __syncthreads();
-    if (tid < w && ids[base + tid] != ids[first]) atomicMax(&edge[0], base + tid);
-    __syncthreads();
-    const int found = edge[0];
-    __syncthreads();
-    start = found < 0 ? base : found + 1;
-    if (found >= 0) break;
-    to = base;
-  }
-  int end = last + 1;
-  for (int from = last + 1; from < len;) {
-    const int w = min(DT, len - from);
-    if (tid == 0) edge[1] = 0x7fffffff;
-    __syncthreads();
-    if (tid < w && ids[from + tid] != ids[last]) atomicMin(&edge[1], from + tid);
-    __syncthreads();
-    const int found = edge[1];
-    __syncthreads();
-    end = found == 0x7fffffff ? from + w : found;
-    if (found != 0x7fffffff) break;
-    from += w;
-  }
-  // inside the block: the last start at or before a token, the first end after it
-  scan[0][tid] = tid == 0 ? start : (in && ids[j - 1] != id ? j : -1);
-  scan[1][tid] = j == last ? end : (in && j < last && ids[j + 1] != id ? j + 1 : 0x7fffffff);
+  const int id = in ? ids[j] : 0, before = in && j > 0 ? ids[j - 1] : 0, after = in && j < len - 1 ? ids[j + 1] : 0;
+  const unsigned long long s = __ballot(in && (j == 0 || before != id));
+  const unsigned long long e = __ballot(in && (j == len - 1 || after != id));
+  if (lane == 0) starts[wave] = s, ends[wave] = e;
   __syncthreads();
-  for (int step = 1; step < DT; step *= 2) {
-    const int s = tid >= step ? scan[0][tid - step] : -1;
-    const int e = tid + step < DT ? scan[1][tid + step] : 0x7fffffff;
-    __syncthreads();
-    scan[0][tid] = max(scan[0][tid], s);
-    scan[1][tid] = min(scan[1][tid], e);
-    __syncthreads();
+  int start = first, end = last + 1;   // of the runs that come in and go out
+  if (!(starts[0] & 1)) {
+    for (int to = first; to > 0;) {
+      const int w = min(4 * n, to), base = to - w;
+      if (tid == 0) edge = -1;
+      __syncthreads();
+      int found = -1;
+      for (int k = tid; k < w; k += n)
+        if (ids[base + k] != ids[first]) found = base + k;
+      if (found >= 0) atomicMax(&edge, found);
+      __syncthreads();
+      found = edge;
+      __syncthreads();
+      start = found < 0 ? base : found + 1;
+      if (found >= 0) break;
+      to = base;
+    }
   }
-  if (in) runs[j] = make_int2(scan[0][tid], scan[1][tid]);
+  if (!(ends[(last - first) >> 6] >> ((last - first) & 63) & 1)) {
+    for (int from = last + 1; from < len;) {
+      const int w = min(4 * n, len - from);
+      if (tid == 0) edge = 0x7fffffff;
+      __syncthreads();
+      int found = 0x7fffffff;
+      for (int k = tid; k < w; k += n)
+        if (ids[from + k] != ids[last]) found = min(found, from + k);
+      if (found != 0x7fffffff) atomicMin(&edge, found);
+      __syncthreads();
+      found = edge;
+      __syncthreads();
+      end = found == 0x7fffffff ? from + w : found;
+      if (found != 0x7fffffff) break;
+      from += w;
+    }
+  }
+  if (!in) return;
+  // the last start at or before the token, the first end at or after it
+  unsigned long long m = starts[wave] & (~0ull >> (63 - lane));
+  int w = wave;
+  while (m == 0 && w > 0) m = starts[--w];
+  const int x = m ? first + 64 * w + 63 - __clzll(m) : start;
+  m = ends[wave] & (~0ull << lane);
+  w = wave;
+  while (m == 0 && 64 * (w + 1) < n) m = ends[++w];
+  const int y = m ? first + 64 * w + __ffsll(m) : end;
+  runs[j] = make_int2(x, y);
 }
 
 // One block's place: its (sequence, kv head) and tile. Consecutive blocks take
@@ -308,25 +346,28 @@ struct Running {
 
   // Takes in 32 N keys from k0 on. cut: the tile's columns are compared with the
   // row's keys.
-  template <bool CAP, int N>
+  template <bool PLAIN, int N>
   __device__ __forceinline__ void take(const Args& a, const Lane<DH>& frag, const char* Ks, const char* Vs,
                                        const bf16x8_t (&fq)[DH / 16], int k0, int p, float slope, int2 mine, bool cut,
                                        int lane) {
     f32x16_t s[N];
-    float t;
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      s[n] = product<DH>(fq, Ks, 32 * n, frag);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[n][r] = score<CAP>(a, s[n][r], t);
-    }
-    if (a.slopes) {
+    for (int n = 0; n < N; ++n) s[n] = product<DH>(fq, Ks, 32 * n, frag);
+    if (!PLAIN) {
+      float t;
 #pragma unroll
       for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          s[n][r] -= slope * fabsf(static_cast<float>(p - (k0 + 32 * n + col_of(r, lane))));
+        for (int r = 0; r < 16; ++r) s[n][r] = score(a, s[n][r], t);
+      if (a.slopes) {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[n][r] -= slope * fabsf(static_cast<float>(p - (k0 + 32 * n + col_of(r, lane))));
+      }
     }
+    const float c1 = PLAIN ? a.c1 : 1.0f;   // s c1: the scores
     if (cut) {
 #pragma unroll
       for (int n = 0; n < N; ++n)
@@ -341,7 +382,7 @@ struct Running {
     for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[n][r]);
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = fmaxf(top, __shfl_xor(top, 32)) * c1;
     if (__any(top > m + SLACK)) {
       const float next = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - (next == -INFINITY ? 0.0f : next));
       m = next;
@@ -354,11 +395,13 @@ struct Running {
     const float base = m == -INFINITY ? 0.0f : m;   // nothing seen so far weighs zero
 #pragma unroll
     for (int n = 0; n < N; ++n) {
+      float part[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        s[n][r] = __builtin_amdgcn_exp2f(s[n][r] - base);
-        sum += s[n][r];
+        s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], c1, -base));
+        part[r & 1] += s[n][r];
       }
+      sum += part[0] + part[1];
       accumulate<DH>(s[n], Vs, 32 * n, frag, o);
     }
   }
@@ -370,7 +413,7 @@ __device__ __forceinline__ long row_index(const Args& a, int b, int head, int i)
 __device__ __forceinline__ float lse_of(float m, float sum) { return sum == 0.0f ? -INFINITY : m * LN2 + logf(sum); }
 
 // A block: 128 rows, or one piece of their keys.
-template <int DH, bool CAP>
+template <int DH, bool PLAIN>
 __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   using T = Tile<DH>;
   __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, K or V
@@ -382,20 +425,23 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   const int i = a.by_group.div(row), head = at.kh * a.group + row - i * a.group, p = a.q_offset + i;
   const int2 mine = seq.keys(a, p);
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
-  const int2 wfirst = seq.keys(a, position(row0)), wlast = seq.keys(a, position(row0 + 31));
-  int begin = seq.keys(a, position(at.tile * ROWS)).x / KT * KT;
-  int end = seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y;
+  const int2 wfirst = uniform(seq.keys(a, position(row0))), wlast = uniform(seq.keys(a, position(row0 + 31)));
+  int begin = uniform(seq.keys(a, position(at.tile * ROWS)).x / KT * KT);
+  int end = uniform(seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y);
   share<KT>(at.piece, a.pieces, begin, end);
   const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
   const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
+  Loader<DH, KT, NT> kl, vl;
+  kl.init(tid, a.dim, [&](int r) { return r * a.sk.t; });
+  vl.init(tid, a.dim, [&](int r) { return r * a.sv.t; });
   const auto fetch = [&](int k0, int buf) {
-    stage<DH>(lds_address(lds[buf][0]), k0, seq.limit, a.dim, tid, [&](int j) { return k + j * a.sk.t; });
-    stage<DH>(lds_address(lds[buf][1]), k0, seq.limit, a.dim, tid, [&](int j) { return v + j * a.sv.t; });
+    kl.start(k + k0 * a.sk.t, lds_address(lds[buf][0]), k0, seq.limit, tid);
+    vl.start(v + k0 * a.sv.t, lds_address(lds[buf][1]), k0, seq.limit, tid);
   };
   if (begin < end) fetch(begin, 0);
   const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
   bf16x8_t fq[DH / 16];
-  load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq);
+  load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq, a.flip);
 
   Running<DH> run;
   zero(run.o);
@@ -405,7 +451,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
     __syncthreads();
     if (k0 + KT < end) fetch(k0 + KT, buf ^ 1);
     if (k0 >= wlast.y || k0 + KT <= wfirst.x) continue;
-    run.template take<CAP, KT / 32>(a, frag, lds[buf][0], lds[buf][1], fq, k0, p, slope, mine,
+    run.template take<PLAIN, KT / 32>(a, frag, lds[buf][0], lds[buf][1], fq, k0, p, slope, mine,
                                     k0 < wlast.x || k0 + KT > wfirst.y, lane);
   }
   const float sum = run.sum + __shfl_xor(run.sum, 32);
@@ -425,10 +471,10 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
 // by reading the keys and values once, so the block's waves share out the keys,
 // each with tiles of 32 of its own that no other wave waits for, and join their
 // sums at the end.
-template <int DH, bool CAP>
+template <int DH, bool PLAIN>
 __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   using T = Tile<DH>;
-  constexpr int FT = 32, BYTES = T::BYTES / (KT / FT), V = FT * T::C / 64;
+  constexpr int FT = 32, BYTES = T::BYTES / (KT / FT);
   __shared__ __attribute__((aligned(16))) char lds[NT / 64][2][2][BYTES];   // wave, buffer, K or V
   __shared__ float2 ml[NT / 64][32];
   static_assert(4 * BYTES >= 32 * DH * 4, "a wave's tiles hold its result");
@@ -440,28 +486,22 @@ __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   const int i = a.by_group.div(row), head = at.kh * a.group + row - i * a.group, p = a.q_offset + i;
   const int2 mine = seq.keys(a, p);
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
-  const int2 first = seq.keys(a, position(row0)), last = seq.keys(a, position(row0 + 31));
+  const int2 first = uniform(seq.keys(a, position(row0))), last = uniform(seq.keys(a, position(row0 + 31)));
   int begin = first.x / FT * FT, end = last.y;
   share<FT>(at.piece * (NT / 64) + wave, a.pieces * (NT / 64), begin, end);
   const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
   const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
+  Loader<DH, FT, 64> kl, vl;
+  kl.init(lane, a.dim, [&](int r) { return r * a.sk.t; });
+  vl.init(lane, a.dim, [&](int r) { return r * a.sv.t; });
   const auto fetch = [&](int k0, int buf) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint32_t to = lds_address(lds[wave][buf][t]);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const int c = lane + 64 * e, r = c / T::C, j = k0 + r, col = ((c % T::C) ^ T::swizzle(r)) * 8;
-        const void* g = &zero16;
-        if (j < seq.limit && col < a.dim) g = (t == 0 ? k + j * a.sk.t : v + j * a.sv.t) + col;
-        direct16(g, to + 1024 * e);
-      }
-    }
+    kl.start(k + k0 * a.sk.t, lds_address(lds[wave][buf][0]), k0, seq.limit, lane);
+    vl.start(v + k0 * a.sv.t, lds_address(lds[wave][buf][1]), k0, seq.limit, lane);
   };
   if (begin < end) fetch(begin, 0);
   const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
   bf16x8_t fq[DH / 16];
-  load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq);
+  load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq, a.flip);
 
   Running<DH> run;
   zero(run.o);
@@ -470,7 +510,7 @@ __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
     landed();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other buffer has been read
     if (k0 + FT < end) fetch(k0 + FT, buf ^ 1);
-    run.template take<CAP, 1>(a, frag, lds[wave][buf][0], lds[wave][buf][1], fq, k0, p, slope, mine,
+    run.template take<PLAIN, 1>(a, frag, lds[wave][buf][0], lds[wave][buf][1], fq, k0, p, slope, mine,
                               k0 < last.x || k0 + FT > first.y, lane);
   }
   const float sum = run.sum + __shfl_xor(run.sum, 32);
@@ -568,34 +608,16 @@ __global__ __launch_bounds__(NT) void attention_sum_kernel(Sums all) {
       make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
 
-// delta = out . dout of every row, 16 lanes a row.
-__global__ __launch_bounds__(NT) void attention_delta_kernel(Args a, long rows, FastDiv by_heads, FastDiv by_len) {
-  const long r = static_cast<long>(blockIdx.x) * (NT / 16) + threadIdx.x / 16;
-  if (r >= rows) return;   // whole 16-lane groups leave
-  const uint32_t t = by_heads.div(static_cast<uint32_t>(r)), h = static_cast<uint32_t>(r) - t * by_heads.d;
-  const uint32_t b = by_len.div(t), i = t - b * by_len.d;
-  const int col = (threadIdx.x % 16) * 8;
-  float s = 0.0f;
-  if (col < a.dim) {
-    const u16x8_t o = *reinterpret_cast<const u16x8_t*>(a.out + b * a.so.b + i * a.so.t + h * a.so.h + col);
-    const u16x8_t d = *reinterpret_cast<const u16x8_t*>(a.dout + b * a.sdo.b + i * a.sdo.t + h * a.sdo.h + col);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(bf16_to_f32(o[e]), bf16_to_f32(d[e]), s);
-  }
-#pragma unroll
-  for (int w = 8; w >= 1; w /= 2) s += __shfl_xor(s, w);
-  if (threadIdx.x % 16 == 0) a.delta[(static_cast<long>(b) * a.heads + h) * a.q_len + i] = s;
+// log2 of a row's sum for the backward: infinite where the row has no weight,
+// so that every probability is zero.
+__device__ __forceinline__ float log2_sum(const Args& a, long row) {
+  const float l = a.lse[row];
+  return l == -INFINITY ? INFINITY : l * LOG2E;
 }
 
-// A row's statistics for the backward: log2 of its sum (infinite where the row
-// has no weight, so every probability is zero) and delta.
-__device__ __forceinline__ float2 row_stats(const Args& a, int b, int head, int i) {
-  const long at = (static_cast<long>(b) * a.heads + head) * a.q_len + i;
-  const float l = a.lse[at];
-  return make_float2(l == -INFINITY ? INFINITY : l * LOG2E, a.delta[at]);
-}
-
-template <int DH, bool CAP>
+// dQ of 128 rows (or a piece of it), and delta = out . dout of each for the
+// other kernel.
+template <int DH, bool PLAIN>
 __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   using T = Tile<DH>;
   __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, K or V
@@ -607,22 +629,39 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   const int i = a.by_group.div(row), head = at.kh * a.group + row - i * a.group, p = a.q_offset + i;
   const int2 mine = seq.keys(a, p);
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
-  const int2 wfirst = seq.keys(a, position(row0)), wlast = seq.keys(a, position(row0 + 31));
-  int begin = seq.keys(a, position(at.tile * ROWS)).x / KT * KT;
-  int end = seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y;
+  const int2 wfirst = uniform(seq.keys(a, position(row0))), wlast = uniform(seq.keys(a, position(row0 + 31)));
+  int begin = uniform(seq.keys(a, position(at.tile * ROWS)).x / KT * KT);
+  int end = uniform(seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y);
   share<KT>(at.piece, a.pieces, begin, end);
   const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
   const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
+  Loader<DH, KT, NT> kl, vl;
+  kl.init(tid, a.dim, [&](int r) { return r * a.sk.t; });
+  vl.init(tid, a.dim, [&](int r) { return r * a.sv.t; });
   const auto fetch = [&](int k0, int buf) {
-    stage<DH>(lds_address(lds[buf][0]), k0, seq.limit, a.dim, tid, [&](int j) { return k + j * a.sk.t; });
-    stage<DH>(lds_address(lds[buf][1]), k0, seq.limit, a.dim, tid, [&](int j) { return v + j * a.sv.t; });
+    kl.start(k + k0 * a.sk.t, lds_address(lds[buf][0]), k0, seq.limit, tid);
+    vl.start(v + k0 * a.sv.t, lds_address(lds[buf][1]), k0, seq.limit, tid);
   };
   if (begin < end) fetch(begin, 0);
   const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
   bf16x8_t fq[DH / 16], fo[DH / 16];
-  load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq);
+  load_row<DH>(a.q + at.b * a.sq.b + i * a.sq.t + head * a.sq.h, a.dim, lane, fq, a.flip);
   load_row<DH>(a.dout + at.b * a.sdo.b + i * a.sdo.t + head * a.sdo.h, a.dim, lane, fo);
-  const float2 st = row_stats(a, at.b, head, i);
+  const long at_row = row_index(a, at.b, head, i);
+  const float lsum = log2_sum(a, at_row);
+  float delta = 0.0f;
+  {
+    bf16x8_t f[DH / 16];
+    load_row<DH>(a.out + at.b * a.so.b + i * a.so.t + head * a.so.h, a.dim, lane, f);
+#pragma unroll
+    for (int q = 0; q < DH / 16; ++q) {
+      const u16x8_t x = __builtin_bit_cast(u16x8_t, f[q]), y = __builtin_bit_cast(u16x8_t, fo[q]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = fmaf(bf16_to_f32(x[e]), bf16_to_f32(y[e]), delta);
+    }
+    delta += __shfl_xor(delta, 32);
+    if (at.piece == 0 && lane < 32 && row0 + lane < a.rows) a.delta[at_row] = delta;
+  }
 
   f32x16_t o[DH / 32];
   zero(o);
@@ -638,22 +677,25 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
     for (int n = 0; n < KT / 32; ++n) {
       f32x16_t s = product<DH>(fq, Ks, 32 * n, frag);
       const f32x16_t dp = product<DH>(fo, Vs, 32 * n, frag);
-      f32x16_t t;
+      if (PLAIN) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float tr;
-        s[r] = score<CAP>(a, s[r], tr);
-        if (CAP) t[r] = tr;
-      }
-      if (a.slopes) {
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c1, -lsum)) * (dp[r] - delta);
+      } else {
+        f32x16_t t;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          s[r] -= slope * fabsf(static_cast<float>(p - (k0 + 32 * n + col_of(r, lane))));
-      }
+        for (int r = 0; r < 16; ++r) {
+          float tr = 0.0f;
+          s[r] = score(a, s[r], tr);
+          t[r] = tr;
+        }
+        if (a.slopes) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[r] = __builtin_amdgcn_exp2f(s[r] - st.x) * (dp[r] - st.y);
-        if (CAP) s[r] *= 1.0f - t[r] * t[r];
+          for (int r = 0; r < 16; ++r)
+            s[r] -= slope * fabsf(static_cast<float>(p - (k0 + 32 * n + col_of(r, lane))));
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r)   // t is 0 where there is no cap
+          s[r] = __builtin_amdgcn_exp2f(s[r] - lsum) * (dp[r] - delta) * (1.0f - t[r] * t[r]);
       }
       if (cut) {
 #pragma unroll
@@ -682,7 +724,7 @@ struct RowInfo {
 };
 
 // dK and dV of 128 keys: the wave's own 32 are keys, the walked columns rows.
-template <int DH, bool CAP>
+template <int DH, bool PLAIN>
 __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
   using T = Tile<DH>;
   __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, Q or dO
@@ -703,22 +745,36 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
     pb = seq.doc[valid - 1].y;
   }
   const long first = max(0L, static_cast<long>(pa) - a.q_offset) * a.group;
-  int begin = static_cast<int>(min(first, static_cast<long>(a.rows))) / KT * KT;
+  int begin = uniform(static_cast<int>(min(first, static_cast<long>(a.rows))) / KT * KT);
   int end = key0 < valid ? static_cast<int>(min(max(static_cast<long>(pb) - a.q_offset, 0L) * a.group,
                                                 static_cast<long>(a.rows)))
                          : 0;
+  end = uniform(end);
   share<KT>(at.piece, a.pieces, begin, end);
+  // Row r of the tile at r0 is query (r0 + r) / group of head (r0 + r) % group;
+  // its offset from the tile's first query is the same for every tile where the
+  // group divides the tile.
+  const auto offset = [&](const AttentionArgs::Strides& st, int r0, int r) {
+    const int i = a.by_group.div(r0 + r);
+    return (i - static_cast<int>(a.by_group.div(r0))) * st.t + (r0 + r - i * a.group) * st.h;
+  };
+  const bool regular = KT % a.group == 0;
+  Loader<DH, KT, NT> ql, dol;
+  ql.init(tid, a.dim, [&](int r) { return offset(a.sq, 0, r); });
+  dol.init(tid, a.dim, [&](int r) { return offset(a.sdo, 0, r); });
   const auto fetch = [&](int r0, int buf) {
-    int here = tid;
-    asm volatile("" : "+v"(here));   // as Lane::here
-    stage<DH>(lds_address(lds[buf][0]), r0, a.rows, a.dim, here, [&](int r) {
-      const int i = a.by_group.div(r);
-      return q + i * a.sq.t + (r - i * a.group) * a.sq.h;
-    });
-    stage<DH>(lds_address(lds[buf][1]), r0, a.rows, a.dim, here, [&](int r) {
-      const int i = a.by_group.div(r);
-      return dout + i * a.sdo.t + (r - i * a.group) * a.sdo.h;
-    });
+    const int i0 = a.by_group.div(r0);
+    const bf16_t *qb = q + i0 * a.sq.t, *ob = dout + i0 * a.sdo.t;
+    if (regular) {
+      ql.start(qb, lds_address(lds[buf][0]), r0, a.rows, tid);
+      dol.start(ob, lds_address(lds[buf][1]), r0, a.rows, tid);
+      return;
+    }
+    Loader<DH, KT, NT> l;
+    l.init(tid, a.dim, [&](int r) { return offset(a.sq, r0, r); });
+    l.start(qb, lds_address(lds[buf][0]), r0, a.rows, tid);
+    l.init(tid, a.dim, [&](int r) { return offset(a.sdo, r0, r); });
+    l.start(ob, lds_address(lds[buf][1]), r0, a.rows, tid);
   };
   // rows past the last have an infinite sum: they weigh zero
   float sm = INFINITY, sd = 0.0f, ss = 0.0f;
@@ -728,8 +784,8 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
     sm = INFINITY, sd = 0.0f, ss = 0.0f, sk = make_int2(0, 0), sp = 0;
     if (tid < KT && r0 + tid < a.rows) {
       const int i = a.by_group.div(r0 + tid), head = at.kh * a.group + r0 + tid - i * a.group;
-      const float2 st = row_stats(a, at.b, head, i);
-      sm = st.x, sd = st.y, sp = a.q_offset + i;
+      const long at_row = row_index(a, at.b, head, i);
+      sm = log2_sum(a, at_row), sd = a.delta[at_row], sp = a.q_offset + i;
       sk = seq.keys(a, sp);
       if (a.slopes) ss = a.slopes[head] * LOG2E;
     }
@@ -749,7 +805,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
   bf16x8_t fk[DH / 16], fv[DH / 16];
   f32x16_t dk[DH / 32], dv[DH / 32];
   const int kc = min(key, a.kv_len - 1), dim = kc < seq.limit ? a.dim : 0;
-  load_row<DH>(a.k + at.b * a.sk.b + kc * a.sk.t + at.kh * a.sk.h, dim, lane, fk);
+  load_row<DH>(a.k + at.b * a.sk.b + kc * a.sk.t + at.kh * a.sk.h, dim, lane, fk, a.flip);
   load_row<DH>(a.v + at.b * a.sv.b + kc * a.sv.t + at.kh * a.sv.h, dim, lane, fv);
   zero(dk);
   zero(dv);
@@ -773,19 +829,22 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
         f32x16_t s = product<DH>(fk, Qs, 32 * n, lf);
         f32x16_t dp = product<DH>(fv, Os, 32 * n, lf);
         f32x16_t t;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float tr;
-          s[r] = score<CAP>(a, s[r], tr);
-          if (CAP) t[r] = tr;
-        }
-        if (a.slopes) {
+        if (!PLAIN) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int c = 32 * n + col_of(r, lane);
-            s[r] -= w.slope[c] * fabsf(static_cast<float>(w.position[c] - key));
+            float tr = 0.0f;
+            s[r] = score(a, s[r], tr);
+            t[r] = 1.0f - tr * tr;
+          }
+          if (a.slopes) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int c = 32 * n + col_of(r, lane);
+              s[r] -= w.slope[c] * fabsf(static_cast<float>(w.position[c] - key));
+            }
           }
         }
+        const float c1 = PLAIN ? a.c1 : 1.0f;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           __builtin_amdgcn_sched_barrier(0);   // one group's statistics at a time: registers
@@ -796,9 +855,9 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = 4 * g + e;
-            s[r] = __builtin_amdgcn_exp2f(s[r] - sus[e]);
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c1, -sus[e]));
             dp[r] = s[r] * (dp[r] - des[e]);
-            if (CAP) dp[r] *= 1.0f - t[r] * t[r];
+            if (!PLAIN) dp[r] *= t[r];
           }
         }
         if (cut) {   // both, also where dP is not finite
@@ -855,8 +914,8 @@ Plan plan(const AttentionArgs& a) {
   const long row_tiles = (a.rows + ROWS - 1L) / ROWS, key_tiles = (a.kv_len + ROWS - 1L) / ROWS;
   p.few = a.rows <= 64;
   p.fwd = p.few ? pieces_for(bh * ((a.rows + 31) / 32), (a.kv_len + 127L) / 128, 1024, 2)
-                : pieces_for(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 768, 8);
-  p.dq = pieces_for(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 768, 8);
+                : pieces_for(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8);
+  p.dq = pieces_for(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8);
   p.dkv = pieces_for(bh * key_tiles, (a.rows + KT - 1L) / KT, 1024, 8);
   return p;
 }
@@ -870,24 +929,30 @@ hipError_t prepare(const AttentionArgs& in, Args& a, hipStream_t s) {
   a.by_group = FastDiv(in.group);
   a.by_bh = FastDiv(in.batch * in.kv_heads);
   a.by_kv = FastDiv(in.kv_heads);
-  a.c1 = in.cap > 0.0f ? 2.0f * in.scale / in.cap * LOG2E : in.scale * LOG2E;
+  // a scale of zero stays above it, so that hidden columns are still -infinity times it
+  const float scale = std::max(std::fabs(in.scale), 1e-30f);
+  a.c1 = in.cap > 0.0f ? 2.0f * scale / in.cap * LOG2E : scale * LOG2E;
   a.c2 = in.cap * LOG2E;
+  a.flip = in.scale < 0.0f;
   if (!in.documents || in.kv_len == 0) return hipSuccess;
   int2* runs = reinterpret_cast<int2*>(in.ws);
   a.doc = runs;
-  const unsigned chunks = (in.kv_len + DT - 1) / DT;
-  hipLaunchKernelGGL(document_runs_kernel, dim3(chunks * in.batch), dim3(DT), 0, s, in.documents, in.kv_len,
+  const int threads = std::min((in.kv_len + 63) / 64 * 64, 1024);
+  const unsigned chunks = (in.kv_len + threads - 1) / threads;
+  hipLaunchKernelGGL(document_runs_kernel, dim3(chunks * in.batch), dim3(threads), 0, s, in.documents, in.kv_len,
                      FastDiv(chunks), runs);
   return hipGetLastError();
 }
 
-// Calls f with the smallest compiled head width that holds dim, and the cap.
+// Calls f with the smallest compiled head width that holds dim, and whether
+// scores are products times the scale and no more.
 template <typename F>
-void with_width(int dim, bool cap, F&& f) {
+void with_width(const Args& a, F&& f) {
   auto pick = [&](auto width) {
-    if (cap) f(width, std::true_type{});
-    else f(width, std::false_type{});
+    if (a.cap > 0.0f || a.slopes) f(width, std::false_type{});
+    else f(width, std::true_type{});
   };
+  const int dim = a.dim;
   if (dim <= 32) pick(std::integral_constant<int, 32>{});
   else if (dim <= 64) pick(std::integral_constant<int, 64>{});
   else if (dim <= 96) pick(std::integral_constant<int, 96>{});
@@ -922,9 +987,9 @@ hipError_t attention_masked_fwd(const AttentionArgs& in, hipStream_t s) {
   const Plan p = plan(in);
   a.part = reinterpret_cast<float*>(in.ws + doc_bytes(in));
   a.part_ml = reinterpret_cast<float2*>(in.ws + doc_bytes(in) + part_bytes(p.fwd, q_rows(in), in.dim));
-  with_width(a.dim, a.cap > 0.0f, [&](auto width, auto cap) {
-    e = p.few ? launch(attention_masked_few_kernel<width(), cap()>, a, a.rows, 32, p.fwd, s)
-              : launch(attention_masked_fwd_kernel<width(), cap()>, a, a.rows, ROWS, p.fwd, s);
+  with_width(a, [&](auto width, auto plain) {
+    e = p.few ? launch(attention_masked_few_kernel<width(), plain()>, a, a.rows, 32, p.fwd, s)
+              : launch(attention_masked_fwd_kernel<width(), plain()>, a, a.rows, ROWS, p.fwd, s);
   });
   if (e != hipSuccess || p.fwd == 1) return e;
   const long rows = static_cast<long>(q_rows(in));
@@ -955,23 +1020,17 @@ hipError_t attention_masked_bwd(const AttentionArgs& in, hipStream_t s) {
     sums.sum[nsums++] = {part, out, to, static_cast<long>(rows), FastDiv(heads), FastDiv(tokens), pieces};
     most = std::max(most, static_cast<long>(rows));
   };
-  if (a.q_len > 0) {
-    const long rows = static_cast<long>(q_rows(in));
-    hipLaunchKernelGGL(attention_delta_kernel, dim3(static_cast<unsigned>((rows + NT / 16 - 1) / (NT / 16))), dim3(NT),
-                       0, s, a, rows, FastDiv(a.heads), FastDiv(a.q_len));
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  with_width(a.dim, a.cap > 0.0f, [&](auto width, auto cap) {
+  with_width(a, [&](auto width, auto plain) {
     if (a.q_len > 0) {
       a.part = part_q;
-      e = launch(attention_masked_dq_kernel<width(), cap()>, a, a.rows, ROWS, p.dq, s);
+      e = launch(attention_masked_dq_kernel<width(), plain()>, a, a.rows, ROWS, p.dq, s);
       if (e != hipSuccess) return;
       if (p.dq > 1) sum(part_q, a.dq, a.sdq, q_rows(in), a.heads, a.q_len, p.dq);
     }
     if (a.kv_len == 0) return;
     a.part = part_k;
     a.part2 = part_v;
-    e = launch(attention_masked_dkv_kernel<width(), cap()>, a, a.kv_len, ROWS, p.dkv, s);
+    e = launch(attention_masked_dkv_kernel<width(), plain()>, a, a.kv_len, ROWS, p.dkv, s);
     if (e != hipSuccess) return;
     if (p.dkv > 1) {
       sum(part_k, a.dk, a.sdk, k_rows(in), a.kv_heads, a.kv_len, p.dkv);

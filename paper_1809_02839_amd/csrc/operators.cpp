@@ -144,6 +144,17 @@ AttentionArgs attention_args(const spectrain_attention_desc* desc, bool backward
       check_strides(d.dv, 8, "dv");
     }
   }
+  if (layout) {   // byte offsets inside a tile of 64 rows are 32 bits wide
+    const int64_t g = d.heads / d.kv_heads, q = std::min<int64_t>(d.q_len, 64 / g + 1), k = std::min(d.kv_len, 64);
+    const auto span = [&](const spectrain_strides& st, int64_t tokens, int64_t heads, const char* what) {
+      if (std::max<int64_t>(tokens - 1, 0) * st.token + (heads - 1) * st.head >= int64_t{1} << 29)
+        fail(std::string(what) + ": 64 tokens, and the heads of a group, may span at most 2^29 elements");
+    };
+    span(d.q, q, g, "q");
+    span(d.k, k, 1, "k");
+    span(d.v, k, 1, "v");
+    if (backward) span(d.dout, q, g, "dout");
+  }
   AttentionArgs a;
   a.batch = d.batch;
   a.heads = d.heads;
