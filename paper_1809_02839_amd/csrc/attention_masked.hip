@@ -26,22 +26,30 @@ struct Args : AttentionArgs {
   float c1 = 0.0f;                // uncapped: |scale| log2(e); capped: 2 |scale| / cap log2(e)
   float c2 = 0.0f;                // capped: cap log2(e)
   int flip = 0;                   // scale < 0: one operand of the scores changes sign instead
-  FastDiv by_group, by_bh, by_kv, by_pieces;
+  FastDiv by_group, by_bh, by_kv, by_tiles;
   int tiles = 0;
-  int pieces = 1;                 // blocks that share a tile's walk, each writing a partial result
+  int pieces = 1;                 // most pieces that a tile's walk is cut into, a block each
+  int quantum = 1;                // fewest steps of a piece
   float* part = nullptr;          // [pieces][...][dim] partial results (pieces > 1)
   float2* part_ml = nullptr;      // [pieces][batch][heads][q_len] maximum and sum (forward)
   float* part2 = nullptr;         // dV's (part is dK's)
 };
 
-// The piece'th of `pieces` equal shares of the tiles of width W in [begin, end).
+// A walk over [begin, end) in steps of W is cut into at most a.pieces equal
+// pieces, none shorter than about a.quantum steps: long walks are shared out,
+// short ones stay whole and write their results at once.
 template <int W>
-__device__ __forceinline__ void share(int piece, int pieces, int& begin, int& end) {
-  if (pieces == 1) return;
-  const long n = max(0, (end - begin + W - 1) / W);
-  const int b = begin;
-  begin = b + static_cast<int>(n * piece / pieces) * W;
-  end = min(end, b + static_cast<int>(n * (piece + 1) / pieces) * W);
+__device__ __forceinline__ int pieces_of(const Args& a, int begin, int end) {
+  if (a.pieces == 1) return 1;
+  const int steps = max(0, end - begin + W - 1) / W;
+  return max(1, min(a.pieces, (steps + a.quantum - 1) / a.quantum));
+}
+// The n'th of `of` equal shares.
+template <int W>
+__device__ __forceinline__ void share(int n, int of, int& begin, int& end) {
+  const int steps = max(0, end - begin + W - 1) / W, b = begin, part = steps / of, rest = steps - part * of;
+  begin = b + (n * part + min(n, rest)) * W;
+  end = min(end, b + ((n + 1) * part + min(n + 1, rest)) * W);
 }
 
 struct Sequence {
@@ -53,16 +61,39 @@ struct Sequence {
         doc(a.doc ? a.doc + static_cast<long>(b) * a.kv_len : nullptr) {}
   // Keys [x, y) that the row at position p sees (none if y <= x).
   __device__ __forceinline__ int2 keys(const Args& a, int p) const {
-    int lo = 0, hi = limit;
+    return clip(a, p, doc ? doc[p] : make_int2(0, 0x7fffffff));
+  }
+  // The same from its document's first and past-the-last token.
+  __device__ __forceinline__ int2 clip(const Args& a, int p, int2 d) const {
+    int hi = min(limit, d.y);
     if (a.causal) hi = min(hi, max(p + 1, prefix));
-    if (doc) {
-      const int2 d = doc[p];
-      lo = d.x;
-      hi = min(hi, d.y);
-    }
-    return make_int2(lo, hi);
+    return make_int2(d.x, hi);
   }
 };
+
+// Keys that the rows [row0, row0 + n) see between them, from a multiple of W on.
+template <int W>
+__device__ __forceinline__ int2 key_walk(const Args& a, const Sequence& seq, int row0, int n) {
+  const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
+  return make_int2(seq.keys(a, position(row0)).x / W * W, seq.keys(a, position(row0 + n - 1)).y);
+}
+
+// Rows that see one of the keys [key0, key0 + n), from a multiple of W on.
+template <int W>
+__device__ __forceinline__ int2 row_walk(const Args& a, const Sequence& seq, int key0, int n) {
+  const int valid = min(seq.limit, key0 + n);
+  if (key0 >= valid) return make_int2(0, 0);
+  int pa = -(1 << 30), pb = 0x7fffffff;   // their positions
+  if (a.causal && key0 >= seq.prefix) pa = key0;
+  if (seq.doc) {
+    pa = max(pa, seq.doc[key0].x);
+    pb = seq.doc[valid - 1].y;
+  }
+  const auto row = [&](int p) {
+    return static_cast<int>(min(max(static_cast<long>(p) - a.q_offset, 0L) * a.group, static_cast<long>(a.rows)));
+  };
+  return make_int2(row(pa) / W * W, row(pb));
+}
 
 // Score of one product in units of log2: s log2(e), and tanh(z / cap) where
 // capped. PLAIN scores are the product times c1.
@@ -321,12 +352,12 @@ __global__ __launch_bounds__(1024) void document_runs_kernel(const int32_t* ids,
 // One block's place: its (sequence, kv head) and tile. Consecutive blocks take
 // different kv heads (of one XCD each where their number is a multiple of 8),
 // and the tiles with the most work under a causal mask first: the last rows,
-// the first keys.
+// the first keys. Blocks that run together walk the same pieces.
 struct Block {
   int b, kh, tile, piece;
   __device__ __forceinline__ Block(const Args& a, bool last_first) {
-    const uint32_t x = blockIdx.x, tp = a.by_bh.div(x), bh = x - tp * a.by_bh.d, t = a.by_pieces.div(tp);
-    piece = tp - t * a.by_pieces.d;
+    const uint32_t x = blockIdx.x, pt = a.by_bh.div(x), bh = x - pt * a.by_bh.d, t = pt - a.by_tiles.div(pt) * a.tiles;
+    piece = a.by_tiles.div(pt);
     b = a.by_kv.div(bh);
     kh = bh - b * a.kv_heads;
     tile = last_first ? a.tiles - 1 - static_cast<int>(t) : static_cast<int>(t);
@@ -426,9 +457,11 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   const int2 mine = seq.keys(a, p);
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
   const int2 wfirst = uniform(seq.keys(a, position(row0))), wlast = uniform(seq.keys(a, position(row0 + 31)));
-  int begin = uniform(seq.keys(a, position(at.tile * ROWS)).x / KT * KT);
-  int end = uniform(seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y);
-  share<KT>(at.piece, a.pieces, begin, end);
+  const int2 walk = uniform(key_walk<KT>(a, seq, at.tile * ROWS, ROWS));
+  int begin = walk.x, end = walk.y;
+  const int pieces = pieces_of<KT>(a, begin, end);
+  if (at.piece >= pieces) return;
+  share<KT>(at.piece, pieces, begin, end);
   const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
   const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
   Loader<DH, KT, NT> kl, vl;
@@ -457,7 +490,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   const float sum = run.sum + __shfl_xor(run.sum, 32);
   if (row0 + (lane & 31) >= a.rows) return;
   const long r = row_index(a, at.b, head, i);
-  if (a.pieces > 1) {
+  if (pieces > 1) {
     const long rp = at.piece * static_cast<long>(a.batch) * a.heads * a.q_len + r;
     store_part<DH>(a.part + rp * a.dim, a.dim, run.o, 1.0f, lane);
     if (lane < 32) a.part_ml[rp] = make_float2(run.m, sum);
@@ -488,7 +521,9 @@ __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
   const int2 first = uniform(seq.keys(a, position(row0))), last = uniform(seq.keys(a, position(row0 + 31)));
   int begin = first.x / FT * FT, end = last.y;
-  share<FT>(at.piece * (NT / 64) + wave, a.pieces * (NT / 64), begin, end);
+  const int pieces = pieces_of<FT>(a, begin, end);
+  if (at.piece >= pieces) return;
+  share<FT>(at.piece * (NT / 64) + wave, pieces * (NT / 64), begin, end);
   const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
   const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
   Loader<DH, FT, 64> kl, vl;
@@ -536,7 +571,7 @@ __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
     }
     const int ri = a.by_group.div(rr), rh = at.kh * a.group + rr - ri * a.group;
     const long at_row = row_index(a, at.b, rh, ri);
-    if (a.pieces > 1) {
+    if (pieces > 1) {
       const long rp = at.piece * static_cast<long>(a.batch) * a.heads * a.q_len + at_row;
       *reinterpret_cast<float4*>(a.part + rp * a.dim + col) = x;
       if (col == 0) a.part_ml[rp] = make_float2(m, l);
@@ -549,16 +584,26 @@ __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   }
 }
 
-// Joins the pieces of the forward: 16 lanes a row, eight columns each.
-__global__ __launch_bounds__(NT) void attention_join_kernel(Args a, long rows, FastDiv by_len, FastDiv by_heads) {
+// Joins the pieces of the forward: 16 lanes a row, eight columns each. few: the
+// pieces are those of the kernel for few rows.
+__global__ __launch_bounds__(NT) void attention_join_kernel(Args a, long rows, FastDiv by_len, FastDiv by_heads,
+                                                            int few) {
   const long r = static_cast<long>(blockIdx.x) * (NT / 16) + threadIdx.x / 16;
   const int col = threadIdx.x % 16 * 8;
   if (r >= rows || col >= a.dim) return;
+  const uint32_t bh = by_len.div(static_cast<uint32_t>(r)), i = static_cast<uint32_t>(r) - bh * by_len.d;
+  const uint32_t b = by_heads.div(bh), h = bh - b * by_heads.d;
+  const Sequence seq(a, b);
+  const int packed = i * a.group + (h - a.by_group.div(h) * a.group), tile = few ? 32 : ROWS;
+  const int2 walk = few ? key_walk<32>(a, seq, packed / tile * tile, tile)
+                        : key_walk<KT>(a, seq, packed / tile * tile, tile);
+  const int pieces = few ? pieces_of<32>(a, walk.x, walk.y) : pieces_of<KT>(a, walk.x, walk.y);
+  if (pieces == 1) return;   // written already
   float m = -INFINITY;
-  for (int u = 0; u < a.pieces; ++u) m = fmaxf(m, a.part_ml[u * rows + r].x);
+  for (int u = 0; u < pieces; ++u) m = fmaxf(m, a.part_ml[u * rows + r].x);
   const float base = m == -INFINITY ? 0.0f : m;
   float l = 0.0f, x[8] = {};
-  for (int u = 0; u < a.pieces; ++u) {
+  for (int u = 0; u < pieces; ++u) {
     const float2 ml = a.part_ml[u * rows + r];
     const float w = __builtin_amdgcn_exp2f(ml.x - base);
     const float4* y = reinterpret_cast<const float4*>(a.part + (u * rows + r) * a.dim + col);
@@ -568,8 +613,6 @@ __global__ __launch_bounds__(NT) void attention_join_kernel(Args a, long rows, F
     x[4] = fmaf(w, hi.x, x[4]), x[5] = fmaf(w, hi.y, x[5]), x[6] = fmaf(w, hi.z, x[6]), x[7] = fmaf(w, hi.w, x[7]);
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const uint32_t bh = by_len.div(static_cast<uint32_t>(r)), i = static_cast<uint32_t>(r) - bh * by_len.d;
-  const uint32_t b = by_heads.div(bh), h = bh - b * by_heads.d;
   *reinterpret_cast<uint4*>(a.out + b * a.so.b + i * a.so.t + h * a.so.h + col) =
       make_uint4(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv),
                  pack_bf16x2(x[4] * inv, x[5] * inv), pack_bf16x2(x[6] * inv, x[7] * inv));
@@ -577,33 +620,41 @@ __global__ __launch_bounds__(NT) void attention_join_kernel(Args a, long rows, F
 }
 
 // Sums the pieces of a gradient [batch][token][head] in piece order: 16 lanes a
-// row, eight columns each; up to three gradients by blockIdx.y.
+// row, eight columns each; dQ (blockIdx.y 0), dK and dV.
 struct Sum {
   const float* part;
   bf16_t* out;
   AttentionArgs::Strides to;
-  long rows;            // batch * tokens * heads
+  long rows;            // batch * tokens * heads; 0: nothing in pieces
   FastDiv by_heads, by_tokens;
-  int pieces;
+  int pieces, quantum;
 };
 struct Sums {
   Sum sum[3];
-  int dim;
+  int keys;             // of a tile of the kernel for dK and dV
 };
-__global__ __launch_bounds__(NT) void attention_sum_kernel(Sums all) {
+__global__ __launch_bounds__(NT) void attention_sum_kernel(Args a, Sums all) {
   const Sum& j = all.sum[blockIdx.y];
   const long r = static_cast<long>(blockIdx.x) * (NT / 16) + threadIdx.x / 16;
   const int col = threadIdx.x % 16 * 8;
-  if (r >= j.rows || col >= all.dim) return;
+  if (r >= j.rows || col >= a.dim) return;
+  const uint32_t bt = j.by_heads.div(static_cast<uint32_t>(r)), h = static_cast<uint32_t>(r) - bt * j.by_heads.d;
+  const uint32_t b = j.by_tokens.div(bt), t = bt - b * j.by_tokens.d;
+  const Sequence seq(a, b);
+  const int packed = t * a.group + (h - a.by_group.div(h) * a.group);
+  const int2 walk = blockIdx.y == 0 ? key_walk<KT>(a, seq, packed / ROWS * ROWS, ROWS)
+                                    : row_walk<KT>(a, seq, static_cast<int>(t) / all.keys * all.keys, all.keys);
+  a.pieces = j.pieces;
+  a.quantum = j.quantum;
+  const int pieces = pieces_of<KT>(a, walk.x, walk.y);
+  if (pieces == 1) return;   // written already
   float x[8] = {};
-  for (int u = 0; u < j.pieces; ++u) {
-    const float4* y = reinterpret_cast<const float4*>(j.part + (u * j.rows + r) * all.dim + col);
+  for (int u = 0; u < pieces; ++u) {
+    const float4* y = reinterpret_cast<const float4*>(j.part + (u * j.rows + r) * a.dim + col);
     const float4 lo = y[0], hi = y[1];
     x[0] += lo.x, x[1] += lo.y, x[2] += lo.z, x[3] += lo.w;
     x[4] += hi.x, x[5] += hi.y, x[6] += hi.z, x[7] += hi.w;
   }
-  const uint32_t bt = j.by_heads.div(static_cast<uint32_t>(r)), h = static_cast<uint32_t>(r) - bt * j.by_heads.d;
-  const uint32_t b = j.by_tokens.div(bt), t = bt - b * j.by_tokens.d;
   *reinterpret_cast<uint4*>(j.out + b * j.to.b + t * j.to.t + h * j.to.h + col) =
       make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
@@ -630,9 +681,11 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   const int2 mine = seq.keys(a, p);
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
   const int2 wfirst = uniform(seq.keys(a, position(row0))), wlast = uniform(seq.keys(a, position(row0 + 31)));
-  int begin = uniform(seq.keys(a, position(at.tile * ROWS)).x / KT * KT);
-  int end = uniform(seq.keys(a, position(at.tile * ROWS + ROWS - 1)).y);
-  share<KT>(at.piece, a.pieces, begin, end);
+  const int2 walk = uniform(key_walk<KT>(a, seq, at.tile * ROWS, ROWS));
+  int begin = walk.x, end = walk.y;
+  const int pieces = pieces_of<KT>(a, begin, end);
+  if (at.piece >= pieces) return;
+  share<KT>(at.piece, pieces, begin, end);
   const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
   const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
   Loader<DH, KT, NT> kl, vl;
@@ -708,7 +761,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
     }
   }
   if (row0 + (lane & 31) >= a.rows) return;
-  if (a.pieces > 1) {
+  if (pieces > 1) {
     const long r = ((static_cast<long>(at.piece) * a.batch + at.b) * a.q_len + i) * a.heads + head;
     store_part<DH>(a.part + r * a.dim, a.dim, o, a.scale, lane);
     return;
@@ -716,41 +769,39 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   store_row<DH>(a.dq + at.b * a.sdq.b + i * a.sdq.t + head * a.sdq.h, a.dim, o, a.scale, lane);
 }
 
-// What dK and dV need of a staged row: log2 of its sum, delta, slope, position
-// and keys.
+// What dK and dV need of a staged row: minus log2 of its sum (PLAIN: over c1),
+// minus delta, slope, position and keys.
 struct RowInfo {
   float sum[KT], delta[KT], slope[KT];
   int position[KT], lo[KT], hi[KT];
 };
 
-// dK and dV of 128 keys: the wave's own 32 are keys, the walked columns rows.
-template <int DH, bool PLAIN>
-__global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
+// dK and dV of WAVES * 32 keys: the wave's own 32 are keys, the walked columns
+// rows. At 128 columns the two results and the fragments of K and V would fill
+// the registers of two waves a SIMD (35 spilled, 2460 us for 16384 causal tokens
+// of 16 heads); eight waves, which share a staged tile and leave LDS for it, keep
+// V there instead (XX us).
+template <int DH, bool PLAIN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Args a) {
   using T = Tile<DH>;
   __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, Q or dO
   __shared__ __attribute__((aligned(16))) RowInfo info[2];
+  constexpr bool V_IN_LDS = DH == 128 && WAVES == 8;
+  __shared__ __attribute__((aligned(16))) char own_v[V_IN_LDS ? WAVES : 1][V_IN_LDS ? T::BYTES / 2 : 16];
+  constexpr int THREADS = 64 * WAVES, KEYS = 32 * WAVES;
   const Block at(a, false);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const Lane<DH> frag(lane);
   const Sequence seq(a, at.b);
-  const int key0 = at.tile * ROWS, wkey0 = key0 + 32 * wave, key = wkey0 + (lane & 31);
-  const int valid = min(seq.limit, key0 + ROWS);
+  const int key0 = at.tile * KEYS, wkey0 = key0 + 32 * wave, key = wkey0 + (lane & 31);
+  const int valid = min(seq.limit, key0 + KEYS);
   const bf16_t* q = a.q + at.b * a.sq.b + at.kh * a.group * a.sq.h;
   const bf16_t* dout = a.dout + at.b * a.sdo.b + at.kh * a.group * a.sdo.h;
-  // rows that see one of the block's keys: positions [pa, pb)
-  int pa = -(1 << 30), pb = 0x7fffffff;
-  if (a.causal && key0 >= seq.prefix) pa = key0;
-  if (seq.doc && key0 < valid) {
-    pa = max(pa, seq.doc[key0].x);
-    pb = seq.doc[valid - 1].y;
-  }
-  const long first = max(0L, static_cast<long>(pa) - a.q_offset) * a.group;
-  int begin = uniform(static_cast<int>(min(first, static_cast<long>(a.rows))) / KT * KT);
-  int end = key0 < valid ? static_cast<int>(min(max(static_cast<long>(pb) - a.q_offset, 0L) * a.group,
-                                                static_cast<long>(a.rows)))
-                         : 0;
-  end = uniform(end);
-  share<KT>(at.piece, a.pieces, begin, end);
+  const int2 walk = uniform(row_walk<KT>(a, seq, key0, KEYS));
+  int begin = walk.x, end = walk.y;
+  const int pieces = pieces_of<KT>(a, begin, end);
+  if (at.piece >= pieces) return;
+  share<KT>(at.piece, pieces, begin, end);
   // Row r of the tile at r0 is query (r0 + r) / group of head (r0 + r) % group;
   // its offset from the tile's first query is the same for every tile where the
   // group divides the tile.
@@ -759,7 +810,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
     return (i - static_cast<int>(a.by_group.div(r0))) * st.t + (r0 + r - i * a.group) * st.h;
   };
   const bool regular = KT % a.group == 0;
-  Loader<DH, KT, NT> ql, dol;
+  Loader<DH, KT, THREADS> ql, dol;
   ql.init(tid, a.dim, [&](int r) { return offset(a.sq, 0, r); });
   dol.init(tid, a.dim, [&](int r) { return offset(a.sdo, 0, r); });
   const auto fetch = [&](int r0, int buf) {
@@ -770,71 +821,114 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
       dol.start(ob, lds_address(lds[buf][1]), r0, a.rows, tid);
       return;
     }
-    Loader<DH, KT, NT> l;
+    Loader<DH, KT, THREADS> l;
     l.init(tid, a.dim, [&](int r) { return offset(a.sq, r0, r); });
     l.start(qb, lds_address(lds[buf][0]), r0, a.rows, tid);
     l.init(tid, a.dim, [&](int r) { return offset(a.sdo, r0, r); });
     l.start(ob, lds_address(lds[buf][1]), r0, a.rows, tid);
   };
-  // rows past the last have an infinite sum: they weigh zero
-  float sm = INFINITY, sd = 0.0f, ss = 0.0f;
-  int2 sk = make_int2(0, 0);
-  int sp = 0;
+  // The staged rows' statistics: loaded as the tile is (nothing waits for them
+  // there), worked out and stored in LDS after the products of the tile before.
+  float rl = 0.0f, rd = 0.0f, rs = 0.0f;
+  int2 rdoc = make_int2(0, 0x7fffffff);
   const auto look = [&](int r0) {
-    sm = INFINITY, sd = 0.0f, ss = 0.0f, sk = make_int2(0, 0), sp = 0;
     if (tid < KT && r0 + tid < a.rows) {
       const int i = a.by_group.div(r0 + tid), head = at.kh * a.group + r0 + tid - i * a.group;
       const long at_row = row_index(a, at.b, head, i);
-      sm = log2_sum(a, at_row), sd = a.delta[at_row], sp = a.q_offset + i;
-      sk = seq.keys(a, sp);
-      if (a.slopes) ss = a.slopes[head] * LOG2E;
+      rl = a.lse[at_row];
+      rd = a.delta[at_row];
+      if (seq.doc) rdoc = seq.doc[a.q_offset + i];
+      if (a.slopes) rs = a.slopes[head];
     }
   };
-  const auto note = [&](int buf) {
+  const auto note = [&](int r0, int buf) {
     if (tid < KT) {
       RowInfo& w = info[buf];
-      w.sum[tid] = sm, w.delta[tid] = sd, w.slope[tid] = ss;
-      w.position[tid] = sp, w.lo[tid] = sk.x, w.hi[tid] = sk.y;
+      const bool row = r0 + tid < a.rows;   // past the last: it weighs zero
+      const int p = a.q_offset + static_cast<int>(a.by_group.div(r0 + tid));
+      const int2 keys = seq.clip(a, p, rdoc);
+      // also where the row has no weight
+      w.sum[tid] = row && rl != -INFINITY ? -rl * (PLAIN ? LOG2E / a.c1 : LOG2E) : -INFINITY;
+      w.delta[tid] = row ? -rd : 0.0f;
+      w.slope[tid] = rs * LOG2E;
+      w.position[tid] = p;
+      w.lo[tid] = row ? keys.x : 0;
+      w.hi[tid] = row ? keys.y : 0;
     }
   };
+  // from the end: under a causal mask that is where the walks of a head's blocks
+  // meet (from their starts they read rows apart, and past the L2: 1046 us in
+  // place of XX)
+  const int top = begin + max(0, end - begin - 1) / KT * KT;
   if (begin < end) {
-    fetch(begin, 0);
-    look(begin);
-    note(0);
+    fetch(top, 0);
+    look(top);
+    note(top, 0);
   }
-  bf16x8_t fk[DH / 16], fv[DH / 16];
+  bf16x8_t fk[DH / 16], fv[V_IN_LDS ? 1 : DH / 16];
   f32x16_t dk[DH / 32], dv[DH / 32];
   const int kc = min(key, a.kv_len - 1), dim = kc < seq.limit ? a.dim : 0;
   load_row<DH>(a.k + at.b * a.sk.b + kc * a.sk.t + at.kh * a.sk.h, dim, lane, fk, a.flip);
-  load_row<DH>(a.v + at.b * a.sv.b + kc * a.sv.t + at.kh * a.sv.h, dim, lane, fv);
+  const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
+  const char* my_v = own_v[V_IN_LDS ? uniform(wave) : 0];
+  if constexpr (V_IN_LDS) {
+    Loader<DH, 32, 64> l;
+    l.init(lane, a.dim, [&](int r) { return r * a.sv.t; });
+    const int first_key = uniform(wkey0);
+    l.start(v + first_key * a.sv.t, lds_address(my_v), first_key, seq.limit, lane);
+  } else {
+    load_row<DH>(v + kc * a.sv.t, dim, lane, fv);
+  }
   zero(dk);
   zero(dv);
   int buf = 0;
-  for (int r0 = begin; r0 < end; r0 += KT, buf ^= 1) {
+  for (int r0 = begin < end ? top : begin - 1; r0 >= begin; r0 -= KT, buf ^= 1) {
     landed();
     __syncthreads();
-    const bool more = r0 + KT < end;
+    const bool more = r0 > begin;
     if (more) {
-      fetch(r0 + KT, buf ^ 1);
-      look(r0 + KT);
+      fetch(r0 - KT, buf ^ 1);
+      look(r0 - KT);
     }
     const RowInfo& w = info[buf];
     const int tail = min(KT, a.rows - r0) - 1;
     if (wkey0 < valid && wkey0 < w.hi[tail] && wkey0 + 32 > w.lo[0]) {
       const char *Qs = lds[buf][0], *Os = lds[buf][1];
       const bool cut = wkey0 < w.lo[tail] || wkey0 + 32 > w.hi[0];
-#pragma unroll 1
+#pragma unroll(DH <= 64 ? 2 : 1)
       for (int n = 0; n < KT / 32; ++n) {
         const Lane<DH> lf = frag.here();
-        f32x16_t s = product<DH>(fk, Qs, 32 * n, lf);
-        f32x16_t dp = product<DH>(fv, Os, 32 * n, lf);
-        f32x16_t t;
-        if (!PLAIN) {
+        // PLAIN: the rows' statistics are what the products start from, so that
+        // they cost no registers of their own and nothing waits for them
+        f32x16_t s, dp;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          const int c = 32 * n + col_of(4 * g, lane);
+          const float4 su = PLAIN ? *reinterpret_cast<const float4*>(w.sum + c) : z;
+          const float4 de = *reinterpret_cast<const float4*>(w.delta + c);
+          s[4 * g] = su.x, s[4 * g + 1] = su.y, s[4 * g + 2] = su.z, s[4 * g + 3] = su.w;
+          dp[4 * g] = de.x, dp[4 * g + 1] = de.y, dp[4 * g + 2] = de.z, dp[4 * g + 3] = de.w;
+        }
+#pragma unroll
+        for (int q = 0; q < DH / 16; ++q) s = mfma(lf.row_frag(Qs, 32 * n, q), fk[q], s);
+#pragma unroll
+        for (int q = 0; q < DH / 16; ++q) {
+          if constexpr (V_IN_LDS) dp = mfma(lf.row_frag(Os, 32 * n, q), lf.row_frag(my_v, 0, q), dp);
+          else dp = mfma(lf.row_frag(Os, 32 * n, q), fv[q], dp);
+        }
+        if (PLAIN) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            float tr = 0.0f;
-            s[r] = score(a, s[r], tr);
-            t[r] = 1.0f - tr * tr;
+            s[r] = __builtin_amdgcn_exp2f(s[r] * a.c1);
+            dp[r] *= s[r];
+          }
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            float t = 0.0f;
+            s[r] = score(a, s[r], t);
+            dp[r] *= 1.0f - t * t;
           }
           if (a.slopes) {
 #pragma unroll
@@ -843,21 +937,17 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
               s[r] -= w.slope[c] * fabsf(static_cast<float>(w.position[c] - key));
             }
           }
-        }
-        const float c1 = PLAIN ? a.c1 : 1.0f;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          __builtin_amdgcn_sched_barrier(0);   // one group's statistics at a time: registers
-          const int c = 32 * n + col_of(4 * g, lane);
-          const float4 su = *reinterpret_cast<const float4*>(w.sum + c);
-          const float4 de = *reinterpret_cast<const float4*>(w.delta + c);
-          const float sus[4] = {su.x, su.y, su.z, su.w}, des[4] = {de.x, de.y, de.z, de.w};
+          for (int g = 0; g < 4; ++g) {
+            __builtin_amdgcn_sched_barrier(0);   // one group's statistics at a time: registers
+            const float4 u = *reinterpret_cast<const float4*>(w.sum + 32 * n + col_of(4 * g, lane));
+            const float su[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 4 * g + e;
-            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c1, -sus[e]));
-            dp[r] = s[r] * (dp[r] - des[e]);
-            if (!PLAIN) dp[r] *= t[r];
+            for (int e = 0; e < 4; ++e) {
+              const int r = 4 * g + e;
+              s[r] = __builtin_amdgcn_exp2f(s[r] + su[e]);
+              dp[r] *= s[r];
+            }
           }
         }
         if (cut) {   // both, also where dP is not finite
@@ -877,10 +967,10 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dkv_kernel(Args a) {
         }
       }
     }
-    if (more) note(buf ^ 1);
+    if (more) note(r0 - KT, buf ^ 1);
   }
   if (key >= a.kv_len) return;
-  if (a.pieces > 1) {
+  if (pieces > 1) {
     const long r = ((static_cast<long>(at.piece) * a.batch + at.b) * a.kv_len + key) * a.kv_heads + at.kh;
     store_part<DH>(a.part + r * a.dim, a.dim, dk, a.scale, lane);
     store_part<DH>(a.part2 + r * a.dim, a.dim, dv, 1.0f, lane);
@@ -895,32 +985,49 @@ size_t doc_bytes(const AttentionArgs& a) { return round256(static_cast<size_t>(a
 size_t q_rows(const AttentionArgs& a) { return static_cast<size_t>(a.batch) * a.heads * a.q_len; }
 size_t k_rows(const AttentionArgs& a) { return static_cast<size_t>(a.batch) * a.kv_heads * a.kv_len; }
 
-// Into how many pieces the walk of each of `blocks` tiles is cut: few blocks of
-// a long walk leave CUs idle, and a causal walk ends in its longest block. At
-// least `least` steps stay in a piece, so that a partial result's write and
-// read stay small beside its products.
-int pieces_for(long blocks, long steps, long want, long least) {
-  if (blocks <= 0 || steps <= 0) return 1;
-  return static_cast<int>(std::max(1L, std::min({(want + blocks - 1) / blocks, steps / least, 128L})));
+// How the walks of a kernel's blocks are cut. Few blocks of a long walk leave
+// CUs idle; and documents make walks unlike, where the longest is waited for
+// unless it is shared (a causal walk alone is even enough: its longest blocks
+// start first).
+struct Cut {
+  int planes = 1;                // partial results there is room for, whatever the masks
+  int pieces = 1, quantum = 1;   // as in Args
+};
+// blocks of at most `steps` steps; about `want` blocks fill the chip; a piece has
+// at least `least` steps, so that a partial result's write and read stay small
+// beside its products.
+Cut cut(long blocks, long steps, long want, long least, bool documents) {
+  Cut c;
+  if (blocks <= 0 || steps <= 0) return c;
+  const long fill = std::max(1L, std::min({(want + blocks - 1) / blocks, steps / least, 128L}));
+  const bool even = fill == 1 && blocks < 4 * want && steps >= 64;   // two pieces for the longest documents
+  c.planes = static_cast<int>(even ? 2 : fill);
+  c.pieces = even && !documents ? 1 : c.planes;
+  c.quantum = static_cast<int>(even ? steps / 4 : least);
+  return c;
 }
 
 struct Plan {
   bool few;                      // forward by the kernel for few rows
-  int fwd, dq, dkv;              // pieces
+  bool wide;                     // dK and dV by blocks of 256 keys, else of 128
+  Cut fwd, dq, dkv;
 };
 Plan plan(const AttentionArgs& a) {
   Plan p;
   const long bh = static_cast<long>(a.batch) * a.kv_heads;
-  const long row_tiles = (a.rows + ROWS - 1L) / ROWS, key_tiles = (a.kv_len + ROWS - 1L) / ROWS;
+  const long row_tiles = (a.rows + ROWS - 1L) / ROWS;
+  const bool doc = a.documents != nullptr;
   p.few = a.rows <= 64;
-  p.fwd = p.few ? pieces_for(bh * ((a.rows + 31) / 32), (a.kv_len + 127L) / 128, 1024, 2)
-                : pieces_for(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8);
-  p.dq = pieces_for(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8);
-  p.dkv = pieces_for(bh * key_tiles, (a.rows + KT - 1L) / KT, 1024, 8);
+  p.fwd = p.few ? cut(bh * ((a.rows + 31) / 32), (a.kv_len + 31L) / 32, 1024, 8, doc)
+                : cut(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8, doc);
+  p.dq = cut(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8, doc);
+  p.wide = a.dim > 96 && a.kv_len > 128;
+  p.dkv = cut(bh * (p.wide ? (a.kv_len + 255L) / 256 : (a.kv_len + 127L) / 128), (a.rows + KT - 1L) / KT,
+              p.wide ? 512 : 1024, 8, doc);
   return p;
 }
-size_t part_bytes(int pieces, size_t rows, int dim) {
-  return pieces > 1 ? round256(static_cast<size_t>(pieces) * rows * dim * sizeof(float)) : 0;
+size_t part_bytes(const Cut& c, size_t rows, int dim) {
+  return c.planes > 1 ? round256(static_cast<size_t>(c.planes) * rows * dim * sizeof(float)) : 0;
 }
 
 // Launch-independent values, and the document runs if there are documents.
@@ -960,11 +1067,14 @@ void with_width(const Args& a, F&& f) {
 }
 
 template <typename K>
-hipError_t launch(K* kernel, Args& a, long length, int tile, int pieces, hipStream_t s) {
+hipError_t launch(K* kernel, int threads, Args& a, long length, int tile, const Cut& c, hipStream_t s) {
   a.tiles = static_cast<int>((length + tile - 1) / tile);
-  a.pieces = pieces;
-  a.by_pieces = FastDiv(pieces);
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(a.tiles) * pieces * a.batch * a.kv_heads), dim3(NT), 0, s, a);
+  a.pieces = c.pieces;
+  a.quantum = c.quantum;
+  a.by_tiles = FastDiv(a.tiles);
+
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(a.tiles) * a.pieces * a.batch * a.kv_heads), dim3(threads), 0, s,
+                     a);
   return hipGetLastError();
 }
 
@@ -973,7 +1083,7 @@ hipError_t launch(K* kernel, Args& a, long length, int tile, int pieces, hipStre
 size_t attention_ws_bytes(const AttentionArgs& a, bool backward) {
   const Plan p = plan(a);
   const size_t forward = doc_bytes(a) + part_bytes(p.fwd, q_rows(a), a.dim) +
-                         (p.fwd > 1 ? round256(p.fwd * q_rows(a) * sizeof(float2)) : 0);
+                         (p.fwd.planes > 1 ? round256(p.fwd.planes * q_rows(a) * sizeof(float2)) : 0);
   if (!backward) return forward;
   return std::max(forward, doc_bytes(a) + round256(q_rows(a) * sizeof(float)) + part_bytes(p.dq, q_rows(a), a.dim) +
                                2 * part_bytes(p.dkv, k_rows(a), a.dim));
@@ -988,13 +1098,13 @@ hipError_t attention_masked_fwd(const AttentionArgs& in, hipStream_t s) {
   a.part = reinterpret_cast<float*>(in.ws + doc_bytes(in));
   a.part_ml = reinterpret_cast<float2*>(in.ws + doc_bytes(in) + part_bytes(p.fwd, q_rows(in), in.dim));
   with_width(a, [&](auto width, auto plain) {
-    e = p.few ? launch(attention_masked_few_kernel<width(), plain()>, a, a.rows, 32, p.fwd, s)
-              : launch(attention_masked_fwd_kernel<width(), plain()>, a, a.rows, ROWS, p.fwd, s);
+    e = p.few ? launch(attention_masked_few_kernel<width(), plain()>, NT, a, a.rows, 32, p.fwd, s)
+              : launch(attention_masked_fwd_kernel<width(), plain()>, NT, a, a.rows, ROWS, p.fwd, s);
   });
-  if (e != hipSuccess || p.fwd == 1) return e;
+  if (e != hipSuccess || p.fwd.pieces == 1) return e;
   const long rows = static_cast<long>(q_rows(in));
   hipLaunchKernelGGL(attention_join_kernel, dim3(static_cast<unsigned>((rows + NT / 16 - 1) / (NT / 16))), dim3(NT), 0,
-                     s, a, rows, FastDiv(a.q_len), FastDiv(a.heads));
+                     s, a, rows, FastDiv(a.q_len), FastDiv(a.heads), p.few ? 1 : 0);
   return hipGetLastError();
 }
 
@@ -1011,35 +1121,38 @@ hipError_t attention_masked_bwd(const AttentionArgs& in, hipStream_t s) {
   ws += part_bytes(p.dq, q_rows(in), in.dim);
   float* part_k = reinterpret_cast<float*>(ws);
   float* part_v = reinterpret_cast<float*>(ws + part_bytes(p.dkv, k_rows(in), in.dim));
-  Sums sums;
-  sums.dim = a.dim;
-  int nsums = 0;
+  Sums sums{};
+  sums.keys = p.wide ? 256 : 128;
   long most = 0;
-  const auto sum = [&](const float* part, bf16_t* out, const AttentionArgs::Strides& to, size_t rows, int heads,
-                       int tokens, int pieces) {
-    sums.sum[nsums++] = {part, out, to, static_cast<long>(rows), FastDiv(heads), FastDiv(tokens), pieces};
+  const auto sum = [&](int at, const float* part, bf16_t* out, const AttentionArgs::Strides& to, size_t rows, int heads,
+                       int tokens, const Cut& c) {
+    if (c.pieces == 1) return;
+    sums.sum[at] = {part, out, to, static_cast<long>(rows), FastDiv(heads), FastDiv(tokens), c.pieces, c.quantum};
     most = std::max(most, static_cast<long>(rows));
   };
   with_width(a, [&](auto width, auto plain) {
     if (a.q_len > 0) {
       a.part = part_q;
-      e = launch(attention_masked_dq_kernel<width(), plain()>, a, a.rows, ROWS, p.dq, s);
+      e = launch(attention_masked_dq_kernel<width(), plain()>, NT, a, a.rows, ROWS, p.dq, s);
       if (e != hipSuccess) return;
-      if (p.dq > 1) sum(part_q, a.dq, a.sdq, q_rows(in), a.heads, a.q_len, p.dq);
+      sum(0, part_q, a.dq, a.sdq, q_rows(in), a.heads, a.q_len, p.dq);
     }
     if (a.kv_len == 0) return;
     a.part = part_k;
     a.part2 = part_v;
-    e = launch(attention_masked_dkv_kernel<width(), plain()>, a, a.kv_len, ROWS, p.dkv, s);
-    if (e != hipSuccess) return;
-    if (p.dkv > 1) {
-      sum(part_k, a.dk, a.sdk, k_rows(in), a.kv_heads, a.kv_len, p.dkv);
-      sum(part_v, a.dv, a.sdv, k_rows(in), a.kv_heads, a.kv_len, p.dkv);
+    constexpr bool kWide = width() == 128;
+    if constexpr (kWide) {
+      if (p.wide) e = launch(attention_masked_dkv_kernel<width(), plain(), 8>, 512, a, a.kv_len, 256, p.dkv, s);
     }
+    if (!kWide || !p.wide)
+      e = launch(attention_masked_dkv_kernel<width(), plain(), 4>, 256, a, a.kv_len, 128, p.dkv, s);
+    if (e != hipSuccess) return;
+    sum(1, part_k, a.dk, a.sdk, k_rows(in), a.kv_heads, a.kv_len, p.dkv);
+    sum(2, part_v, a.dv, a.sdv, k_rows(in), a.kv_heads, a.kv_len, p.dkv);
   });
-  if (e != hipSuccess || nsums == 0) return e;
-  hipLaunchKernelGGL(attention_sum_kernel, dim3(static_cast<unsigned>((most + NT / 16 - 1) / (NT / 16)), nsums),
-                     dim3(NT), 0, s, sums);
+  if (e != hipSuccess || most == 0) return e;
+  hipLaunchKernelGGL(attention_sum_kernel, dim3(static_cast<unsigned>((most + NT / 16 - 1) / (NT / 16)), 3), dim3(NT), 0,
+                     s, a, sums);
   return hipGetLastError();
 }
 
