@@ -26,7 +26,8 @@ struct Args : AttentionArgs {
   float c1 = 0.0f;                // uncapped: |scale| log2(e); capped: 2 |scale| / cap log2(e)
   float c2 = 0.0f;                // capped: cap log2(e)
   int flip = 0;                   // scale < 0: one operand of the scores changes sign instead
-  FastDiv by_group, by_bh, by_kv, by_tiles;
+  FastDiv by_group, by_bh, by_kv, by_tiles, by_step;
+  int step = KT;                  // rows of a step of the walk over rows: whole queries, where a group fits a tile
   int tiles = 0;
   int pieces = 1;                 // most pieces that a tile's walk is cut into, a block each
   int quantum = 1;                // fewest steps of a piece
@@ -35,19 +36,22 @@ struct Args : AttentionArgs {
   float* part2 = nullptr;         // dV's (part is dK's)
 };
 
+// Values that are the same in every lane, for scalar registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int2 uniform(int2 v) { return make_int2(uniform(v.x), uniform(v.y)); }
+
 // A walk over [begin, end) in steps of W is cut into at most a.pieces equal
 // pieces, none shorter than about a.quantum steps: long walks are shared out,
 // short ones stay whole and write their results at once.
-template <int W>
-__device__ __forceinline__ int pieces_of(const Args& a, int begin, int end) {
+__device__ __forceinline__ int pieces_of(const Args& a, int W, int begin, int end) {
   if (a.pieces == 1) return 1;
   const int steps = max(0, end - begin + W - 1) / W;
   return max(1, min(a.pieces, (steps + a.quantum - 1) / a.quantum));
 }
-// The n'th of `of` equal shares.
-template <int W>
-__device__ __forceinline__ void share(int n, int of, int& begin, int& end) {
-  const int steps = max(0, end - begin + W - 1) / W, b = begin, part = steps / of, rest = steps - part * of;
+// The n'th of `of` equal shares (all of it the same in every lane).
+__device__ __forceinline__ void share(int W, int n, int of, int& begin, int& end) {
+  const int steps = uniform(max(0, end - begin + W - 1) / W), b = begin;
+  const int part = uniform(steps / of), rest = steps - part * of;
   begin = b + (n * part + min(n, rest)) * W;
   end = min(end, b + ((n + 1) * part + min(n + 1, rest)) * W);
 }
@@ -78,8 +82,7 @@ __device__ __forceinline__ int2 key_walk(const Args& a, const Sequence& seq, int
   return make_int2(seq.keys(a, position(row0)).x / W * W, seq.keys(a, position(row0 + n - 1)).y);
 }
 
-// Rows that see one of the keys [key0, key0 + n), from a multiple of W on.
-template <int W>
+// Rows that see one of the keys [key0, key0 + n), from a multiple of a.step on.
 __device__ __forceinline__ int2 row_walk(const Args& a, const Sequence& seq, int key0, int n) {
   const int valid = min(seq.limit, key0 + n);
   if (key0 >= valid) return make_int2(0, 0);
@@ -92,7 +95,7 @@ __device__ __forceinline__ int2 row_walk(const Args& a, const Sequence& seq, int
   const auto row = [&](int p) {
     return static_cast<int>(min(max(static_cast<long>(p) - a.q_offset, 0L) * a.group, static_cast<long>(a.rows)));
   };
-  return make_int2(row(pa) / W * W, row(pb));
+  return make_int2(a.by_step.div(row(pa)) * a.step, row(pb));
 }
 
 // Score of one product in units of log2: s log2(e), and tanh(z / cap) where
@@ -129,7 +132,10 @@ __device__ __forceinline__ void direct16(__amdgpu_buffer_rsrc_t r, uint32_t lds,
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
                : "memory", "m0");
 }
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const bf16_t* p) {
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const bf16_t* p) {   // p: the same in every lane
+  const uint64_t u = reinterpret_cast<uintptr_t>(p);
+  p = reinterpret_cast<const bf16_t*>(static_cast<uint64_t>(static_cast<uint32_t>(uniform(static_cast<int>(u >> 32)))) << 32 |
+                                      static_cast<uint32_t>(uniform(static_cast<int>(u))));
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(p), static_cast<short>(0), 0x7fffffe0, 0x00020000);
 }
 constexpr int OUTSIDE = 0x7ffffff0;   // past every resource
@@ -153,14 +159,16 @@ struct Loader {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const int e = t + THREADS * i, r = e / T::C, col = ((e % T::C) ^ T::swizzle(r)) * 8;
-      off[i] = col < dim ? static_cast<int>(2 * (row(r) + col)) : OUTSIDE;
+      off[i] = col < dim ? static_cast<int>(min(2 * (row(r) + col), static_cast<long>(OUTSIDE))) : OUTSIDE;
     }
   }
-  // Starts the copy of rows first .. (zero from `limit` on) into LDS.
-  __device__ __forceinline__ void start(const bf16_t* base, uint32_t lds, int first, int limit, int t) const {
+  // Starts the copy of rows first .. (zero from `limit` on) into LDS; of a tile
+  // with fewer rows the others are OUTSIDE as they are.
+  __device__ __forceinline__ void start(const bf16_t* base, uint32_t lds, int first, int limit, int t,
+                                        int rows = N) const {
     const __amdgpu_buffer_rsrc_t r = resource(base);
-    const uint32_t to = lds + (THREADS > 64 ? 1024 * __builtin_amdgcn_readfirstlane(t >> 6) : 0);
-    if (first + N <= limit) {
+    const uint32_t to = uniform(static_cast<int>(lds)) + (THREADS > 64 ? 1024 * __builtin_amdgcn_readfirstlane(t >> 6) : 0);
+    if (first + rows <= limit) {
 #pragma unroll
       for (int i = 0; i < V; ++i) direct16(r, to + 16 * THREADS * i, off[i]);
     } else {
@@ -170,9 +178,6 @@ struct Loader {
     }
   }
 };
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int2 uniform(int2 v) { return make_int2(uniform(v.x), uniform(v.y)); }
 
 // Byte offsets of a lane's fragments in a tile: rows c0 + lane % 32, columns
 // 16 q + 8 (lane / 32) .. at rows ^ (q << 5) + c0 * pitch; and, transposed (see
@@ -391,11 +396,11 @@ struct Running {
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[n][r] = score(a, s[n][r], t);
       if (a.slopes) {
+        const float far = static_cast<float>(p - k0 - col_of(0, lane));
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            s[n][r] -= slope * fabsf(static_cast<float>(p - (k0 + 32 * n + col_of(r, lane))));
+          for (int r = 0; r < 16; ++r) s[n][r] -= slope * fabsf(far - static_cast<float>(32 * n + col_of(r, 0)));
       }
     }
     const float c1 = PLAIN ? a.c1 : 1.0f;   // s c1: the scores
@@ -459,9 +464,9 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   const int2 wfirst = uniform(seq.keys(a, position(row0))), wlast = uniform(seq.keys(a, position(row0 + 31)));
   const int2 walk = uniform(key_walk<KT>(a, seq, at.tile * ROWS, ROWS));
   int begin = walk.x, end = walk.y;
-  const int pieces = pieces_of<KT>(a, begin, end);
+  const int pieces = uniform(pieces_of(a, KT, begin, end));
   if (at.piece >= pieces) return;
-  share<KT>(at.piece, pieces, begin, end);
+  share(KT, at.piece, pieces, begin, end);
   const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
   const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
   Loader<DH, KT, NT> kl, vl;
@@ -521,9 +526,9 @@ __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
   const int2 first = uniform(seq.keys(a, position(row0))), last = uniform(seq.keys(a, position(row0 + 31)));
   int begin = first.x / FT * FT, end = last.y;
-  const int pieces = pieces_of<FT>(a, begin, end);
+  const int pieces = uniform(pieces_of(a, FT, begin, end));
   if (at.piece >= pieces) return;
-  share<FT>(at.piece * (NT / 64) + wave, pieces * (NT / 64), begin, end);
+  share(FT, at.piece * (NT / 64) + wave, pieces * (NT / 64), begin, end);
   const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
   const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
   Loader<DH, FT, 64> kl, vl;
@@ -597,7 +602,7 @@ __global__ __launch_bounds__(NT) void attention_join_kernel(Args a, long rows, F
   const int packed = i * a.group + (h - a.by_group.div(h) * a.group), tile = few ? 32 : ROWS;
   const int2 walk = few ? key_walk<32>(a, seq, packed / tile * tile, tile)
                         : key_walk<KT>(a, seq, packed / tile * tile, tile);
-  const int pieces = few ? pieces_of<32>(a, walk.x, walk.y) : pieces_of<KT>(a, walk.x, walk.y);
+  const int pieces = few ? pieces_of(a, 32, walk.x, walk.y) : pieces_of(a, KT, walk.x, walk.y);
   if (pieces == 1) return;   // written already
   float m = -INFINITY;
   for (int u = 0; u < pieces; ++u) m = fmaxf(m, a.part_ml[u * rows + r].x);
@@ -643,10 +648,10 @@ __global__ __launch_bounds__(NT) void attention_sum_kernel(Args a, Sums all) {
   const Sequence seq(a, b);
   const int packed = t * a.group + (h - a.by_group.div(h) * a.group);
   const int2 walk = blockIdx.y == 0 ? key_walk<KT>(a, seq, packed / ROWS * ROWS, ROWS)
-                                    : row_walk<KT>(a, seq, static_cast<int>(t) / all.keys * all.keys, all.keys);
+                                    : row_walk(a, seq, static_cast<int>(t) / all.keys * all.keys, all.keys);
   a.pieces = j.pieces;
   a.quantum = j.quantum;
-  const int pieces = pieces_of<KT>(a, walk.x, walk.y);
+  const int pieces = pieces_of(a, blockIdx.y == 0 ? KT : a.step, walk.x, walk.y);
   if (pieces == 1) return;   // written already
   float x[8] = {};
   for (int u = 0; u < pieces; ++u) {
@@ -683,9 +688,9 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   const int2 wfirst = uniform(seq.keys(a, position(row0))), wlast = uniform(seq.keys(a, position(row0 + 31)));
   const int2 walk = uniform(key_walk<KT>(a, seq, at.tile * ROWS, ROWS));
   int begin = walk.x, end = walk.y;
-  const int pieces = pieces_of<KT>(a, begin, end);
+  const int pieces = uniform(pieces_of(a, KT, begin, end));
   if (at.piece >= pieces) return;
-  share<KT>(at.piece, pieces, begin, end);
+  share(KT, at.piece, pieces, begin, end);
   const bf16_t* k = a.k + at.b * a.sk.b + at.kh * a.sk.h;
   const bf16_t* v = a.v + at.b * a.sv.b + at.kh * a.sv.h;
   Loader<DH, KT, NT> kl, vl;
@@ -716,6 +721,10 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
     if (at.piece == 0 && lane < 32 && row0 + lane < a.rows) a.delta[at_row] = delta;
   }
 
+  // One key in sight: its probability is 1 whatever the score (dP and delta
+  // would differ by their rounding). Such a row's tile is always cut.
+  const bool alone = mine.y - mine.x <= 1;
+
   f32x16_t o[DH / 32];
   zero(o);
   int buf = 0;
@@ -742,9 +751,9 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
           t[r] = tr;
         }
         if (a.slopes) {
+          const float far = static_cast<float>(p - k0 - 32 * n - col_of(0, lane));
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            s[r] -= slope * fabsf(static_cast<float>(p - (k0 + 32 * n + col_of(r, lane))));
+          for (int r = 0; r < 16; ++r) s[r] -= slope * fabsf(far - static_cast<float>(col_of(r, 0)));
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r)   // t is 0 where there is no cap
@@ -754,7 +763,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int j = k0 + 32 * n + col_of(r, lane);
-          if (j < mine.x || j >= mine.y) s[r] = 0.0f;
+          if (j < mine.x || j >= mine.y || alone) s[r] = 0.0f;
         }
       }
       accumulate<DH>(s, Ks, 32 * n, frag, o);
@@ -797,19 +806,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
   const int valid = min(seq.limit, key0 + KEYS);
   const bf16_t* q = a.q + at.b * a.sq.b + at.kh * a.group * a.sq.h;
   const bf16_t* dout = a.dout + at.b * a.sdo.b + at.kh * a.group * a.sdo.h;
-  const int2 walk = uniform(row_walk<KT>(a, seq, key0, KEYS));
+  const int2 walk = uniform(row_walk(a, seq, key0, KEYS));
   int begin = walk.x, end = walk.y;
-  const int pieces = pieces_of<KT>(a, begin, end);
+  const int pieces = uniform(pieces_of(a, a.step, begin, end));
   if (at.piece >= pieces) return;
-  share<KT>(at.piece, pieces, begin, end);
-  // Row r of the tile at r0 is query (r0 + r) / group of head (r0 + r) % group;
-  // its offset from the tile's first query is the same for every tile where the
-  // group divides the tile.
+  share(a.step, at.piece, pieces, begin, end);
+  // Row r of the tile at r0 is query (r0 + r) / group of head (r0 + r) % group. A
+  // step is a whole number of queries, so a row's offset from the tile's first
+  // query is the same for every tile; with a group past a tile it is worked out
+  // for each.
   const auto offset = [&](const AttentionArgs::Strides& st, int r0, int r) {
     const int i = a.by_group.div(r0 + r);
-    return (i - static_cast<int>(a.by_group.div(r0))) * st.t + (r0 + r - i * a.group) * st.h;
+    return r < a.step ? (i - static_cast<int>(a.by_group.div(r0))) * st.t + (r0 + r - i * a.group) * st.h
+                      : static_cast<long>(OUTSIDE / 2);
   };
-  const bool regular = KT % a.group == 0;
+  const bool regular = a.group <= KT;
   Loader<DH, KT, THREADS> ql, dol;
   ql.init(tid, a.dim, [&](int r) { return offset(a.sq, 0, r); });
   dol.init(tid, a.dim, [&](int r) { return offset(a.sdo, 0, r); });
@@ -817,8 +828,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
     const int i0 = a.by_group.div(r0);
     const bf16_t *qb = q + i0 * a.sq.t, *ob = dout + i0 * a.sdo.t;
     if (regular) {
-      ql.start(qb, lds_address(lds[buf][0]), r0, a.rows, tid);
-      dol.start(ob, lds_address(lds[buf][1]), r0, a.rows, tid);
+      ql.start(qb, lds_address(lds[buf][0]), r0, a.rows, tid, a.step);
+      dol.start(ob, lds_address(lds[buf][1]), r0, a.rows, tid, a.step);
       return;
     }
     Loader<DH, KT, THREADS> l;
@@ -832,7 +843,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
   float rl = 0.0f, rd = 0.0f, rs = 0.0f;
   int2 rdoc = make_int2(0, 0x7fffffff);
   const auto look = [&](int r0) {
-    if (tid < KT && r0 + tid < a.rows) {
+    if (tid < a.step && r0 + tid < a.rows) {
       const int i = a.by_group.div(r0 + tid), head = at.kh * a.group + r0 + tid - i * a.group;
       const long at_row = row_index(a, at.b, head, i);
       rl = a.lse[at_row];
@@ -844,7 +855,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
   const auto note = [&](int r0, int buf) {
     if (tid < KT) {
       RowInfo& w = info[buf];
-      const bool row = r0 + tid < a.rows;   // past the last: it weighs zero
+      const bool row = tid < a.step && r0 + tid < a.rows;   // else it weighs zero
       const int p = a.q_offset + static_cast<int>(a.by_group.div(r0 + tid));
       const int2 keys = seq.clip(a, p, rdoc);
       // also where the row has no weight
@@ -859,7 +870,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
   // from the end: under a causal mask that is where the walks of a head's blocks
   // meet (from their starts they read rows apart, and past the L2: 1046 us in
   // place of XX)
-  const int top = begin + max(0, end - begin - 1) / KT * KT;
+  const int top = uniform(begin + static_cast<int>(a.by_step.div(max(0, end - begin - 1))) * a.step);
   if (begin < end) {
     fetch(top, 0);
     look(top);
@@ -882,16 +893,16 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
   zero(dk);
   zero(dv);
   int buf = 0;
-  for (int r0 = begin < end ? top : begin - 1; r0 >= begin; r0 -= KT, buf ^= 1) {
+  for (int r0 = begin < end ? top : begin - 1; r0 >= begin; r0 -= a.step, buf ^= 1) {
     landed();
     __syncthreads();
     const bool more = r0 > begin;
     if (more) {
-      fetch(r0 - KT, buf ^ 1);
-      look(r0 - KT);
+      fetch(r0 - a.step, buf ^ 1);
+      look(r0 - a.step);
     }
     const RowInfo& w = info[buf];
-    const int tail = min(KT, a.rows - r0) - 1;
+    const int tail = min(a.step, a.rows - r0) - 1;
     if (wkey0 < valid && wkey0 < w.hi[tail] && wkey0 + 32 > w.lo[0]) {
       const char *Qs = lds[buf][0], *Os = lds[buf][1];
       const bool cut = wkey0 < w.lo[tail] || wkey0 + 32 > w.hi[0];
@@ -954,7 +965,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int c = 32 * n + col_of(r, lane);
-            if (key < w.lo[c] || key >= w.hi[c]) s[r] = dp[r] = 0.0f;
+            const int lo = w.lo[c], hi = w.hi[c];
+            if (key < lo || key >= hi) s[r] = dp[r] = 0.0f;
+            if (hi - lo <= 1) dp[r] = 0.0f;   // one key in sight: no gradient, as for dQ
           }
         }
 #pragma unroll
@@ -967,7 +980,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
         }
       }
     }
-    if (more) note(r0 - KT, buf ^ 1);
+    if (more) note(r0 - a.step, buf ^ 1);
   }
   if (key >= a.kv_len) return;
   if (pieces > 1) {
@@ -993,13 +1006,13 @@ struct Cut {
   int planes = 1;                // partial results there is room for, whatever the masks
   int pieces = 1, quantum = 1;   // as in Args
 };
-// blocks of at most `steps` steps; about `want` blocks fill the chip; a piece has
+// blocks of at most `steps` steps; up to `want` blocks fill the chip; a piece has
 // at least `least` steps, so that a partial result's write and read stay small
 // beside its products.
 Cut cut(long blocks, long steps, long want, long least, bool documents) {
   Cut c;
   if (blocks <= 0 || steps <= 0) return c;
-  const long fill = std::max(1L, std::min({(want + blocks - 1) / blocks, steps / least, 128L}));
+  const long fill = std::max(1L, std::min({want / blocks, steps / least, 128L}));
   const bool even = fill == 1 && blocks < 4 * want && steps >= 64;   // two pieces for the longest documents
   c.planes = static_cast<int>(even ? 2 : fill);
   c.pieces = even && !documents ? 1 : c.planes;
@@ -1022,7 +1035,8 @@ Plan plan(const AttentionArgs& a) {
                 : cut(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8, doc);
   p.dq = cut(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8, doc);
   p.wide = a.dim > 96 && a.kv_len > 128;
-  p.dkv = cut(bh * (p.wide ? (a.kv_len + 255L) / 256 : (a.kv_len + 127L) / 128), (a.rows + KT - 1L) / KT,
+  const long step = a.group <= KT ? KT / a.group * a.group : KT;
+  p.dkv = cut(bh * (p.wide ? (a.kv_len + 255L) / 256 : (a.kv_len + 127L) / 128), (a.rows + step - 1) / step,
               p.wide ? 512 : 1024, 8, doc);
   return p;
 }
@@ -1041,6 +1055,8 @@ hipError_t prepare(const AttentionArgs& in, Args& a, hipStream_t s) {
   a.c1 = in.cap > 0.0f ? 2.0f * scale / in.cap * LOG2E : scale * LOG2E;
   a.c2 = in.cap * LOG2E;
   a.flip = in.scale < 0.0f;
+  a.step = in.group <= KT ? KT / in.group * in.group : KT;
+  a.by_step = FastDiv(a.step);
   if (!in.documents || in.kv_len == 0) return hipSuccess;
   int2* runs = reinterpret_cast<int2*>(in.ws);
   a.doc = runs;

@@ -293,6 +293,21 @@ def test_attention_gradients_match_differences():
         assert abs(float((grads[n].double() * d).sum()) - slope) <= tol, name
 
 
+def test_rows_with_one_key_in_sight_have_no_score_gradient():
+    """A softmax over one key is 1 whatever its score: dq is zero exactly, and so is dk where every row is such."""
+    for c in ((3, 8, 2, 64, 1, 1, 0, True, "", 0.0, False), (2, 4, 4, 128, 150, 150, 0, False, "every", 20.0, True),
+              (2, 6, 2, 80, 90, 90, 0, True, "every", 0.0, False)):
+        q, k, v, dout, m = _case(c)
+        out, lse, dq, dk, dv = _run(_attention(c), q, k, v, dout, m)
+        r = Reference(q, k, v, c[3] ** -0.5, c[9], m.get("slopes"), _see(c, m), c[6], dout)
+        assert not bool(dq.any()) and not bool(dk.any())
+        _close(dv, r.dv, r.dv_tol, "dv")
+        _close(out, r.out, r.out_tol, "out")
+    c = (2, 4, 2, 64, 70, 70, 0, True, "", 0.0, False)       # the first row of a causal sequence
+    q, k, v, dout, m = _case(c)
+    assert not bool(_run(_attention(c), q, k, v, dout, m)[2][:, 0].any())
+
+
 def test_attention_scale_and_large_scores():
     """Scores of thousands, a negative and a zero scale."""
     from paper_1809_02839_amd import native
