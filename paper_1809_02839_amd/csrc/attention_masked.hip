@@ -98,12 +98,21 @@ __device__ __forceinline__ int2 row_walk(const Args& a, const Sequence& seq, int
   return make_int2(a.by_step.div(row(pa)) * a.step, row(pb));
 }
 
-// Score of one product in units of log2: s log2(e), and tanh(z / cap) where
-// capped. PLAIN scores are the product times c1.
-__device__ __forceinline__ float score(const Args& a, float acc, float& t) {
-  if (a.c2 == 0.0f) return acc * a.c1;
-  t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(acc * a.c1));
-  return t * a.c2;
+// Scores of a group's products in units of log2: s log2(e). Where they are
+// capped, f(r, tanh(z / cap)) is called for each.
+template <typename F>
+__device__ __forceinline__ void scores(const Args& a, f32x16_t& s, F&& f) {
+  if (a.c2 == 0.0f) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] *= a.c1;
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const float t = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[r] * a.c1)), 1.0f);
+    f(r, t);
+    s[r] = t * a.c2;
+  }
 }
 
 // A staged tile: KT rows of C 16-byte chunks in LDS, chunk c of row r in place
@@ -390,11 +399,8 @@ struct Running {
 #pragma unroll
     for (int n = 0; n < N; ++n) s[n] = product<DH>(fq, Ks, 32 * n, frag);
     if (!PLAIN) {
-      float t;
 #pragma unroll
-      for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[n][r] = score(a, s[n][r], t);
+      for (int n = 0; n < N; ++n) scores(a, s[n], [](int, float) {});
       if (a.slopes) {
         const float far = static_cast<float>(p - k0 - col_of(0, lane));
 #pragma unroll
@@ -743,21 +749,17 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c1, -lsum)) * (dp[r] - delta);
       } else {
-        f32x16_t t;
+        f32x16_t dz = dp;   // (dP - delta) by the cap's slope
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float tr = 0.0f;
-          s[r] = score(a, s[r], tr);
-          t[r] = tr;
-        }
+        for (int r = 0; r < 16; ++r) dz[r] -= delta;
+        scores(a, s, [&](int r, float t) { dz[r] *= fmaf(-t, t, 1.0f); });
         if (a.slopes) {
           const float far = static_cast<float>(p - k0 - 32 * n - col_of(0, lane));
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] -= slope * fabsf(far - static_cast<float>(col_of(r, 0)));
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r)   // t is 0 where there is no cap
-          s[r] = __builtin_amdgcn_exp2f(s[r] - lsum) * (dp[r] - delta) * (1.0f - t[r] * t[r]);
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] - lsum) * dz[r];
       }
       if (cut) {
 #pragma unroll
@@ -935,12 +937,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
             dp[r] *= s[r];
           }
         } else {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float t = 0.0f;
-            s[r] = score(a, s[r], t);
-            dp[r] *= 1.0f - t * t;
-          }
+          scores(a, s, [&](int r, float t) { dp[r] *= fmaf(-t, t, 1.0f); });
           if (a.slopes) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
