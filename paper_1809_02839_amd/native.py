@@ -353,18 +353,18 @@ def _dtype_code(t, what):
     raise ValueError(f"{what} must be torch.bfloat16 or torch.float32, got {t.dtype}")
 
 
-def _on(device, stream, call):
-    """call(stream pointer) with `device` current, on `stream` (None: the device's current torch stream)."""
+def _on(device, stream, entry, *args):
+    """entry(*args, stream pointer) with `device` current, on `stream` (None: the device's current torch stream)."""
     import torch
     if device.type != "cuda":
         raise ValueError("operators take GPU tensors")
+    # the current stream's pointer without a Stream object, half of a small call's host time
+    raw = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
     if device.index == torch.cuda.current_device():
-        raw = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
-        _check(call(raw))
+        _check(entry(*args, raw))
         return
     with torch.cuda.device(device):
-        raw = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
-        _check(call(raw))
+        _check(entry(*args, raw))
 
 
 def _heads4(t, shape, dtype, device, what):
@@ -421,7 +421,7 @@ class Rotary:
             d.x, d.out = Strides(*x.stride()[:3]), Strides(*out.stride()[:3])
             self._layout = layout
         d.first_position = first_position
-        _on(x.device, stream, lambda s: lib().spectrain_rotary(ctypes.byref(d), xp, pp, int(bool(inverse)), op, s))
+        _on(x.device, stream, lib().spectrain_rotary, ctypes.byref(d), xp, pp, 1 if inverse else 0, op)
         return out
 
 
@@ -483,8 +483,7 @@ class Attention:
         lp = _side(lse, (d.batch, d.heads, d.q_len), "torch.float32", dev, "lse")
         m = self._masks(dev, documents, prefix, kv_lengths, slopes)
         wp, wn = self._scratch(workspace, dev)
-        _on(dev, stream, lambda s: lib().spectrain_attention_forward(ctypes.byref(d), ctypes.byref(m), *ptr, lp, wp, wn,
-                                                                     s))
+        _on(dev, stream, lib().spectrain_attention_forward, ctypes.byref(d), ctypes.byref(m), *ptr, lp, wp, wn)
 
     def backward(self, q, k, v, out, lse, dout, dq, dk, dv, *, workspace, documents=None, prefix=None, kv_lengths=None,
                  slopes=None, stream=None):
@@ -497,9 +496,8 @@ class Attention:
         lp = _side(lse, (d.batch, d.heads, d.q_len), "torch.float32", dev, "lse")
         m = self._masks(dev, documents, prefix, kv_lengths, slopes)
         wp, wn = self._scratch(workspace, dev)
-        _on(dev, stream, lambda s: lib().spectrain_attention_backward(
-            ctypes.byref(d), ctypes.byref(m), ptr["q"], ptr["k"], ptr["v"], ptr["out"], lp, ptr["dout"], ptr["dq"],
-            ptr["dk"], ptr["dv"], wp, wn, s))
+        _on(dev, stream, lib().spectrain_attention_backward, ctypes.byref(d), ctypes.byref(m), ptr["q"], ptr["k"],
+            ptr["v"], ptr["out"], lp, ptr["dout"], ptr["dq"], ptr["dk"], ptr["dv"], wp, wn)
 
 
 def _checkpoint_args(t, codes, scales, what):
@@ -517,11 +515,11 @@ def checkpoint_pack(x, codes, scales, stream=None):
     """x [rows, cols] to 8-bit codes uint8 [rows, cols] and scales uint8 [rows, ceil(cols / 32)]."""
     dt, rows, cols, cp, sp, ld = _checkpoint_args(x, codes, scales, "x")
     xp = x.data_ptr()
-    _on(x.device, stream, lambda s: lib().spectrain_checkpoint_pack(dt, rows, cols, xp, ld, cp, sp, s))
+    _on(x.device, stream, lib().spectrain_checkpoint_pack, dt, rows, cols, xp, ld, cp, sp)
 
 
 def checkpoint_restore(codes, scales, out, stream=None):
     """The values that codes and scales stand for, into out [rows, cols]."""
     dt, rows, cols, cp, sp, ld = _checkpoint_args(out, codes, scales, "out")
     op = out.data_ptr()
-    _on(out.device, stream, lambda s: lib().spectrain_checkpoint_restore(dt, rows, cols, cp, sp, op, ld, s))
+    _on(out.device, stream, lib().spectrain_checkpoint_restore, dt, rows, cols, cp, sp, op, ld)
