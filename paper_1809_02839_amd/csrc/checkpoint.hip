@@ -63,12 +63,14 @@ __global__ __launch_bounds__(NT) void checkpoint_pack_kernel(Jobs jobs) {
   const Place p = place(a);
   const T* x = static_cast<const T*>(a.x) + p.row * a.ld + p.col;
   float v[PER];
+  uint4 raw = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
   for (int i = 0; i < PER; ++i) v[i] = 0.0f;
   if (WIDE) {
     if (p.live && p.n) {
       if constexpr (sizeof(T) == 2) {
-        const u16x8_t u = *reinterpret_cast<const u16x8_t*>(x);
+        raw = *reinterpret_cast<const uint4*>(x);
+        const u16x8_t u = __builtin_bit_cast(u16x8_t, raw);
 #pragma unroll
         for (int i = 0; i < PER; ++i) v[i] = bf16_to_f32(u[i]);
       } else {
@@ -81,37 +83,63 @@ __global__ __launch_bounds__(NT) void checkpoint_pack_kernel(Jobs jobs) {
     for (int i = 0; i < PER; ++i)
       if (p.live && i < p.n) v[i] = to_float(x[i]);
   }
-  uint32_t top = 0;   // bits of the largest finite magnitude: ordered as the values
+  // bits of the largest magnitude, ordered as the values are
+  uint32_t top = 0;
+  if constexpr (WIDE && sizeof(T) == 2) {
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+    const auto pair = [&](uint32_t w) { return __builtin_bit_cast(u16x2_t, w & 0x7fff7fffu); };
+    const u16x2_t m = __builtin_elementwise_max(__builtin_elementwise_max(pair(raw.x), pair(raw.y)),
+                                                __builtin_elementwise_max(pair(raw.z), pair(raw.w)));
+    top = static_cast<uint32_t>(max(m[0], m[1])) << 16;
+  } else {
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu;
-    if (m < 0x7f800000u) top = max(top, m);
+    for (int i = 0; i < PER; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
   }
   top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1)));
   top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2)));
   // smallest e with top / 2^e <= 448 = 1.75 * 2^8
-  const int e = min(max(static_cast<int>(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u), -117), 120);
-  const float inv = power_of_two(-e), limit = e == 120 ? 240.0f : 448.0f;   // 256 * 2^120 would be infinite
-  uint32_t word[2];
+  const auto exponent = [](uint32_t t) {
+    return min(max(static_cast<int>(t >> 23) - 127 - 8 + ((t & 0x7fffffu) > 0x600000u), -117), 120);
+  };
+  int e = exponent(top);
+  uint32_t word[2] = {0u, 0u};
+  const auto convert = [&](const float (&z)[PER]) {
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    float z[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float t = v[4 * w + i], y = fminf(fmaxf(t * inv, -limit), limit);
-      z[i] = (__float_as_uint(t) & 0x7fffffffu) < 0x7f800000u ? y : __uint_as_float(0x7fc00000u);
+    for (int w = 0; w < 2; ++w) {
+      int c = __builtin_amdgcn_cvt_pk_fp8_f32(z[4 * w], z[4 * w + 1], 0, false);
+      word[w] = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(z[4 * w + 2], z[4 * w + 3], c, true));
     }
-    int c = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
-    c = __builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], c, true);
-    uint32_t u = static_cast<uint32_t>(c);
+  };
+  float z[PER];
+  constexpr float LEAST = 1.0f / 512.0f;   // 2^-9: what is not zero becomes at least this
+  if (!__any(e == 120)) {
+    // no value that is not finite (its bits would make e 120), and none that
+    // needs a limit: a third fewer vector instructions, which bounded the pass
+    const float inv = power_of_two(-e);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {   // what is not zero stays so
-      const bool lost = (u >> (8 * i) & 0x7fu) == 0 && (__float_as_uint(v[4 * w + i]) & 0x7fffffffu) != 0;
-      u |= lost ? 1u << (8 * i) : 0u;
-      u |= lost && v[4 * w + i] < 0.0f ? 0x80u << (8 * i) : 0u;
+    for (int i = 0; i < PER; ++i) {
+      const float m = fmaxf(fabsf(v[i] * inv), LEAST);
+      z[i] = copysignf(v[i] == 0.0f ? 0.0f : m, v[i]);
     }
-    word[w] = u;
+  } else {
+    uint32_t finite = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu;
+      if (m < 0x7f800000u) finite = max(finite, m);
+    }
+    finite = max(finite, static_cast<uint32_t>(__shfl_xor(static_cast<int>(finite), 1)));
+    finite = max(finite, static_cast<uint32_t>(__shfl_xor(static_cast<int>(finite), 2)));
+    e = exponent(finite);
+    const float inv = power_of_two(-e), limit = e == 120 ? 240.0f : 448.0f;   // 256 * 2^120 would be infinite
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const float m = fminf(fmaxf(fabsf(v[i] * inv), LEAST), limit);
+      const float y = copysignf(v[i] == 0.0f ? 0.0f : m, v[i]);
+      z[i] = (__float_as_uint(v[i]) & 0x7fffffffu) < 0x7f800000u ? y : __uint_as_float(0x7fc00000u);
+    }
   }
+  convert(z);
   if (!p.live) return;
   uint8_t* out = a.codes + p.row * a.cols + p.col;
   if (WIDE) {
