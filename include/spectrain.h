@@ -376,8 +376,8 @@ int spectrain_rotary(const spectrain_rotary_desc* desc, const void* x_dev, const
  *   slopes      float32 [heads]
  *   lse         float32 [batch, heads, q_len], contiguous
  * head_dim: a multiple of 8 up to 128; batch * heads * ceil(length / 32) below
- * 2^23 for both lengths. 64 tokens of k and v, and 64 / group tokens by the
- * heads of a group of q and dout, span at most 2^29 elements. Strides are multiples of 8 elements and
+ * 2^23 for both lengths. 64 tokens of k and v, and 64 / group + 1 tokens by
+ * the heads of a group of q and dout, span at most 2^29 elements. Strides are multiples of 8 elements and
  * tensors 16-byte aligned. out may not overlap q, k, v; the gradients may not
  * overlap each other or an input, but all of them may be parts of one packed
  * tensor. */
@@ -388,8 +388,8 @@ typedef struct {
   int32_t q_len, kv_len;
   int32_t q_offset;          /* position of the first query row */
   int32_t causal;            /* 0 or 1; prefix needs 1 */
-  float scale;               /* finite */
-  float cap;                 /* 0: none; > 0 */
+  float scale;               /* |scale| <= 2^100 */
+  float cap;                 /* 0: none; > 0, cap and |scale| / cap <= 2^100 */
   spectrain_strides q, k, v, out;
   spectrain_strides dout, dq, dk, dv;   /* backward only */
 } spectrain_attention_desc;

@@ -1047,8 +1047,7 @@ hipError_t prepare(const AttentionArgs& in, Args& a, hipStream_t s) {
   a.by_group = FastDiv(in.group);
   a.by_bh = FastDiv(in.batch * in.kv_heads);
   a.by_kv = FastDiv(in.kv_heads);
-  // a scale of zero stays above it, so that hidden columns are still -infinity times it
-  const float scale = std::max(std::fabs(in.scale), 1e-30f);
+  const float scale = std::fabs(in.scale);
   a.c1 = in.cap > 0.0f ? 2.0f * scale / in.cap * LOG2E : scale * LOG2E;
   a.c2 = in.cap * LOG2E;
   a.flip = in.scale < 0.0f;
@@ -1065,11 +1064,12 @@ hipError_t prepare(const AttentionArgs& in, Args& a, hipStream_t s) {
 }
 
 // Calls f with the smallest compiled head width that holds dim, and whether
-// scores are products times the scale and no more.
+// scores are products times the scale and no more (and not of a vanishing one:
+// PLAIN divides by it, and hides columns before they are multiplied).
 template <typename F>
 void with_width(const Args& a, F&& f) {
   auto pick = [&](auto width) {
-    if (a.cap > 0.0f || a.slopes) f(width, std::false_type{});
+    if (a.cap > 0.0f || a.slopes || a.c1 < 0x1p-60f) f(width, std::false_type{});
     else f(width, std::true_type{});
   };
   const int dim = a.dim;

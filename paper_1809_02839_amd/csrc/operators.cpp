@@ -123,6 +123,10 @@ AttentionArgs attention_args(const spectrain_attention_desc* desc, bool backward
   if (d.causal != 0 && d.causal != 1) fail("causal must be 0 or 1");
   if (!std::isfinite(d.scale)) fail("scale must be finite");
   if (!(d.cap >= 0.0f) || !std::isfinite(d.cap)) fail("cap must be finite and >= 0");
+  // scores and the factors that form them stay finite
+  constexpr float LARGEST = 1.2676506e30f;   // 2^100
+  if (std::fabs(d.scale) > LARGEST || (d.cap > 0.0f && (d.cap > LARGEST || std::fabs(d.scale) > d.cap * LARGEST)))
+    fail("|scale|, cap and |scale| / cap must be at most 2^100");
   constexpr int MAX_LEN = 1 << 30;   // positions and tile ends stay inside 32 bits
   if (d.q_len > MAX_LEN || d.kv_len > MAX_LEN || d.q_offset > MAX_LEN || d.q_offset < -MAX_LEN)
     fail("q_len, kv_len and |q_offset| must be at most 2^30");
@@ -149,7 +153,7 @@ AttentionArgs attention_args(const spectrain_attention_desc* desc, bool backward
     }
   }
   if (layout) {   // byte offsets inside a tile of 64 rows are 32 bits wide
-    const int64_t g = d.heads / d.kv_heads, q = std::min<int64_t>(d.q_len, 64 / g + 1), k = std::min(d.kv_len, 64);
+    const int64_t g = d.heads / d.kv_heads, q = std::min<int64_t>(d.q_len, 64 / g + 2), k = std::min(d.kv_len, 64);
     const auto span = [&](const spectrain_strides& st, int64_t tokens, int64_t heads, const char* what) {
       if (std::max<int64_t>(tokens - 1, 0) * st.token + (heads - 1) * st.head >= int64_t{1} << 29)
         fail(std::string(what) + ": 64 tokens, and the heads of a group, may span at most 2^29 elements");

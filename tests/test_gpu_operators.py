@@ -203,6 +203,11 @@ CASES = [
     (1, 7, 7, 16, 300, 300, 0, True, "every", 0.0, False),     # every token its own document
     (1, 3, 3, 24, 2100, 2100, 0, True, "doc", 0.0, False),     # runs over several blocks of the run search
     (1, 64, 1, 64, 6, 6, 0, True, "", 0.0, False),
+    (2, 96, 1, 32, 7, 40, 33, True, "len", 0.0, False),        # more heads to a key head than a tile has rows
+    (1, 144, 2, 128, 5, 300, 0, False, "", 12.0, False),
+    (1, 12, 4, 80, 1100, 1100, 0, True, "doc prefix", 0.0, False),   # groups of 3, walks in pieces
+    (2, 1, 1, 128, 4300, 4300, 0, True, "doc", 0.0, False),    # two pieces for long documents
+    (3, 10, 2, 96, 33, 4100, 4067, True, "len", 25.0, True),
 ]
 
 
@@ -314,7 +319,7 @@ def test_attention_scale_and_large_scores():
     g = _gen(5)
     q, k, v, dout = (_randn((1, 100, 2, 64), g, scale=s) for s in (8.0, 8.0, 1.0, 1.0))
     see = _visible(1, 100, 100, 0, True, None, None, None)
-    for scale in (1.0, -0.5, 0.0):
+    for scale in (1.0, -0.5, 0.0, 1e-25, -1e-12):
         a = native.Attention(1, 2, 2, 64, 100, 100, causal=True, scale=scale)
         r = Reference(q, k, v, scale, 0.0, None, see, 0, dout)
         got = _run(a, q, k, v, dout, {})

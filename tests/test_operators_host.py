@@ -93,6 +93,11 @@ def _call(d, masks=None, ws=P, ws_bytes=1 << 20, out=3 * P, q=P, dq=4 * P, dk=5 
     (dict(scale=float("nan")), "scale"),
     (dict(cap=-1.0), "cap"),
     (dict(cap=float("inf")), "cap"),
+    (dict(scale=3e38), "2^100"),
+    (dict(cap=1e-37), "2^100"),
+    (dict(cap=2e30), "2^100"),
+    (dict(k=native.Strides(1 << 34, 1 << 26, 64)), "2^29"),
+    (dict(q=native.Strides(0, 64, 1 << 29)), "2^29"),
     (dict(q_offset=(1 << 30) + 1), "2^30"),
     (dict(kv_len=(1 << 30) + 1), "2^30"),
     (dict(batch=1 << 20, q_len=1 << 10), "2^23"),
