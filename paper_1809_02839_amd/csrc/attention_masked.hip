@@ -611,9 +611,11 @@ __global__ __launch_bounds__(NT) void attention_join_kernel(Args a, long rows, F
   const int pieces = few ? pieces_of(a, 32, walk.x, walk.y) : pieces_of(a, KT, walk.x, walk.y);
   if (pieces == 1) return;   // written already
   float m = -INFINITY;
+#pragma unroll 8   // loads of several pieces under way at once
   for (int u = 0; u < pieces; ++u) m = fmaxf(m, a.part_ml[u * rows + r].x);
   const float base = m == -INFINITY ? 0.0f : m;
   float l = 0.0f, x[8] = {};
+#pragma unroll 4
   for (int u = 0; u < pieces; ++u) {
     const float2 ml = a.part_ml[u * rows + r];
     const float w = __builtin_amdgcn_exp2f(ml.x - base);
@@ -660,6 +662,7 @@ __global__ __launch_bounds__(NT) void attention_sum_kernel(Args a, Sums all) {
   const int pieces = pieces_of(a, blockIdx.y == 0 ? KT : a.step, walk.x, walk.y);
   if (pieces == 1) return;   // written already
   float x[8] = {};
+#pragma unroll 4
   for (int u = 0; u < pieces; ++u) {
     const float4* y = reinterpret_cast<const float4*>(j.part + (u * j.rows + r) * a.dim + col);
     const float4 lo = y[0], hi = y[1];
