@@ -793,8 +793,8 @@ struct RowInfo {
 // dK and dV of WAVES * 32 keys: the wave's own 32 are keys, the walked columns
 // rows. At 128 columns the two results and the fragments of K and V would fill
 // the registers of two waves a SIMD (35 spilled, 2460 us for 16384 causal tokens
-// of 16 heads); eight waves, which share a staged tile and leave LDS for it, keep
-// V there instead (XX us).
+// of 16 heads, two to a key head); eight waves, which share a staged tile and leave LDS for it, keep
+// V there instead (2195 us; with V in registers 2399).
 template <int DH, bool PLAIN, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Args a) {
   using T = Tile<DH>;
@@ -872,14 +872,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
       w.hi[tid] = row ? keys.y : 0;
     }
   };
-  // from the end: under a causal mask that is where the walks of a head's blocks
-  // meet (from their starts they read rows apart, and past the L2: 1046 us in
-  // place of XX)
-  const int top = uniform(begin + static_cast<int>(a.by_step.div(max(0, end - begin - 1))) * a.step);
   if (begin < end) {
-    fetch(top, 0);
-    look(top);
-    note(top, 0);
+    fetch(begin, 0);
+    look(begin);
+    note(begin, 0);
   }
   bf16x8_t fk[DH / 16], fv[V_IN_LDS ? 1 : DH / 16];
   f32x16_t dk[DH / 32], dv[DH / 32];
@@ -898,13 +894,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
   zero(dk);
   zero(dv);
   int buf = 0;
-  for (int r0 = begin < end ? top : begin - 1; r0 >= begin; r0 -= a.step, buf ^= 1) {
+  for (int r0 = begin; r0 < end; r0 += a.step, buf ^= 1) {
     landed();
     __syncthreads();
-    const bool more = r0 > begin;
+    const bool more = r0 + a.step < end;
     if (more) {
-      fetch(r0 - a.step, buf ^ 1);
-      look(r0 - a.step);
+      fetch(r0 + a.step, buf ^ 1);
+      look(r0 + a.step);
     }
     const RowInfo& w = info[buf];
     const int tail = min(a.step, a.rows - r0) - 1;
@@ -980,7 +976,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
         }
       }
     }
-    if (more) note(r0 - a.step, buf ^ 1);
+    if (more) note(r0 + a.step, buf ^ 1);
   }
   if (key >= a.kv_len) return;
   if (pieces > 1) {
