@@ -206,7 +206,7 @@ CASES = [
     (2, 96, 1, 32, 7, 40, 33, True, "len", 0.0, False),        # more heads to a key head than a tile has rows
     (1, 144, 2, 128, 5, 300, 0, False, "", 12.0, False),
     (1, 12, 4, 80, 1100, 1100, 0, True, "doc prefix", 0.0, False),   # groups of 3, walks in pieces
-    (2, 1, 1, 128, 4300, 4300, 0, True, "doc", 0.0, False),    # two pieces for long documents
+    (2, 1, 1, 128, 4300, 4300, 0, True, "doc", 0.0, False),    # walks in many pieces
     (3, 10, 2, 96, 33, 4100, 4067, True, "len", 25.0, True),
 ]
 
