@@ -8,6 +8,13 @@
 // Rows are the queries of every head that shares a key/value head (row r: query
 // r / group, head r % group of the group), so one staging of a key tile serves
 // the whole group.
+//
+// The fragment of the walked operand goes first into the matrix instruction, so a
+// lane ends with scores of one row of its own: masks, maxima and sums of a row are
+// scalars of a lane, and the registers of a group of 32 columns are already an
+// operand of the next product (attention_long.hip). Probabilities and score
+// gradients are rounded to bf16 for it, 2^-8 of each at random, as the results are
+// once more; scores, maxima, sums and results stay float32.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -454,7 +461,12 @@ __device__ __forceinline__ long row_index(const Args& a, int b, int head, int i)
 }
 __device__ __forceinline__ float lse_of(float m, float sum) { return sum == 0.0f ? -INFINITY : m * LN2 + logf(sum); }
 
-// A block: 128 rows, or one piece of their keys.
+// A block: 128 rows, or one piece of their keys; one pass over the keys. The
+// matrix instructions are busy 53% of the time at 128 columns (16 heads, 8192
+// causal tokens, 338 us, 814 TFLOP/s; 16384 tokens with two heads to a key head
+// 1045 us, 1050 TFLOP/s); the rest waits on the exponentials between the two
+// products, four instructions' time each, which the other wave of a SIMD only
+// partly covers. At 64 columns they bound the kernel (905 TFLOP/s).
 template <int DH, bool PLAIN>
 __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   using T = Tile<DH>;
@@ -511,10 +523,11 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   if (a.lse && lane < 32) a.lse[r] = lse_of(run.m, sum);
 }
 
-// Up to 32 rows (single tokens, and what little a group makes of a few): bound
-// by reading the keys and values once, so the block's waves share out the keys,
-// each with tiles of 32 of its own that no other wave waits for, and join their
-// sums at the end.
+// Up to 32 rows (single tokens, and what a group makes of a few): bound by reading
+// the keys and values once, so the block's waves share out the keys, each with
+// tiles of 32 of its own that no other wave waits for, and join their sums at the
+// end. 1.6 GB of 16 ragged caches in 280 us, 5.7 TB/s, where a copy of 1 GiB moves
+// 5.1; 128 rows a block would keep one wave of four busy (1225 us).
 template <int DH, bool PLAIN>
 __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   using T = Tile<DH>;
@@ -680,8 +693,10 @@ __device__ __forceinline__ float log2_sum(const Args& a, long row) {
   return l == -INFINITY ? INFINITY : l * LOG2E;
 }
 
-// dQ of 128 rows (or a piece of it), and delta = out . dout of each for the
-// other kernel.
+// dQ of 128 rows (or a piece of it), and delta = out . dout of each for the other
+// kernel. Scores and dP are formed again from the tiles (three products; matrix
+// instructions busy 62% at 128 columns): 1400 us for 16384 causal tokens of 16
+// heads, two to a key head.
 template <int DH, bool PLAIN>
 __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   using T = Tile<DH>;
@@ -791,10 +806,12 @@ struct RowInfo {
 };
 
 // dK and dV of WAVES * 32 keys: the wave's own 32 are keys, the walked columns
-// rows. At 128 columns the two results and the fragments of K and V would fill
-// the registers of two waves a SIMD (35 spilled, 2460 us for 16384 causal tokens
-// of 16 heads, two to a key head); eight waves, which share a staged tile and leave LDS for it, keep
-// V there instead (2195 us; with V in registers 2399).
+// rows (four products). At 128 columns the two results and the fragments of K and
+// V would fill the registers of two waves a SIMD (35 spilled, 2460 us for 16384
+// causal tokens of 16 heads, two to a key head); eight waves, which share a staged
+// tile and leave LDS for it, keep V there instead (2195 us; with V in registers
+// 2399). Heads that share a key head are walked by one block, so their sum needs
+// no atomics and has one order.
 template <int DH, bool PLAIN, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Args a) {
   using T = Tile<DH>;
@@ -1020,10 +1037,18 @@ Plan plan(const AttentionArgs& a) {
   Plan p;
   const long bh = static_cast<long>(a.batch) * a.kv_heads;
   const long row_tiles = (a.rows + ROWS - 1L) / ROWS;
-  p.few = a.rows <= 64;
-  p.fwd = p.few ? cut(bh * ((a.rows + 31) / 32), (a.kv_len + 31L) / 32, 1024, 8)
-                : cut(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8);
+  // Rows of one wave go to the kernel whose waves share out the keys: 4 rows of 16
+  // x 8 key heads over 32768 keys take 371 us there and 409 in tiles of 128 rows, 8
+  // rows of 32 x 8 over 2048 keys 24 and 33; 64 rows would read the keys twice (30
+  // and 23 over 8192). One block a CU: more gain nothing and have to be joined (4 x
+  // 8 heads of 8192 keys 30 us in 256 blocks, 34 in 512, 45 in 1024).
+  p.few = a.rows <= 32;
+  p.fwd = p.few ? cut(bh, (a.kv_len + 31L) / 32, 256, 8)
+                : cut(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8);   // two blocks a CU
   p.dq = cut(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8);
+  // Eight waves, four: 64 x 1024 tokens and heads 130 us of a backward, 137; 64 x 8
+  // of 256 tokens 116, 121; 2 x 16 of 4096 481, 541. At 128 keys half of the eight
+  // have none: 62, 56.
   p.wide = a.dim > 96 && a.kv_len > 128;
   const long step = a.group <= KT ? KT / a.group * a.group : KT;
   p.dkv = cut(bh * (p.wide ? (a.kv_len + 255L) / 256 : (a.kv_len + 127L) / 128), (a.rows + step - 1) / step,
