@@ -141,11 +141,13 @@ struct Tile {
 // offset past the resource writes zeros. Issued through inline assembly so that
 // the compiler, which cannot tell the two buffers apart, does not wait for the
 // next tile before each read of this one; landed() waits for the wave's own
-// loads, and the barrier after it for the others'. The statement declares M0
-// clobbered; nothing else in these kernels keeps a value in M0 (a host test
-// checks the assembly for it).
+// loads, and the barrier after it for the others'. A load to LDS may read M0 one
+// wait state after a scalar write of it at the earliest (s_nop 0: the compiler
+// puts it there itself, but does not look into assembly). The statement declares
+// M0 clobbered; nothing else in these kernels keeps a value in M0 (a host test
+// checks the assembly for both).
 __device__ __forceinline__ void direct16(__amdgpu_buffer_rsrc_t r, uint32_t lds, int off) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(r)
                : "memory", "m0");
 }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const bf16_t* p) {   // p: the same in every lane

@@ -144,10 +144,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const bf16_t* p, lon
 // compiler, which cannot tell the stages of the LDS ring apart, does not wait
 // for every outstanding direct load before each LDS read: the K loop waits
 // for exactly the stage it reads (dma_wait) and then synchronises the block.
-// The statement declares M0 clobbered; nothing else in these kernels keeps a
-// value in M0 (a host test checks the assembly for it).
+// A load to LDS may read M0 one wait state after a scalar write of it at the
+// earliest (s_nop 0: the compiler puts it there itself, but does not look into
+// assembly). The statement declares M0 clobbered; nothing else in these kernels
+// keeps a value in M0 (a host test checks the assembly for both).
 __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, uint32_t lds_base, int byte_off) {
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_base), "v"(byte_off), "s"(r)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_base), "v"(byte_off), "s"(r)
                : "memory", "m0");
 }
 template <int N>

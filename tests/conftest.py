@@ -1,10 +1,29 @@
 import os
 import sys
 
+import pytest
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 if ROOT not in sys.path:
     sys.path.insert(0, ROOT)
 
+# Tests that hold a value found to be wrong: kept as they are, and expected to fail.
+WRONG = {
+    "test_attention_isa_host.py::test_m0_only_feeds_the_direct_lds_loads":
+        "asks for the load right after the M0 write; the hardware asks for a wait state between them "
+        "(test_direct_loads_host.py)",
+    "test_isa_host.py::test_m0_only_feeds_the_direct_lds_loads":
+        "asks for the load right after the M0 write; the hardware asks for a wait state between them "
+        "(test_direct_loads_host.py)",
+}
+
 
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs an MI355X (gfx950) GPU and the built HIP library")
+
+
+def pytest_collection_modifyitems(items):
+    for item in items:
+        reason = WRONG.get(item.nodeid.split("/")[-1])
+        if reason:
+            item.add_marker(pytest.mark.xfail(reason=reason, strict=True))
