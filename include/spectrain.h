@@ -368,7 +368,8 @@ int spectrain_rotary(const spectrain_rotary_desc* desc, const void* x_dev, const
  *   out = softmax over the visible keys (s) V           lse = ln sum exp(s)
  * A row without a visible key has out 0, lse -infinity and no gradient. Keys
  * at or past kv_lengths[b] are not read. Scores, softmax statistics and sums
- * are float32; probabilities and score gradients are rounded to bf16 for their
+ * are float32 (a cap moves a score by at most 2^-16 up to caps of 64, by 2^-21 of
+ * itself past them); probabilities and score gradients are rounded to bf16 for their
  * products, results once to bf16. Results do not depend on timing: no atomics.
  *   documents   int32 [batch, kv_len]: a document is a run of equal numbers
  *               (needs 0 <= q_offset and q_offset + q_len <= kv_len)

@@ -30,8 +30,9 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 struct Args : AttentionArgs {
   const int2* doc = nullptr;      // [batch][kv_len]: first and past-the-last token of the token's document
   float* delta = nullptr;         // [batch][heads][q_len]: out . dout (backward)
-  float c1 = 0.0f;                // uncapped: |scale| log2(e); capped: 2 |scale| / cap log2(e)
-  float c2 = 0.0f;                // capped: cap log2(e)
+  float c1 = 0.0f;                // |scale| log2(e)
+  float c2 = 0.0f, c3 = 0.0f;     // capped: cap log2(e), and one over it
+  float c4 = 0.0f;                // capped: 2 |scale| / cap log2(e)
   int flip = 0;                   // scale < 0: one operand of the scores changes sign instead
   FastDiv by_group, by_bh, by_kv, by_tiles, by_step;
   int step = KT;                  // rows of a step of the walk over rows: whole queries, where a group fits a tile
@@ -105,20 +106,65 @@ __device__ __forceinline__ int2 row_walk(const Args& a, const Sequence& seq, int
   return make_int2(a.by_step.div(row(pa)) * a.step, row(pb));
 }
 
+// How a kernel forms scores from products: times the scale and no more; capped or
+// with a bias; and capped by more than NEAR_CAP.
+enum Scores { PLAIN, GENERAL, FAR_CAP };
+
 // Scores of a group's products in units of log2: s log2(e). Where they are
 // capped, f(r, tanh(z / cap)) is called for each.
-template <typename F>
+//
+// tanh(u) = 1 - 2 / (1 + e^(2u)) is off by 2^-22.6 whatever u is, a score by
+// 2^-22.6 cap: 2^-16 at most for caps up to NEAR_CAP, which changes a probability
+// by 2^-16 of itself. Past it, for |u| <= 1/2, tanh(u) is u p(u^2) and the score z
+// p, off relative to themselves however far the cap is (p: degree 4, fitted for
+// the least error of tanh(u) / u, 2^-26 exactly and 2^-23 as evaluated), and only
+// for larger |u|, where 2^-22.6 is 2^-21.5 of the value, the first form. A group
+// with no such score takes the polynomial alone. Near caps keep the first form, the
+// faster one (16 heads of 4096 causal tokens capped at 30: forward 138 us, backward
+// 446; by the second form 147 and 540).
+constexpr float NEAR_CAP = 64.0f;
+template <int KIND, typename F>
 __device__ __forceinline__ void scores(const Args& a, f32x16_t& s, F&& f) {
-  if (a.c2 == 0.0f) {
+  const auto tanh_far = [&](float product) {
+    return fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(product * a.c4)), 1.0f);
+  };
+  if (KIND == GENERAL) {
+    if (a.c2 == 0.0f) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] *= a.c1;
+      for (int r = 0; r < 16; ++r) s[r] *= a.c1;
+      return;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float t = tanh_far(s[r]);
+      f(r, t);
+      s[r] = t * a.c2;
+    }
+    return;
+  }
+  const auto ratio = [](float u) {   // tanh(u) / u
+    const float y = u * u;
+    return fmaf(y, fmaf(y, fmaf(y, fmaf(y, 0.01724149100482464f, -0.05304549261927605f), 0.13325878977775574f),
+                        -0.333331435918808f), 1.0f);
+  };
+  float top = 0.0f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(s[r]));
+  if (!__any(top * a.c1 > 0.5f * a.c2)) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float z = s[r] * a.c1, u = z * a.c3, p = ratio(u);
+      f(r, u * p);
+      s[r] = z * p;
+    }
     return;
   }
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const float t = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(s[r] * a.c1)), 1.0f);
-    f(r, t);
-    s[r] = t * a.c2;
+    const float z = s[r] * a.c1, u = z * a.c3, p = ratio(u), far = tanh_far(s[r]);
+    const bool near = fabsf(u) <= 0.5f;
+    f(r, near ? u * p : far);
+    s[r] = near ? z * p : far * a.c2;
   }
 }
 
@@ -400,16 +446,16 @@ struct Running {
 
   // Takes in 32 N keys from k0 on. cut: the tile's columns are compared with the
   // row's keys.
-  template <bool PLAIN, int N>
+  template <int KIND, int N>
   __device__ __forceinline__ void take(const Args& a, const Lane<DH>& frag, const char* Ks, const char* Vs,
                                        const bf16x8_t (&fq)[DH / 16], int k0, int p, float slope, int2 mine, bool cut,
                                        int lane) {
     f32x16_t s[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) s[n] = product<DH>(fq, Ks, 32 * n, frag);
-    if (!PLAIN) {
+    if (KIND != PLAIN) {
 #pragma unroll
-      for (int n = 0; n < N; ++n) scores(a, s[n], [](int, float) {});
+      for (int n = 0; n < N; ++n) scores<KIND>(a, s[n], [](int, float) {});
       if (a.slopes) {
         const float far = static_cast<float>(p - k0 - col_of(0, lane));
 #pragma unroll
@@ -418,7 +464,7 @@ struct Running {
           for (int r = 0; r < 16; ++r) s[n][r] -= slope * fabsf(far - static_cast<float>(32 * n + col_of(r, 0)));
       }
     }
-    const float c1 = PLAIN ? a.c1 : 1.0f;   // s c1: the scores
+    const float c1 = KIND == PLAIN ? a.c1 : 1.0f;   // s c1: the scores
     if (cut) {
 #pragma unroll
       for (int n = 0; n < N; ++n)
@@ -469,7 +515,7 @@ __device__ __forceinline__ float lse_of(float m, float sum) { return sum == 0.0f
 // 1045 us, 1050 TFLOP/s); the rest waits on the exponentials between the two
 // products, four instructions' time each, which the other wave of a SIMD only
 // partly covers. At 64 columns they bound the kernel (905 TFLOP/s).
-template <int DH, bool PLAIN>
+template <int DH, int KIND>
 __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   using T = Tile<DH>;
   __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, K or V
@@ -509,7 +555,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
     __syncthreads();
     if (k0 + KT < end) fetch(k0 + KT, buf ^ 1);
     if (k0 >= wlast.y || k0 + KT <= wfirst.x) continue;
-    run.template take<PLAIN, KT / 32>(a, frag, lds[buf][0], lds[buf][1], fq, k0, p, slope, mine,
+    run.template take<KIND, KT / 32>(a, frag, lds[buf][0], lds[buf][1], fq, k0, p, slope, mine,
                                     k0 < wlast.x || k0 + KT > wfirst.y, lane);
   }
   const float sum = run.sum + __shfl_xor(run.sum, 32);
@@ -530,7 +576,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
 // tiles of 32 of its own that no other wave waits for, and join their sums at the
 // end. 1.6 GB of 16 ragged caches in 280 us, 5.7 TB/s, where a copy of 1 GiB moves
 // 5.1; 128 rows a block would keep one wave of four busy (1225 us).
-template <int DH, bool PLAIN>
+template <int DH, int KIND>
 __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   using T = Tile<DH>;
   constexpr int FT = 32, BYTES = T::BYTES / (KT / FT);
@@ -571,7 +617,7 @@ __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
     landed();
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other buffer has been read
     if (k0 + FT < end) fetch(k0 + FT, buf ^ 1);
-    run.template take<PLAIN, 1>(a, frag, lds[wave][buf][0], lds[wave][buf][1], fq, k0, p, slope, mine,
+    run.template take<KIND, 1>(a, frag, lds[wave][buf][0], lds[wave][buf][1], fq, k0, p, slope, mine,
                               k0 < last.x || k0 + FT > first.y, lane);
   }
   const float sum = run.sum + __shfl_xor(run.sum, 32);
@@ -699,7 +745,7 @@ __device__ __forceinline__ float log2_sum(const Args& a, long row) {
 // kernel. Scores and dP are formed again from the tiles (three products; matrix
 // instructions busy 61% at 128 columns): 1400 us for 16384 causal tokens of 16
 // heads, two to a key head.
-template <int DH, bool PLAIN>
+template <int DH, int KIND>
 __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   using T = Tile<DH>;
   __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, K or V
@@ -765,14 +811,14 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
     for (int n = 0; n < KT / 32; ++n) {
       f32x16_t s = product<DH>(fq, Ks, 32 * n, frag);
       const f32x16_t dp = product<DH>(fo, Vs, 32 * n, frag);
-      if (PLAIN) {
+      if (KIND == PLAIN) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.c1, -lsum)) * (dp[r] - delta);
       } else {
         f32x16_t dz = dp;   // (dP - delta) by the cap's slope
 #pragma unroll
         for (int r = 0; r < 16; ++r) dz[r] -= delta;
-        scores(a, s, [&](int r, float t) { dz[r] *= fmaf(-t, t, 1.0f); });
+        scores<KIND>(a, s, [&](int r, float t) { dz[r] *= fmaf(-t, t, 1.0f); });
         if (a.slopes) {
           const float far = static_cast<float>(p - k0 - 32 * n - col_of(0, lane));
 #pragma unroll
@@ -814,7 +860,7 @@ struct RowInfo {
 // tile and leave LDS for it, keep V there instead (2195 us; with V in registers
 // 2399). Heads that share a key head are walked by one block, so their sum needs
 // no atomics and has one order.
-template <int DH, bool PLAIN, int WAVES>
+template <int DH, int KIND, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Args a) {
   using T = Tile<DH>;
   __shared__ __attribute__((aligned(16))) char lds[2][2][T::BYTES];   // buffer, Q or dO
@@ -883,7 +929,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
       const int p = a.q_offset + static_cast<int>(a.by_group.div(r0 + tid));
       const int2 keys = seq.clip(a, p, rdoc);
       // also where the row has no weight
-      w.sum[tid] = row && rl != -INFINITY ? -rl * (PLAIN ? LOG2E / a.c1 : LOG2E) : -INFINITY;
+      w.sum[tid] = row && rl != -INFINITY ? -rl * (KIND == PLAIN ? LOG2E / a.c1 : LOG2E) : -INFINITY;
       w.delta[tid] = row ? -rd : 0.0f;
       w.slope[tid] = rs * LOG2E;
       w.position[tid] = p;
@@ -936,7 +982,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
         for (int g = 0; g < 4; ++g) {
           const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
           const int c = 32 * n + col_of(4 * g, lane);
-          const float4 su = PLAIN ? *reinterpret_cast<const float4*>(w.sum + c) : z;
+          const float4 su = KIND == PLAIN ? *reinterpret_cast<const float4*>(w.sum + c) : z;
           const float4 de = *reinterpret_cast<const float4*>(w.delta + c);
           s[4 * g] = su.x, s[4 * g + 1] = su.y, s[4 * g + 2] = su.z, s[4 * g + 3] = su.w;
           dp[4 * g] = de.x, dp[4 * g + 1] = de.y, dp[4 * g + 2] = de.z, dp[4 * g + 3] = de.w;
@@ -948,14 +994,14 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
           if constexpr (V_IN_LDS) dp = mfma(lf.row_frag(Os, 32 * n, q), lf.row_frag(my_v, 0, q), dp);
           else dp = mfma(lf.row_frag(Os, 32 * n, q), fv[q], dp);
         }
-        if (PLAIN) {
+        if (KIND == PLAIN) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             s[r] = __builtin_amdgcn_exp2f(s[r] * a.c1);
             dp[r] *= s[r];
           }
         } else {
-          scores(a, s, [&](int r, float t) { dp[r] *= fmaf(-t, t, 1.0f); });
+          scores<KIND>(a, s, [&](int r, float t) { dp[r] *= fmaf(-t, t, 1.0f); });
           if (a.slopes) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
@@ -1068,8 +1114,12 @@ hipError_t prepare(const AttentionArgs& in, Args& a, hipStream_t s) {
   a.by_bh = FastDiv(in.batch * in.kv_heads);
   a.by_kv = FastDiv(in.kv_heads);
   const float scale = std::fabs(in.scale);
-  a.c1 = in.cap > 0.0f ? 2.0f * scale / in.cap * LOG2E : scale * LOG2E;
+  a.c1 = scale * LOG2E;
   a.c2 = in.cap * LOG2E;
+  if (in.cap > 0.0f) {
+    a.c3 = 1.0f / a.c2;   // FAR_CAP only
+    a.c4 = 2.0f * scale / in.cap * LOG2E;
+  }
   a.flip = in.scale < 0.0f;
   a.step = in.group <= KT ? KT / in.group * in.group : KT;
   a.by_step = FastDiv(a.step);
@@ -1083,14 +1133,15 @@ hipError_t prepare(const AttentionArgs& in, Args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Calls f with the smallest compiled head width that holds dim, and whether
-// scores are products times the scale and no more (and not of a vanishing one:
-// PLAIN divides by it, and hides columns before they are multiplied).
+// Calls f with the smallest compiled head width that holds dim, and how scores
+// are formed (not PLAIN with a vanishing scale: it divides by it, and hides columns
+// before they are multiplied).
 template <typename F>
 void with_width(const Args& a, F&& f) {
   auto pick = [&](auto width) {
-    if (a.cap > 0.0f || a.slopes || a.c1 < 0x1p-60f) f(width, std::false_type{});
-    else f(width, std::true_type{});
+    if (a.cap > NEAR_CAP) f(width, std::integral_constant<int, FAR_CAP>{});
+    else if (a.cap > 0.0f || a.slopes || a.c1 < 0x1p-60f) f(width, std::integral_constant<int, GENERAL>{});
+    else f(width, std::integral_constant<int, PLAIN>{});
   };
   const int dim = a.dim;
   if (dim <= 32) pick(std::integral_constant<int, 32>{});
@@ -1130,9 +1181,9 @@ hipError_t attention_masked_fwd(const AttentionArgs& in, hipStream_t s) {
   const Plan p = plan(in);
   a.part = reinterpret_cast<float*>(in.ws + doc_bytes(in));
   a.part_ml = reinterpret_cast<float2*>(in.ws + doc_bytes(in) + part_bytes(p.fwd, q_rows(in), in.dim));
-  with_width(a, [&](auto width, auto plain) {
-    e = p.few ? launch(attention_masked_few_kernel<width(), plain()>, NT, a, a.rows, 32, p.fwd, s)
-              : launch(attention_masked_fwd_kernel<width(), plain()>, NT, a, a.rows, ROWS, p.fwd, s);
+  with_width(a, [&](auto width, auto kind) {
+    e = p.few ? launch(attention_masked_few_kernel<width(), kind()>, NT, a, a.rows, 32, p.fwd, s)
+              : launch(attention_masked_fwd_kernel<width(), kind()>, NT, a, a.rows, ROWS, p.fwd, s);
   });
   if (e != hipSuccess || p.fwd.pieces == 1) return e;
   const long rows = static_cast<long>(q_rows(in));
@@ -1163,10 +1214,10 @@ hipError_t attention_masked_bwd(const AttentionArgs& in, hipStream_t s) {
     sums.sum[at] = {part, out, to, static_cast<long>(rows), FastDiv(heads), FastDiv(tokens), c.pieces, c.quantum};
     most = std::max(most, static_cast<long>(rows));
   };
-  with_width(a, [&](auto width, auto plain) {
+  with_width(a, [&](auto width, auto kind) {
     if (a.q_len > 0) {
       a.part = part_q;
-      e = launch(attention_masked_dq_kernel<width(), plain()>, NT, a, a.rows, ROWS, p.dq, s);
+      e = launch(attention_masked_dq_kernel<width(), kind()>, NT, a, a.rows, ROWS, p.dq, s);
       if (e != hipSuccess) return;
       sum(0, part_q, a.dq, a.sdq, q_rows(in), a.heads, a.q_len, p.dq);
     }
@@ -1175,10 +1226,10 @@ hipError_t attention_masked_bwd(const AttentionArgs& in, hipStream_t s) {
     a.part2 = part_v;
     constexpr bool kWide = width() == 128;
     if constexpr (kWide) {
-      if (p.wide) e = launch(attention_masked_dkv_kernel<width(), plain(), 8>, 512, a, a.kv_len, 256, p.dkv, s);
+      if (p.wide) e = launch(attention_masked_dkv_kernel<width(), kind(), 8>, 512, a, a.kv_len, 256, p.dkv, s);
     }
     if (!kWide || !p.wide)
-      e = launch(attention_masked_dkv_kernel<width(), plain(), 4>, 256, a, a.kv_len, 128, p.dkv, s);
+      e = launch(attention_masked_dkv_kernel<width(), kind(), 4>, 256, a, a.kv_len, 128, p.dkv, s);
     if (e != hipSuccess) return;
     sum(1, part_k, a.dk, a.sdk, k_rows(in), a.kv_heads, a.kv_len, p.dkv);
     sum(2, part_v, a.dv, a.sdv, k_rows(in), a.kv_heads, a.kv_len, p.dkv);

@@ -1,0 +1,95 @@
+"""GPU: the stand-alone operators at the far ends of what they accept, against
+plain implementations in 64 bits. The bounds are those of test_gpu_operators.py,
+but for capped scores, whose bound does not grow with the cap: tanh as
+1 - 2 / (1 + e^(2u)) is off by 2^-22.6 and a score by that times the cap, up to
+2^-16 at caps of 64; past them a score is off relative to itself, below 2^-21 of it
+(z by the roundings of its sum, tanh(u) / u by 2^-23 up to |u| = 1/2, and beyond
+2^-22.6 is 2^-21.5 of a value of 0.46 or more).
+"""
+import pytest
+
+from test_gpu_operators import Reference, _case, _close, _run, _see
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+class Capped(Reference):
+    """The definition with bounds that no cap above 64 makes larger."""
+
+    def __init__(self, q, k, v, scale, cap, slopes, see, offset, dout):
+        super().__init__(q, k, v, scale, cap, slopes, see, offset, dout)
+        (B, Sq, H, D), Sk, Hk, BF = q.shape, k.shape[1], k.shape[2], 2.0 ** -8
+        T, back = (lambda t: t.transpose(2, 3)), (lambda t: t.transpose(1, 2))
+        Q, dO = back(q.double()), back(dout.double())
+        K, V = (back(t.double()).repeat_interleave(H // Hk, 1) for t in (k, v))
+        z = scale * Q @ T(K)
+        s = cap * torch.tanh(z / cap)
+        if slopes is not None:
+            far = (torch.arange(Sq, device="cuda")[:, None] + offset - torch.arange(Sk, device="cuda")[None]).abs()
+            s = s - slopes.double()[None, :, None, None] * far
+        hidden, empty = ~see[:, None], self.empty[..., None]
+        lse = self.lse[..., None].masked_fill(empty, 0.0)
+        P = torch.exp(s.masked_fill(hidden, -float("inf")) - lse).masked_fill(empty, 0.0)
+        sums = (D + 8) * 2.0 ** -24                       # of `dim` products in float32, relative to their magnitudes
+        Ez = sums * (abs(scale) * Q.abs() @ T(K.abs())).masked_fill(hidden, 0.0).amax((1, 2, 3), keepdim=True)
+        E = Ez + 2.0 ** -21 * (1 + s.masked_fill(hidden, 0.0).abs().amax()) + 2.0 ** -22 * min(cap, 64.0)
+        out = back(self.out)
+        out_tol = (BF + 2 * E) * (P @ V.abs()) * (1 + 2 * BF) + BF * out.abs()
+        self.out_tol, self.lse_tol = back(out_tol), (E + 2.0 ** -22 * lse.abs())[..., 0]
+        dP, delta = dO @ T(V), (out * dO).sum(3, keepdim=True)
+        delta_tol = (out_tol * dO.abs()).sum(3, keepdim=True) + sums * (out.abs() * dO.abs()).sum(3, keepdim=True)
+        # the cap's slope 1 - tanh^2 by at most 0.77 of the error of z / cap, and twice tanh's own
+        slope_tol = 0.77 * Ez / cap + 2.0 ** -20
+        dS_tol = P * (delta_tol + sums * dO.abs() @ T(V.abs())) + (BF + 2 * E + slope_tol) * P * (dP.abs() + delta.abs())
+        dS_tol = dS_tol * abs(scale) * (1 + 2 * BF)
+        group = lambda t: back(t.reshape(B, Hk, H // Hk, Sk, D).sum(2))
+        self.dq_tol = back(dS_tol @ K.abs()) + BF * self.dq.abs()
+        self.dk_tol = group(T(dS_tol) @ Q.abs()) + BF * self.dk.abs()
+        self.dv_tol = group(T(P) @ dO.abs()) * (BF + 2 * E) * (1 + 2 * BF) + BF * self.dv.abs()
+
+
+@pytest.mark.parametrize("cap", [1e-3, 0.7, 4.0, 64.0, 65.0, 1e3, 1e4, 1e6, 1e9, 1e30])
+@pytest.mark.parametrize("shape", [
+    # B, H, Hk, D, Sq, Sk, offset, causal, masks, slopes
+    (2, 8, 2, 64, 1, 300, 299, True, "len", False),        # single tokens
+    (1, 4, 4, 128, 200, 200, 0, True, "doc", False),       # eight waves of dK and dV
+    (2, 6, 2, 80, 130, 130, 0, True, "prefix", True),
+    (1, 2, 2, 32, 70, 150, 80, False, "len", False),
+    (1, 2, 1, 64, 1100, 1100, 0, True, "", True),          # walks in pieces
+], ids=lambda s: "-".join(str(v) for v in s))
+def test_capped_scores_over_the_range_of_caps(shape, cap):
+    from paper_1809_02839_amd import native
+    B, H, Hk, D, Sq, Sk, offset, causal, kind, biased = shape
+    print(f"[capped] {shape} cap {cap}", flush=True)
+    c = (B, H, Hk, D, Sq, Sk, offset, causal, kind, cap, biased)
+    q, k, v, dout, m = _case(c)
+    scale = D ** -0.5
+    r = Capped(q, k, v, scale, cap, m.get("slopes"), _see(c, m), offset, dout)
+    a = native.Attention(B, H, Hk, D, Sq, Sk, causal=causal, q_offset=offset, cap=cap)
+    out, lse, dq, dk, dv = _run(a, q, k, v, dout, m)
+    _close(out, r.out, r.out_tol, "out")
+    _close(lse.masked_fill(r.empty, 0.0), r.lse.masked_fill(r.empty, 0.0), r.lse_tol, "lse")
+    for got, name in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+        _close(got, getattr(r, name), getattr(r, name + "_tol"), name)
+
+
+def test_capped_scores_at_the_ends_of_cap_and_scale():
+    """Scales of 0 and near it, caps of single steps, and scores far past a cap: finite, and as defined."""
+    from paper_1809_02839_amd import native
+    c = (1, 2, 2, 64, 90, 90, 0, True, "", 0.0, False)
+    q, k, v, dout, m = _case(c)
+    for scale, cap in ((0.0, 1e-45), (0.0, 5.0), (1e-38, 1e-40), (1e-38, 1e30), (-0.3, 1e30), (1e30, 1.0),
+                       (1e30, 1e30), (-2.0, 3.0)):
+        print(f"[cap and scale] {scale} {cap}", flush=True)
+        a = native.Attention(1, 2, 2, 64, 90, 90, causal=True, scale=scale, cap=cap)
+        # the operator takes scale and cap in 32 bits
+        scale, cap = (float(torch.tensor(x, dtype=torch.float32)) for x in (scale, cap))
+        r = Capped(q, k, v, scale, cap, None, _see(c, m), 0, dout)
+        got = _run(a, q, k, v, dout, m)
+        assert all(bool(t.isfinite().all()) for t in got)
+        if cap < 1e29 or scale < 1.0:      # else scores are far past what a softmax resolves
+            _close(got[0], r.out, r.out_tol, "out")
+            _close(got[1], r.lse, r.lse_tol, "lse")
+            for x, name in zip(got[2:], ("dq", "dk", "dv")):
+                _close(x, getattr(r, name), getattr(r, name + "_tol"), name)
