@@ -402,7 +402,8 @@ class Rotary:
         d.rotary_dim = head_dim if rotary_dim is None else rotary_dim
         d.layout, d.scaling = ROTARY_LAYOUTS[layout], ROTARY_SCALINGS[scaling]
         d.base, d.factor, d.original_length = base, factor, original_length
-        self._d, self._layout = d, None
+        self._d = d
+        self._last = (None, None)   # layout of the last call and its descriptor, which no later call changes
 
     def apply(self, x, out=None, positions=None, first_position=0, inverse=False, stream=None):
         """Turn x [batch, token, head, head_dim] into out (None: in place; any
@@ -414,13 +415,15 @@ class Rotary:
         xp = _heads4(x, x.shape, x.dtype, x.device, "x")
         op = _heads4(out, x.shape, x.dtype, x.device, "out")
         pp = _side(positions, x.shape[:2], "torch.int32", x.device, "positions")
-        d, layout = self._d, (x.shape, x.stride(), out.stride(), x.dtype)
-        if layout != self._layout:
+        layout = (x.shape, x.stride(), out.stride(), x.dtype, first_position)
+        last, d = self._last
+        if layout != last:   # a new one: another thread's call may be reading the old
+            d = RotaryDesc.from_buffer_copy(self._d)
             d.dtype = _dtype_code(x, "x")
             d.batch, d.tokens, d.heads = x.shape[:3]
             d.x, d.out = Strides(*x.stride()[:3]), Strides(*out.stride()[:3])
-            self._layout = layout
-        d.first_position = first_position
+            d.first_position = first_position
+            self._last = (layout, d)
         _on(x.device, stream, lib().spectrain_rotary, ctypes.byref(d), xp, pp, 1 if inverse else 0, op)
         return out
 
@@ -440,7 +443,7 @@ class Attention:
         d.scale = head_dim ** -0.5 if scale is None else scale
         d.cap = cap
         self._d = d
-        self._layout = {}
+        self._last = {}   # forward, backward: strides of the last call and its descriptor, which no later call changes
         self._qs, self._ks = (batch, q_len, heads, head_dim), (batch, kv_len, kv_heads, head_dim)
 
     def workspace_bytes(self, backward=False):
@@ -453,14 +456,18 @@ class Attention:
         import torch
         return torch.empty(max(256, self.workspace_bytes(backward)), dtype=torch.uint8, device=device)
 
-    def _tensor(self, name, t, shape, q):
+    def _described(self, pass_, tensors, q):
+        """Pointers of (name, tensor, shape), after their checks, and the descriptor with their strides."""
         import torch
-        p = _heads4(t, shape, torch.bfloat16, q.device, name)
-        st = t.stride()
-        if self._layout.get(name) != st:
-            setattr(self._d, name, Strides(*st[:3]))
-            self._layout[name] = st
-        return p
+        ptr = [_heads4(t, shape, torch.bfloat16, q.device, name) for name, t, shape in tensors]
+        strides = tuple([t.stride() for _, t, _ in tensors])
+        last, d = self._last.get(pass_, (None, None))
+        if strides != last:   # a new one: another thread's call may be reading the old
+            d = AttentionDesc.from_buffer_copy(self._d)
+            for (name, _, _), st in zip(tensors, strides):
+                setattr(d, name, Strides(*st[:3]))
+            self._last[pass_] = (strides, d)
+        return ptr, d
 
     def _masks(self, device, documents, prefix, kv_lengths, slopes):
         d = self._d
@@ -477,9 +484,9 @@ class Attention:
     def forward(self, q, k, v, out, lse=None, *, workspace, documents=None, prefix=None, kv_lengths=None, slopes=None,
                 stream=None):
         """out = attention(q, k, v); lse float32 [batch, heads, q_len] as the backward takes it (None: not wanted)."""
-        dev, d = q.device, self._d
-        ptr = [self._tensor(n, t, s, q) for n, t, s in (("q", q, self._qs), ("k", k, self._ks), ("v", v, self._ks),
-                                                        ("out", out, self._qs))]
+        dev = q.device
+        ptr, d = self._described("forward", (("q", q, self._qs), ("k", k, self._ks), ("v", v, self._ks),
+                                             ("out", out, self._qs)), q)
         lp = _side(lse, (d.batch, d.heads, d.q_len), "torch.float32", dev, "lse")
         m = self._masks(dev, documents, prefix, kv_lengths, slopes)
         wp, wn = self._scratch(workspace, dev)
@@ -488,16 +495,15 @@ class Attention:
     def backward(self, q, k, v, out, lse, dout, dq, dk, dv, *, workspace, documents=None, prefix=None, kv_lengths=None,
                  slopes=None, stream=None):
         """dq, dk, dv (overwritten) from the forward's tensors and masks and dout."""
-        dev, d = q.device, self._d
-        qs, ks = self._qs, self._ks
-        ptr = {n: self._tensor(n, t, s, q) for n, t, s in (
+        dev, qs, ks = q.device, self._qs, self._ks
+        ptr, d = self._described("backward", (
             ("q", q, qs), ("k", k, ks), ("v", v, ks), ("out", out, qs), ("dout", dout, qs), ("dq", dq, qs),
-            ("dk", dk, ks), ("dv", dv, ks))}
+            ("dk", dk, ks), ("dv", dv, ks)), q)
         lp = _side(lse, (d.batch, d.heads, d.q_len), "torch.float32", dev, "lse")
         m = self._masks(dev, documents, prefix, kv_lengths, slopes)
         wp, wn = self._scratch(workspace, dev)
-        _on(dev, stream, lib().spectrain_attention_backward, ctypes.byref(d), ctypes.byref(m), ptr["q"], ptr["k"],
-            ptr["v"], ptr["out"], lp, ptr["dout"], ptr["dq"], ptr["dk"], ptr["dv"], wp, wn)
+        _on(dev, stream, lib().spectrain_attention_backward, ctypes.byref(d), ctypes.byref(m), *ptr[:4], lp,
+            *ptr[4:], wp, wn)
 
 
 def _checkpoint_args(t, codes, scales, what):

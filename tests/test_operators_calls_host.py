@@ -1,0 +1,50 @@
+"""Host-side checks of how the binding calls the operators (no GPU needed)."""
+import pytest
+
+from paper_1809_02839_amd import native
+
+torch = pytest.importorskip("torch")
+
+
+def _heads(*shape):
+    return torch.zeros(*shape, dtype=torch.bfloat16)
+
+
+def _interrupt(monkeypatch, other):
+    """The descriptors that two calls hand to the library, the second made (by `other`) while the first is inside."""
+    seen, depth = [], []
+
+    def on(device, stream, entry, *args):
+        depth.append(args[0])
+        if len(depth) == 1:
+            other()
+        seen.append(type(args[0]._obj).from_buffer_copy(args[0]._obj))
+
+    monkeypatch.setattr(native, "_on", on)
+    return seen
+
+
+def test_rotary_calls_do_not_share_a_descriptor(monkeypatch):
+    """Another thread's call on the same object, with its own layout and position, changes nothing of this one's."""
+    r = native.Rotary(64)
+    seen = _interrupt(monkeypatch, lambda: r.apply(_heads(1, 7, 2, 64), first_position=9))
+    for x, first in ((_heads(2, 3, 4, 64), 5), (_heads(1, 7, 2, 64), 0)):   # another layout; another position only
+        seen.clear()
+        r.apply(x, first_position=first)
+        d = seen[-1]
+        assert (d.batch, d.tokens, d.heads, d.first_position) == (*x.shape[:3], first)
+        assert (d.x.batch, d.x.token, d.x.head) == x.stride()[:3]
+
+
+def test_attention_calls_do_not_share_a_descriptor(monkeypatch):
+    a = native.Attention(2, 4, 2, 64, 3, 3)
+    q, k, ws = _heads(2, 3, 4, 64), _heads(2, 3, 2, 64), torch.empty(256, dtype=torch.uint8)
+    wide = _heads(2, 3, 5, 64)[:, :, :4]
+    lse = torch.zeros(2, 4, 3)
+    seen = _interrupt(monkeypatch, lambda: a.forward(wide, k, k, wide, workspace=ws))
+    a.forward(q, k, k, q, workspace=ws)
+    assert (seen[0].q.token, seen[0].out.token) == (320, 320) and (seen[1].q.token, seen[1].out.token) == (256, 256)
+    seen = _interrupt(monkeypatch, lambda: a.backward(wide, k, k, q, lse, q, wide, k, k, workspace=ws))
+    a.backward(q, k, k, q, lse, wide, q, k, k, workspace=ws)
+    assert (seen[0].q.token, seen[0].dout.token, seen[0].dq.token) == (320, 256, 320)
+    assert (seen[1].q.token, seen[1].dout.token, seen[1].dq.token) == (256, 320, 256)
