@@ -444,7 +444,9 @@ int spectrain_checkpoint_restore(int32_t dtype, int64_t rows, int64_t cols, cons
  * stash keeps the turned qkv, and lse (float32 [B, heads, S]) as buffer 13l+1;
  * buffer 13l+2 is unused. EINVAL for another kind of stage, a head dimension
  * above 128 (or whatever spectrain_rotary refuses); ESTATE while a mini-batch
- * is in flight. The stage's buffers are made anew (ENOMEM leaves the stage as
+ * is in flight, and for an attention that is not causal while masks with a prefix
+ * wait for their mini-batch (masks that wait are kept; attn NULL drops them). The
+ * stage's buffers are made anew (ENOMEM leaves the stage as
  * it was), so graphs captured before the call must not be replayed.
  * Synchronises the stream. */
 typedef struct {

@@ -187,7 +187,7 @@ AttentionArgs attention_args(const spectrain_attention_desc* desc, bool backward
   return a;
 }
 
-void attention_masks(AttentionArgs& a, const spectrain_attention_masks* m, void* ws, size_t ws_bytes, size_t need) {
+void attention_masks(AttentionArgs& a, const spectrain_attention_masks* m) {
   if (m) {
     a.documents = m->documents;
     a.prefix = m->prefix;
@@ -202,6 +202,9 @@ void attention_masks(AttentionArgs& a, const spectrain_attention_masks* m, void*
     fail("documents need 0 <= q_offset and q_offset + q_len <= kv_len");
   if (a.documents && static_cast<int64_t>(a.batch) * ((a.kv_len + 1023) / 1024) >= 1 << 22)
     fail("documents need batch * kv_len / 1024 below 2^22");
+}
+
+void check_workspace(const void* ws, size_t ws_bytes, size_t need) {
   if (need && (!ws || ws_bytes < need))
     fail("workspace of " + std::to_string(ws_bytes) + " bytes is smaller than the " + std::to_string(need) +
          " bytes needed");
@@ -220,11 +223,17 @@ size_t attention_workspace(const spectrain_attention_desc* desc, bool backward) 
   return attention_ws_bytes(a, backward);
 }
 
+void check_attention_masks(const spectrain_attention_desc* desc, const spectrain_attention_masks* masks) {
+  AttentionArgs a = attention_args(desc, false, false);
+  attention_masks(a, masks);
+}
+
 void run_attention_forward(const spectrain_attention_desc* desc, const spectrain_attention_masks* masks, const void* q,
                            const void* k, const void* v, void* out, float* lse, void* ws, size_t ws_bytes,
                            hipStream_t s) {
   AttentionArgs a = attention_args(desc, false);
-  attention_masks(a, masks, ws, ws_bytes, attention_ws_bytes(a, false));
+  attention_masks(a, masks);
+  check_workspace(ws, ws_bytes, attention_ws_bytes(a, false));
   const int64_t nq = static_cast<int64_t>(a.batch) * a.q_len, nk = static_cast<int64_t>(a.batch) * a.kv_len;
   check_tensor(q, nq, "q");
   check_tensor(k, nk, "k");
@@ -245,7 +254,8 @@ void run_attention_backward(const spectrain_attention_desc* desc, const spectrai
                             const void* k, const void* v, const void* out, const float* lse, const void* dout,
                             void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, hipStream_t s) {
   AttentionArgs a = attention_args(desc, true);
-  attention_masks(a, masks, ws, ws_bytes, attention_ws_bytes(a, true));
+  attention_masks(a, masks);
+  check_workspace(ws, ws_bytes, attention_ws_bytes(a, true));
   const int64_t nq = static_cast<int64_t>(a.batch) * a.q_len, nk = static_cast<int64_t>(a.batch) * a.kv_len;
   check_tensor(q, nq, "q");
   check_tensor(k, nk, "k");

@@ -11,6 +11,8 @@ void run_rotary(const spectrain_rotary_desc* d, const void* x, const int32_t* po
                 hipStream_t s);
 
 size_t attention_workspace(const spectrain_attention_desc* d, bool backward);
+// The checks that a forward or backward makes of its masks.
+void check_attention_masks(const spectrain_attention_desc* d, const spectrain_attention_masks* masks);
 void run_attention_forward(const spectrain_attention_desc* d, const spectrain_attention_masks* masks, const void* q,
                            const void* k, const void* v, void* out, float* lse, void* ws, size_t ws_bytes,
                            hipStream_t s);

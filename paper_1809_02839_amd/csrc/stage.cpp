@@ -1404,6 +1404,11 @@ void Stage::set_attention(const spectrain_stage_attention* attn, const float* sl
       for (float v : next.slopes)
         if (!std::isfinite(v)) fail("slopes must be finite");
     }
+    if (!attn->causal)   // masks set for coming mini-batches stay valid
+      for (const auto& [mb, m] : next_masks_)
+        if (m.prefix)
+          throw StageError(SPECTRAIN_ESTATE, "the masks of mini-batch " + std::to_string(mb) +
+                                                 " have a prefix, which needs a causal attention");
   }
   reconfigure(std::move(next));
 }
@@ -1422,9 +1427,8 @@ void Stage::set_masks(int64_t mb, const spectrain_attention_masks* masks) {
   if (!opt_.masked) throw StageError(SPECTRAIN_ESTATE, "masks need spectrain_stage_set_attention");
   if (!masks) fail("masks is NULL");
   if (masks->slopes) fail("slopes belong to the stage's attention");
-  if (masks->prefix && !opt_.attn.causal) fail("prefix needs a causal attention");
-  for (const int32_t* p : {masks->documents, masks->prefix, masks->kv_lengths})
-    if (reinterpret_cast<uintptr_t>(p) % 4) fail("a mask is not 4-byte aligned");
+  const spectrain_attention_desc a = masked_desc(opt_);
+  check_attention_masks(&a, masks);
   for (const Slot& sl : slots_)
     if (sl.used && sl.mb == mb) throw StageError(SPECTRAIN_ESTATE, "mini-batch already in flight");
   next_masks_[mb] = *masks;
