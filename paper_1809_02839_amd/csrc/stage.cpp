@@ -581,11 +581,9 @@ void Stage::plan_buffers() {
             static_cast<size_t>(T * d * 2), static_cast<size_t>(T * d * 2), static_cast<size_t>(T * d * 2),
             static_cast<size_t>(T * 3 * d * 2), static_cast<size_t>(ce ? T * V * 4 : 0),
             static_cast<size_t>(ce ? T * 4 : 0)};
-      if (opt_.masked || opt_.packed) {   // ids 12: masked attention, 13 .. 17: a layer's restored activations
+      if (opt_.masked) {   // id 12
         const spectrain_attention_desc ad = masked_desc(opt_);
-        ws.push_back(opt_.masked ? attention_workspace(&ad, true) : 0);
-        const long widest = std::max(F, d);
-        for (long cols : {widest, d, d, d, d}) ws.push_back(opt_.packed ? static_cast<size_t>(T * cols * 2) : 0);
+        ws.push_back(attention_workspace(&ad, true));
       }
       partial = std::max(partial_floats(T, 3 * d), partial_floats(T, F));
       if (ce) partial = std::max(partial, partial_floats(T, V));
@@ -619,6 +617,11 @@ void Stage::plan_buffers() {
   ws.push_back(std::max<size_t>(gemm_ws_bytes_, 1));                   // split-K partials, stage stream
   ws_split2_ = static_cast<int>(ws.size());
   ws.push_back(std::max<size_t>(gemm_ws_bytes_, 1));                   // split-K partials, side stream
+  ws_restored_ = static_cast<int>(ws.size());
+  if (opt_.packed) {   // f1 (or a layer output), r1, h, r2 and the layer input, restored
+    const size_t T = static_cast<size_t>(B) * dm[3], d = dm[0], widest = std::max(dm[2], dm[0]);
+    for (size_t cols : {widest, d, d, d, d}) ws.push_back(T * cols * 2);
+  }
   if (defer_cap_ > 0) {
     const size_t o = defer_block_.add(static_cast<size_t>(defer_cap_) * 4);
     defer_block_.allocate();
@@ -643,8 +646,9 @@ void Stage::plan_buffers() {
   for (size_t b : st) stash_off_.push_back(probe.add(std::max<size_t>(b, 1)));
   for (size_t b : ws) ws_off_.push_back(ws_block_.add(std::max<size_t>(b, 1)));
   // a second copy for a forward that runs beside a backward (the combined
-  // call), allocated here so that the call itself allocates nothing
-  for (size_t b : ws) ws_block_f_.add(std::max<size_t>(b, 1));
+  // call), allocated here so that the call itself allocates nothing; a forward
+  // restores nothing
+  for (int i = 0; i < ws_restored_; ++i) ws_block_f_.add(std::max<size_t>(ws[i], 1));
   const int nslots = d_.num_stages - d_.stage_index;
   slots_.resize(nslots);
   slot_blocks_.resize(nslots);
@@ -877,9 +881,9 @@ size_t Stage::read_stash(int64_t mb, int index, void* host, size_t capacity) {
     const int j = index % 13;
     if (j == 4 || (j >= 7 && j <= 9) || j == 12) {   // through the workspace: no pass is using it
       const DeviceGuard on(device_);
-      checkpoint(slot, {{index, ws<bf16_t>(13), j == 8 ? d_.dims[2] : d_.dims[0]}}, false);
+      checkpoint(slot, {{index, ws<bf16_t>(ws_restored_), j == 8 ? d_.dims[2] : d_.dims[0]}}, false);
       sync();
-      hip_check(hipMemcpy(host, ws<char>(13), n, hipMemcpyDeviceToHost), "copy stash");
+      hip_check(hipMemcpy(host, ws<char>(ws_restored_), n, hipMemcpyDeviceToHost), "copy stash");
       return n;
     }
   }
@@ -1608,8 +1612,8 @@ void Stage::fwd_tfm(int slot, const void* x, void* y, const int32_t* labels, flo
 
 // workspace ids: 0 scores/dP (f32; kTiles: row sums of P dP), 1 dS, 2/3 layer-output gradient ping-pong,
 // 4 dr2, 5 df1, 6 dh, 7 dr1, 8 dctx, 9 dqkv, 10 logits (f32, CE head),
-// 11 per-token losses (CE head); with positions, masks or an 8-bit stash 12 masked attention, 13 f1, 14 r1, 15 h,
-// 16 r2 and 17 the layer input, restored; then column-sum partials
+// 11 per-token losses (CE head), 12 masked attention (with positions or masks), then column-sum partials and
+// split-K partials; restored from an 8-bit stash: ws_restored_ + 0 f1, 1 r1, 2 h, 3 r2 and 4 the layer input
 void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
   const int L = d_.num_layers, B = d_.batch, d = d_.dims[0], Hh = d_.dims[1], F = d_.dims[2], S = d_.dims[3];
   const int T = B * S, dh = d / Hh;
@@ -1618,13 +1622,14 @@ void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
   const Slot& sl = slots_[slot];
   float* part = ws<float>(ws_colsum_);
   float* part2 = ws<float>(ws_colsum2_);
+  const int back = ws_restored_;
   const void* gy = dy;
   int pp = 2;
   if (d_.head == SPECTRAIN_HEAD_CE) {   // vocabulary head: its gradients and dY of the last layer
     const int V = d_.dims[4];
     const bf16_t* dl = stash<bf16_t>(slot, 13 * L);
-    const void* yL = opt_.packed ? ws<void>(17) : stash<void>(slot, 13 * (L - 1) + 12);
-    if (opt_.packed) checkpoint(slot, {{13 * (L - 1) + 12, ws<bf16_t>(17), d}}, false);
+    const void* yL = opt_.packed ? ws<void>(back + 4) : stash<void>(slot, 13 * (L - 1) + 12);
+    if (opt_.packed) checkpoint(slot, {{13 * (L - 1) + 12, ws<bf16_t>(back + 4), d}}, false);
     GemmDesc gw = gd(V, d, T, opR(dl, V), opR(yL, d), d);
     gw.epi.out_f32 = grad(12 * L);
     gemm(gw);
@@ -1638,15 +1643,15 @@ void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
   for (int l = L - 1; l >= 0; --l) {
     const int p = 12 * l, q = 13 * l;
     auto act = [&](int id, int w) { return opt_.packed ? ws<bf16_t>(w) : stash<bf16_t>(slot, id); };
-    const void* a = l == 0 ? sl.x : act(q - 1, 17);
+    const void* a = l == 0 ? sl.x : act(q - 1, back + 4);
     const bf16_t* qkv = stash<bf16_t>(slot, q);
     const float* P = stash<float>(slot, q + 1);
     const bf16_t* Pb = stash<bf16_t>(slot, q + 2);
     const bf16_t* ctx = stash<bf16_t>(slot, q + 3);
-    const bf16_t* r1 = act(q + 4, 14);
-    const bf16_t* h = act(q + 7, 15);
-    const bf16_t* f1 = act(q + 8, 13);
-    const bf16_t* r2 = act(q + 9, 16);
+    const bf16_t* r1 = act(q + 4, back + 1);
+    const bf16_t* h = act(q + 7, back + 2);
+    const bf16_t* f1 = act(q + 8, back);
+    const bf16_t* r2 = act(q + 9, back + 3);
     bf16_t* dr2 = ws<bf16_t>(4);
     bf16_t* df1 = ws<bf16_t>(5);
     bf16_t* dhh = ws<bf16_t>(6);
@@ -1655,13 +1660,11 @@ void Stage::bwd_tfm(int slot, const void* dy, void* dx) {
     bf16_t* dqkv = ws<bf16_t>(9);
 
     if (opt_.packed) {   // this layer's activations, over those of the layer above
-      for (int w : {13, 15, 17}) protect(ws<void>(w));
-      if (l > 0)
-        checkpoint(slot, {{q + 4, ws<bf16_t>(14), d}, {q + 7, ws<bf16_t>(15), d}, {q + 8, ws<bf16_t>(13), F},
-                          {q + 9, ws<bf16_t>(16), d}, {q - 1, ws<bf16_t>(17), d}}, false);
-      else
-        checkpoint(slot, {{q + 4, ws<bf16_t>(14), d}, {q + 7, ws<bf16_t>(15), d}, {q + 8, ws<bf16_t>(13), F},
-                          {q + 9, ws<bf16_t>(16), d}}, false);
+      for (int w : {0, 2, 4}) protect(ws<void>(back + w));
+      const Packed f1_{q + 8, ws<bf16_t>(back), F}, r1_{q + 4, ws<bf16_t>(back + 1), d}, h_{q + 7, ws<bf16_t>(back + 2), d},
+          r2_{q + 9, ws<bf16_t>(back + 3), d};
+      if (l > 0) checkpoint(slot, {r1_, h_, f1_, r2_, {q - 1, ws<bf16_t>(back + 4), d}}, false);
+      else checkpoint(slot, {r1_, h_, f1_, r2_}, false);
     }
 
     // layer-norm backward rows on the stage stream; its parameter gradients

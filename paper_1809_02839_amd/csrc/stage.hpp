@@ -332,7 +332,7 @@ class Stage {
   bool concurrent_ = false;              // issuing the passes of forward_backward
   // workspace ids after the kind's own buffers: column-sum partials of the
   // stage stream and of the side stream, split-K partials of each stream
-  int ws_colsum_ = -1, ws_colsum2_ = -1, ws_split_ = -1, ws_split2_ = -1;
+  int ws_colsum_ = -1, ws_colsum2_ = -1, ws_split_ = -1, ws_split2_ = -1, ws_restored_ = -1;
   size_t gemm_ws_bytes_ = 0;
   float* ext_ws_ = nullptr;              // split-K partials of the current call, when not the workspace
   hipStream_t s2_ = nullptr;             // side stream (weight gradients), default priority

@@ -49,3 +49,25 @@ def test_waiting_masks_outlive_a_new_attention_only_where_it_takes_them():
     torch.cuda.synchronize()
     for s in (st, other):
         s.destroy()
+
+
+@pytest.mark.parametrize("layers", [1, 3])
+def test_an_8_bit_stash_adds_one_layer_of_activations_to_the_workspace(layers):
+    """Device memory of a stage with one slot: what the slot saves, against one layer's restored activations."""
+    spec, st = _stage(layers=layers, S=1024, k=0, n=1, d=512, batch=32, ffn=2048)
+    T, d, F = 32 * 1024, 512, 2048
+
+    def held():
+        torch.cuda.synchronize()
+        free, total = torch.cuda.mem_get_info()
+        return total - free
+
+    plain = held()
+    st.set_stash("e4m3")
+    packed = held() - plain
+    st.set_stash("bf16")
+    assert abs(held() - plain) <= 8 << 20                # as before, up to the allocator's granules
+    kept = T * (3 * d + F) * layers + T * d * (layers - 1)   # r1, h, r2, f1, and the outputs between layers
+    saved = kept * 2 - kept * 33 // 32
+    assert packed <= T * (F + 4 * d) * 2 - saved + (8 << 20)
+    st.destroy()
