@@ -367,7 +367,9 @@ int spectrain_rotary(const spectrain_rotary_desc* desc, const void* x_dev, const
  *                  and    j <= p or j < prefix[b]       (causal; prefix may be NULL: 0)
  *   out = softmax over the visible keys (s) V           lse = ln sum exp(s)
  * A row without a visible key has out 0, lse -infinity and no gradient. Keys
- * at or past kv_lengths[b] are not read. Scores, softmax statistics and sums
+ * that no row sees (past kv_lengths[b], or past the last row of a causal call) and
+ * rows that see no key may hold anything; a value that is not finite in others may
+ * reach rows and keys beside its own. Scores, softmax statistics and sums
  * are float32 (a cap moves a score by at most 2^-16 up to caps of 64, by 2^-21 of
  * itself past them); probabilities and score gradients are rounded to bf16 for their
  * products, results once to bf16. Results do not depend on timing: no atomics.

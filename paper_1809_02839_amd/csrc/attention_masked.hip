@@ -83,15 +83,15 @@ struct Sequence {
   }
 };
 
-// Keys that the rows [row0, row0 + n) see between them, from a multiple of W on.
-template <int W>
-__device__ __forceinline__ int2 key_walk(const Args& a, const Sequence& seq, int row0, int n) {
+// Keys that the rows [row0, row0 + n) see between them; a walk over them begins
+// at a multiple of its step.
+__device__ __forceinline__ int2 key_span(const Args& a, const Sequence& seq, int row0, int n) {
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
-  return make_int2(seq.keys(a, position(row0)).x / W * W, seq.keys(a, position(row0 + n - 1)).y);
+  return make_int2(seq.keys(a, position(row0)).x, seq.keys(a, position(row0 + n - 1)).y);
 }
 
-// Rows that see one of the keys [key0, key0 + n), from a multiple of a.step on.
-__device__ __forceinline__ int2 row_walk(const Args& a, const Sequence& seq, int key0, int n) {
+// Rows that see one of the keys [key0, key0 + n); likewise.
+__device__ __forceinline__ int2 row_span(const Args& a, const Sequence& seq, int key0, int n) {
   const int valid = min(seq.limit, key0 + n);
   if (key0 >= valid) return make_int2(0, 0);
   int pa = -(1 << 30), pb = 0x7fffffff;   // their positions
@@ -103,7 +103,7 @@ __device__ __forceinline__ int2 row_walk(const Args& a, const Sequence& seq, int
   const auto row = [&](int p) {
     return static_cast<int>(min(max(static_cast<long>(p) - a.q_offset, 0L) * a.group, static_cast<long>(a.rows)));
   };
-  return make_int2(a.by_step.div(row(pa)) * a.step, row(pb));
+  return make_int2(row(pa), row(pb));
 }
 
 // How a kernel forms scores from products: times the scale and no more; capped or
@@ -226,19 +226,23 @@ struct Loader {
       off[i] = col < dim ? static_cast<int>(min(2 * (row(r) + col), static_cast<long>(OUTSIDE))) : OUTSIDE;
     }
   }
-  // Starts the copy of rows first .. (zero from `limit` on) into LDS; of a tile
-  // with fewer rows the others are OUTSIDE as they are.
-  __device__ __forceinline__ void start(const bf16_t* base, uint32_t lds, int first, int limit, int t,
+  // Starts the copy of rows first .. into LDS, zeros for those outside `span`: what
+  // nothing sees may hold anything (memory not written yet), and a probability of
+  // zero would not hide what is not finite. Of a tile with fewer rows the others are
+  // OUTSIDE as they are.
+  __device__ __forceinline__ void start(const bf16_t* base, uint32_t lds, int first, int2 span, int t,
                                         int rows = N) const {
     const __amdgpu_buffer_rsrc_t r = resource(base);
     const uint32_t to = uniform(static_cast<int>(lds)) + (THREADS > 64 ? 1024 * __builtin_amdgcn_readfirstlane(t >> 6) : 0);
-    if (first + rows <= limit) {
+    if (first >= span.x && first + rows <= span.y) {
 #pragma unroll
       for (int i = 0; i < V; ++i) direct16(r, to + 16 * THREADS * i, off[i]);
     } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        direct16(r, to + 16 * THREADS * i, first + (t + THREADS * i) / T::C < limit ? off[i] : OUTSIDE);
+      for (int i = 0; i < V; ++i) {
+        const int at = first + (t + THREADS * i) / T::C;
+        direct16(r, to + 16 * THREADS * i, at >= span.x && at < span.y ? off[i] : OUTSIDE);
+      }
     }
   }
 };
@@ -528,8 +532,8 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   const int2 mine = seq.keys(a, p);
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
   const int2 wfirst = uniform(seq.keys(a, position(row0))), wlast = uniform(seq.keys(a, position(row0 + 31)));
-  const int2 walk = uniform(key_walk<KT>(a, seq, at.tile * ROWS, ROWS));
-  int begin = walk.x, end = walk.y;
+  const int2 span = uniform(key_span(a, seq, at.tile * ROWS, ROWS));
+  int begin = span.x / KT * KT, end = span.y;
   const int pieces = uniform(pieces_of(a, KT, begin, end));
   if (at.piece >= pieces) return;
   share(KT, at.piece, pieces, begin, end);
@@ -539,8 +543,8 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   kl.init(tid, a.dim, [&](int r) { return r * a.sk.t; });
   vl.init(tid, a.dim, [&](int r) { return r * a.sv.t; });
   const auto fetch = [&](int k0, int buf) {
-    kl.start(k + k0 * a.sk.t, lds_address(lds[buf][0]), k0, seq.limit, tid);
-    vl.start(v + k0 * a.sv.t, lds_address(lds[buf][1]), k0, seq.limit, tid);
+    kl.start(k + k0 * a.sk.t, lds_address(lds[buf][0]), k0, span, tid);
+    vl.start(v + k0 * a.sv.t, lds_address(lds[buf][1]), k0, span, tid);
   };
   if (begin < end) fetch(begin, 0);
   const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
@@ -592,7 +596,8 @@ __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   const int2 mine = seq.keys(a, p);
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
   const int2 first = uniform(seq.keys(a, position(row0))), last = uniform(seq.keys(a, position(row0 + 31)));
-  int begin = first.x / FT * FT, end = last.y;
+  const int2 span = make_int2(first.x, last.y);
+  int begin = span.x / FT * FT, end = span.y;
   const int pieces = uniform(pieces_of(a, FT, begin, end));
   if (at.piece >= pieces) return;
   share(FT, at.piece * (NT / 64) + wave, pieces * (NT / 64), begin, end);
@@ -602,8 +607,8 @@ __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   kl.init(lane, a.dim, [&](int r) { return r * a.sk.t; });
   vl.init(lane, a.dim, [&](int r) { return r * a.sv.t; });
   const auto fetch = [&](int k0, int buf) {
-    kl.start(k + k0 * a.sk.t, lds_address(lds[wave][buf][0]), k0, seq.limit, lane);
-    vl.start(v + k0 * a.sv.t, lds_address(lds[wave][buf][1]), k0, seq.limit, lane);
+    kl.start(k + k0 * a.sk.t, lds_address(lds[wave][buf][0]), k0, span, lane);
+    vl.start(v + k0 * a.sv.t, lds_address(lds[wave][buf][1]), k0, span, lane);
   };
   if (begin < end) fetch(begin, 0);
   const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
@@ -667,9 +672,8 @@ __global__ __launch_bounds__(NT) void attention_join_kernel(Args a, long rows, F
   const uint32_t b = by_heads.div(bh), h = bh - b * by_heads.d;
   const Sequence seq(a, b);
   const int packed = i * a.group + (h - a.by_group.div(h) * a.group), tile = few ? 32 : ROWS;
-  const int2 walk = few ? key_walk<32>(a, seq, packed / tile * tile, tile)
-                        : key_walk<KT>(a, seq, packed / tile * tile, tile);
-  const int pieces = few ? pieces_of(a, 32, walk.x, walk.y) : pieces_of(a, KT, walk.x, walk.y);
+  const int2 span = key_span(a, seq, packed / tile * tile, tile);
+  const int pieces = few ? pieces_of(a, 32, span.x / 32 * 32, span.y) : pieces_of(a, KT, span.x / KT * KT, span.y);
   if (pieces == 1) return;   // written already
   float m = -INFINITY;
 #pragma unroll 8   // loads of several pieces under way at once
@@ -716,11 +720,13 @@ __global__ __launch_bounds__(NT) void attention_sum_kernel(Args a, Sums all) {
   const uint32_t b = j.by_tokens.div(bt), t = bt - b * j.by_tokens.d;
   const Sequence seq(a, b);
   const int packed = t * a.group + (h - a.by_group.div(h) * a.group);
-  const int2 walk = blockIdx.y == 0 ? key_walk<KT>(a, seq, packed / ROWS * ROWS, ROWS)
-                                    : row_walk(a, seq, static_cast<int>(t) / all.keys * all.keys, all.keys);
+  const bool by_rows = blockIdx.y == 0;
+  const int2 span = by_rows ? key_span(a, seq, packed / ROWS * ROWS, ROWS)
+                            : row_span(a, seq, static_cast<int>(t) / all.keys * all.keys, all.keys);
   a.pieces = j.pieces;
   a.quantum = j.quantum;
-  const int pieces = pieces_of(a, blockIdx.y == 0 ? KT : a.step, walk.x, walk.y);
+  const int pieces = by_rows ? pieces_of(a, KT, span.x / KT * KT, span.y)
+                             : pieces_of(a, a.step, a.by_step.div(span.x) * a.step, span.y);
   if (pieces == 1) return;   // written already
   float x[8] = {};
 #pragma unroll 4
@@ -758,8 +764,8 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   const int2 mine = seq.keys(a, p);
   const auto position = [&](int r) { return a.q_offset + static_cast<int>(a.by_group.div(min(r, a.rows - 1))); };
   const int2 wfirst = uniform(seq.keys(a, position(row0))), wlast = uniform(seq.keys(a, position(row0 + 31)));
-  const int2 walk = uniform(key_walk<KT>(a, seq, at.tile * ROWS, ROWS));
-  int begin = walk.x, end = walk.y;
+  const int2 span = uniform(key_span(a, seq, at.tile * ROWS, ROWS));
+  int begin = span.x / KT * KT, end = span.y;
   const int pieces = uniform(pieces_of(a, KT, begin, end));
   if (at.piece >= pieces) return;
   share(KT, at.piece, pieces, begin, end);
@@ -769,8 +775,8 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   kl.init(tid, a.dim, [&](int r) { return r * a.sk.t; });
   vl.init(tid, a.dim, [&](int r) { return r * a.sv.t; });
   const auto fetch = [&](int k0, int buf) {
-    kl.start(k + k0 * a.sk.t, lds_address(lds[buf][0]), k0, seq.limit, tid);
-    vl.start(v + k0 * a.sv.t, lds_address(lds[buf][1]), k0, seq.limit, tid);
+    kl.start(k + k0 * a.sk.t, lds_address(lds[buf][0]), k0, span, tid);
+    vl.start(v + k0 * a.sv.t, lds_address(lds[buf][1]), k0, span, tid);
   };
   if (begin < end) fetch(begin, 0);
   const float slope = a.slopes ? a.slopes[head] * LOG2E : 0.0f;
@@ -876,8 +882,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
   const int valid = min(seq.limit, key0 + KEYS);
   const bf16_t* q = a.q + at.b * a.sq.b + at.kh * a.group * a.sq.h;
   const bf16_t* dout = a.dout + at.b * a.sdo.b + at.kh * a.group * a.sdo.h;
-  const int2 walk = uniform(row_walk(a, seq, key0, KEYS));
-  int begin = walk.x, end = walk.y;
+  const int2 span = uniform(row_span(a, seq, key0, KEYS));
+  int begin = uniform(a.by_step.div(span.x) * a.step), end = span.y;
   const int pieces = uniform(pieces_of(a, a.step, begin, end));
   if (at.piece >= pieces) return;
   share(a.step, at.piece, pieces, begin, end);
@@ -898,15 +904,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
     const int i0 = a.by_group.div(r0);
     const bf16_t *qb = q + i0 * a.sq.t, *ob = dout + i0 * a.sdo.t;
     if (regular) {
-      ql.start(qb, lds_address(lds[buf][0]), r0, a.rows, tid, a.step);
-      dol.start(ob, lds_address(lds[buf][1]), r0, a.rows, tid, a.step);
+      ql.start(qb, lds_address(lds[buf][0]), r0, span, tid, a.step);
+      dol.start(ob, lds_address(lds[buf][1]), r0, span, tid, a.step);
       return;
     }
     Loader<DH, KT, THREADS> l;
     l.init(tid, a.dim, [&](int r) { return offset(a.sq, r0, r); });
-    l.start(qb, lds_address(lds[buf][0]), r0, a.rows, tid);
+    l.start(qb, lds_address(lds[buf][0]), r0, span, tid);
     l.init(tid, a.dim, [&](int r) { return offset(a.sdo, r0, r); });
-    l.start(ob, lds_address(lds[buf][1]), r0, a.rows, tid);
+    l.start(ob, lds_address(lds[buf][1]), r0, span, tid);
   };
   // The staged rows' statistics: loaded as the tile is (nothing waits for them
   // there), worked out and stored in LDS after the products of the tile before.
@@ -952,7 +958,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Arg
     Loader<DH, 32, 64> l;
     l.init(lane, a.dim, [&](int r) { return r * a.sv.t; });
     const int first_key = uniform(wkey0);
-    l.start(v + first_key * a.sv.t, lds_address(my_v), first_key, seq.limit, lane);
+    l.start(v + first_key * a.sv.t, lds_address(my_v), first_key, make_int2(0, seq.limit), lane);
   } else {
     load_row<DH>(v + kc * a.sv.t, dim, lane, fv);
   }

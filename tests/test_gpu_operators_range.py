@@ -8,7 +8,7 @@ but for capped scores, whose bound does not grow with the cap: tanh as
 """
 import pytest
 
-from test_gpu_operators import Reference, _case, _close, _run, _see
+from test_gpu_operators import Reference, _attention, _case, _close, _run, _see
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -93,3 +93,47 @@ def test_capped_scores_at_the_ends_of_cap_and_scale():
             _close(got[1], r.lse, r.lse_tol, "lse")
             for x, name in zip(got[2:], ("dq", "dk", "dv")):
                 _close(x, getattr(r, name), getattr(r, name + "_tol"), name)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_what_nothing_sees_may_hold_anything(D):
+    """NaN in the unwritten end of a cache (no lengths given), in a document no query row belongs to, and in rows
+    that see no key (before the first key; in a document past the valid keys) changes nothing."""
+    nan = float("nan")
+
+    def same(c, m, spoil):
+        q, k, v, dout, _ = _case(c)
+        clean = _run(_attention(c), q, k, v, dout, m)
+        for t in clean:
+            assert not bool(t.isnan().any())
+        spoil(q, k, v, dout)
+        for name, x, y in zip(("out", "lse", "dq", "dk", "dv"), clean, _run(_attention(c), q, k, v, dout, m)):
+            assert torch.equal(x, y), name
+
+    for Sq in (1, 9, 100, 150):            # a cache of 333 keys of which 70 + Sq are written
+        print(f"[unseen] {D} {Sq}", flush=True)
+
+        def end_of_cache(q, k, v, dout):
+            k[:, 70 + Sq:], v[:, 70 + Sq:] = nan, nan
+
+        same((2, 4, 2, D, Sq, 333, 70, True, "", 0.0, False), {}, end_of_cache)
+
+    docs = torch.cat([torch.zeros(77), torch.ones(83)]).int().cuda().expand(2, -1).contiguous()
+
+    def other_document(q, k, v, dout):
+        k[:, :77], v[:, :77] = nan, nan
+
+    for Sq in (1, 60):
+        same((2, 4, 2, D, Sq, 160, 160 - Sq, True, "", 0.0, False), {"documents": docs}, other_document)
+
+    def early_rows(q, k, v, dout):
+        q[:, :30], dout[:, :30] = nan, nan
+
+    same((2, 4, 2, D, 130, 100, -30, True, "", 0.0, False), {}, early_rows)
+    lengths = torch.tensor([77, 40], dtype=torch.int32, device="cuda")
+
+    def late_rows(q, k, v, dout):          # the second document lies past the valid keys
+        q[:, 77:], dout[:, 77:] = nan, nan
+        k[0, 77:], v[0, 77:], k[1, 40:], v[1, 40:] = nan, nan, nan, nan
+
+    same((2, 4, 2, D, 160, 160, 0, False, "", 0.0, False), {"documents": docs, "kv_lengths": lengths}, late_rows)
