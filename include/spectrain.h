@@ -307,8 +307,8 @@ int spectrain_stage_read_stash(spectrain_stage_t st, int64_t mb_id, int32_t inde
  * stream) of the current device, which has to be the tensors' device, and
  * allocates and keeps nothing, so it can be captured in a HIP graph. Tensors
  * are device memory; their last dimension is contiguous. A tensor with a
- * dimension of 0 is allowed and makes the call write nothing (an attention
- * with kv_len 0 has rows that see no key: see there).
+ * dimension of 0 is allowed, and nothing of it is touched (an attention with kv_len
+ * 0 has rows that see no key: see there; with q_len 0 its dk and dv are zero).
  * Workspace memory is the caller's: calls that may overlap need one each. */
 
 /* Strides, in elements, of a [batch, token, head, head_dim] tensor, each in

@@ -1199,7 +1199,7 @@ hipError_t attention_masked_fwd(const AttentionArgs& in, hipStream_t s) {
 }
 
 hipError_t attention_masked_bwd(const AttentionArgs& in, hipStream_t s) {
-  if (in.batch == 0) return hipSuccess;
+  if (in.batch == 0 || (in.q_len == 0 && in.kv_len == 0)) return hipSuccess;
   Args a;
   hipError_t e = prepare(in, a, s);
   if (e != hipSuccess) return e;

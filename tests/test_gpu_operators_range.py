@@ -137,3 +137,11 @@ def test_what_nothing_sees_may_hold_anything(D):
         k[0, 77:], v[0, 77:], k[1, 40:], v[1, 40:] = nan, nan, nan, nan
 
     same((2, 4, 2, D, 160, 160, 0, False, "", 0.0, False), {"documents": docs, "kv_lengths": lengths}, late_rows)
+
+
+def test_no_query_rows_leave_zero_gradients_of_keys():
+    for D in (64, 128):
+        c = (2, 4, 2, D, 0, 300, 0, True, "len", 0.0, False)
+        q, k, v, dout, m = _case(c)
+        out, lse, dq, dk, dv = _run(_attention(c), q, k, v, dout, m)
+        assert dk.shape == k.shape and not bool(dk.any()) and not bool(dv.any())

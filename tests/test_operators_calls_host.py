@@ -48,3 +48,13 @@ def test_attention_calls_do_not_share_a_descriptor(monkeypatch):
     a.backward(q, k, k, q, lse, wide, q, k, k, workspace=ws)
     assert (seen[0].q.token, seen[0].dout.token, seen[0].dq.token) == (320, 256, 320)
     assert (seen[1].q.token, seen[1].dout.token, seen[1].dq.token) == (256, 320, 256)
+
+
+def test_a_backward_of_nothing_is_no_error_whatever_the_heads():
+    """batch * kv_heads of 2^32 with no row and no key: nothing is divided by it."""
+    import ctypes
+    d = native.Attention(1 << 16, 1 << 16, 1 << 16, 8, 0, 0)._d
+    for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv"):
+        setattr(d, n, native.Strides(8, 8, 8))
+    assert native.lib().spectrain_attention_backward(ctypes.byref(d), None, *[None] * 9, None, 0, None) == native.OK
+    assert native.lib().spectrain_attention_forward(ctypes.byref(d), None, *[None] * 6, 0, None) == native.OK
