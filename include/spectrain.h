@@ -429,8 +429,9 @@ int spectrain_attention_backward(const spectrain_attention_desc* desc, const spe
  * survives), a value that is not finite becomes NaN, and nothing finite
  * becomes infinite: the largest code is the last one whose value is finite.
  * codes: uint8 [rows, cols]; scales: uint8 [rows, ceil(cols / 32)], both
- * contiguous; x and out: rows `ld` >= cols elements apart. rows *
- * ceil(cols / 32) and cols are below 2^30. */
+ * contiguous; x and out: rows `ld` >= cols elements apart. cols is below 2^30 and
+ * rows * ceil(cols / 32) at most 2^30 - 64. A restore takes what a pack wrote (scale
+ * bytes 10 .. 247). */
 int spectrain_checkpoint_pack(int32_t dtype, int64_t rows, int64_t cols, const void* x_dev, int64_t ld,
                               uint8_t* codes_dev, uint8_t* scales_dev, void* hip_stream);
 int spectrain_checkpoint_restore(int32_t dtype, int64_t rows, int64_t cols, const uint8_t* codes_dev,

@@ -292,8 +292,9 @@ void run_checkpoint(int dtype, int64_t rows, int64_t cols, const void* x, int64_
   if (rows < 0 || cols < 0) fail("rows and cols must be >= 0");
   if (ld < cols || ld > MAX_STRIDE) fail("ld must lie in [cols, 2^40]");
   if (rows == 0 || cols == 0) return;
-  if (cols >= 1 << 30 || rows >= 1 << 30 || rows * ((cols + 31) / 32) >= 1 << 30)
-    fail("cols and rows * ceil(cols / 32) must be below 2^30");
+  // grids of up to 2^32 - 1 threads, four to a group of values
+  if (cols >= 1 << 30 || rows >= 1 << 30 || rows * ((cols + 31) / 32) > (1 << 30) - 64)
+    fail("cols must be below 2^30 and rows * ceil(cols / 32) at most 2^30 - 64");
   if ((!x && !out) || !codes || !scales) fail("a tensor is NULL");
   if (!aligned(x, dtype == SPECTRAIN_BF16 ? 2 : 4) || !aligned(out, dtype == SPECTRAIN_BF16 ? 2 : 4))
     fail("a tensor is not aligned to its elements");

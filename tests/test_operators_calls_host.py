@@ -58,3 +58,13 @@ def test_a_backward_of_nothing_is_no_error_whatever_the_heads():
         setattr(d, n, native.Strides(8, 8, 8))
     assert native.lib().spectrain_attention_backward(ctypes.byref(d), None, *[None] * 9, None, 0, None) == native.OK
     assert native.lib().spectrain_attention_forward(ctypes.byref(d), None, *[None] * 6, 0, None) == native.OK
+
+
+P = 4096          # an aligned address that these calls never touch
+
+
+def test_checkpoint_refuses_what_a_grid_does_not_hold():
+    lib = native.lib()
+    for rows in ((1 << 30) - 1, (1 << 30) - 63):
+        assert lib.spectrain_checkpoint_pack(1, rows, 32, P, 32, P, P, None) == native.EINVAL
+        assert "2^30" in lib.spectrain_last_error().decode()
