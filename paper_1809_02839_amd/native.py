@@ -380,6 +380,11 @@ def _heads4(t, shape, dtype, device, what):
     return t.data_ptr()
 
 
+def _strides(t):
+    """The strides of a [batch, token, head, head_dim] tensor; of a single element any would do, and torch keeps odd ones."""
+    return Strides(*[0 if n == 1 else s for n, s in zip(t.shape[:3], t.stride())])
+
+
 def _side(t, shape, dtype, device, what):
     """Pointer of a contiguous side input (None: absent)."""
     if t is None:
@@ -421,7 +426,7 @@ class Rotary:
             d = RotaryDesc.from_buffer_copy(self._d)
             d.dtype = _dtype_code(x, "x")
             d.batch, d.tokens, d.heads = x.shape[:3]
-            d.x, d.out = Strides(*x.stride()[:3]), Strides(*out.stride()[:3])
+            d.x, d.out = _strides(x), _strides(out)
             d.first_position = first_position
             self._last = (layout, d)
         _on(x.device, stream, lib().spectrain_rotary, ctypes.byref(d), xp, pp, 1 if inverse else 0, op)
@@ -464,8 +469,8 @@ class Attention:
         last, d = self._last.get(pass_, (None, None))
         if strides != last:   # a new one: another thread's call may be reading the old
             d = AttentionDesc.from_buffer_copy(self._d)
-            for (name, _, _), st in zip(tensors, strides):
-                setattr(d, name, Strides(*st[:3]))
+            for name, t, _ in tensors:
+                setattr(d, name, _strides(t))
             self._last[pass_] = (strides, d)
         return ptr, d
 

@@ -50,6 +50,9 @@ def test_attention_calls_do_not_share_a_descriptor(monkeypatch):
     assert (seen[1].q.token, seen[1].dout.token, seen[1].dq.token) == (256, 320, 256)
 
 
+P = 4096          # an aligned address that these calls never touch
+
+
 def test_a_backward_of_nothing_is_no_error_whatever_the_heads():
     """batch * kv_heads of 2^32 with no row and no key: nothing is divided by it."""
     import ctypes
@@ -60,11 +63,26 @@ def test_a_backward_of_nothing_is_no_error_whatever_the_heads():
     assert native.lib().spectrain_attention_forward(ctypes.byref(d), None, *[None] * 6, 0, None) == native.OK
 
 
-P = 4096          # an aligned address that these calls never touch
-
-
 def test_checkpoint_refuses_what_a_grid_does_not_hold():
     lib = native.lib()
     for rows in ((1 << 30) - 1, (1 << 30) - 63):
         assert lib.spectrain_checkpoint_pack(1, rows, 32, P, 32, P, P, None) == native.EINVAL
         assert "2^30" in lib.spectrain_last_error().decode()
+
+
+def test_strides_of_single_elements_do_not_matter(monkeypatch):
+    """A dimension of size 1 may have any stride (torch keeps odd ones there)."""
+    calls = []
+
+    def on(device, stream, entry, *args):
+        calls.append(type(args[0]._obj).from_buffer_copy(args[0]._obj))
+
+    monkeypatch.setattr(native, "_on", on)
+    q = torch.zeros(2, 4, 64, 1, dtype=torch.bfloat16).permute(0, 3, 1, 2)     # strides 256, 1, 64, 1
+    assert q.shape == (2, 1, 4, 64) and q.stride(1) == 1
+    k = _heads(2, 3, 2, 64)
+    a = native.Attention(2, 4, 2, 64, 1, 3)
+    a.forward(q, k, k, torch.empty_like(q), workspace=torch.empty(256, dtype=torch.uint8))
+    native.Rotary(64).apply(q)
+    assert (calls[0].q.batch, calls[0].q.token, calls[0].q.head) == (256, 0, 64)
+    assert (calls[1].x.batch, calls[1].x.token, calls[1].x.head) == (256, 0, 64)
