@@ -33,7 +33,7 @@ def test_rotary_calls_do_not_share_a_descriptor(monkeypatch):
         r.apply(x, first_position=first)
         d = seen[-1]
         assert (d.batch, d.tokens, d.heads, d.first_position) == (*x.shape[:3], first)
-        assert (d.x.batch, d.x.token, d.x.head) == x.stride()[:3]
+        assert (d.x.token, d.x.head) == x.stride()[1:3]
 
 
 def test_attention_calls_do_not_share_a_descriptor(monkeypatch):
