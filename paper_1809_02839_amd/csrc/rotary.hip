@@ -64,7 +64,8 @@ __global__ __launch_bounds__(NT) void rotary_kernel(RotaryArgs a, int per_block,
   const int half = a.rot / 2, row0 = blockIdx.x * per_block, rows = min(per_block, a.rows - row0);
   for (int e = threadIdx.x; e < rows * half; e += NT) {
     const int t = e / half, i = e - t * half, row = row0 + t;
-    const int pos = a.positions ? a.positions[row] : a.first + row % a.tokens;
+    // a sum of two 32-bit numbers need not be one
+    const double pos = a.positions ? a.positions[row] : static_cast<double>(a.first) + row % a.tokens;
     double turn = pos * a.turns[i];
     turn -= rint(turn);
     float s, c;

@@ -8,7 +8,7 @@ but for capped scores, whose bound does not grow with the cap: tanh as
 """
 import pytest
 
-from test_gpu_operators import Reference, _attention, _case, _close, _run, _see
+from test_gpu_operators import Reference, _attention, _case, _close, _gen, _randn, _run, _see, _turned
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -145,3 +145,15 @@ def test_no_query_rows_leave_zero_gradients_of_keys():
         q, k, v, dout, m = _case(c)
         out, lse, dq, dk, dv = _run(_attention(c), q, k, v, dout, m)
         assert dk.shape == k.shape and not bool(dk.any()) and not bool(dv.any())
+
+
+def test_rotary_first_positions_up_to_the_last():
+    """first_position + token past 2^31 - 1 and below 0. A float64 angle of 2^31 radians is off by 2^-22 (the
+    position's, and the power's 2 x 2^-53 where it is largest), here and in the reference."""
+    from paper_1809_02839_amd import native
+    x = _randn((2, 40, 3, 64), _gen(21), torch.float32)
+    for first in ((1 << 31) - 5, -(1 << 31), 0):
+        pos = torch.arange(first, first + 40, device="cuda", dtype=torch.int64).expand(2, 40)
+        want, size = _turned(x, pos, 64, "half", 1e4, "none", 1.0, 0, False)
+        out = native.Rotary(64).apply(x, torch.empty_like(x), first_position=first)
+        assert bool(((out.double() - want).abs() <= (8e-7 + 4 * 2.0 ** -22) * size).all())
