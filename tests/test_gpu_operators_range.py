@@ -157,3 +157,48 @@ def test_rotary_first_positions_up_to_the_last():
         want, size = _turned(x, pos, 64, "half", 1e4, "none", 1.0, 0, False)
         out = native.Rotary(64).apply(x, torch.empty_like(x), first_position=first)
         assert bool(((out.double() - want).abs() <= (8e-7 + 4 * 2.0 ** -22) * size).all())
+
+
+@pytest.mark.parametrize("D", [40, 64, 128])
+@pytest.mark.parametrize("S,doc,cap,biased", [(2, 0, 0.0, False), (3, 0, 4.0, True), (16, 0, 0.0, False),
+                                              (100, 0, 0.0, True), (128, 0, 4.0, False), (1000, 16, 0.0, False),
+                                              (1000, 37, 4.0, True)])
+def test_gradients_of_few_keys_do_not_carry_the_rounding_of_out(S, doc, cap, biased, D):
+    """delta = sum of P dP in float32, not of the rounded out: dS = P (dP - delta) is off by float32 errors of its
+    terms and its own rounding, 2^-8 |dS|, and by nothing that is relative to out."""
+    BF, B, H, Hk = 2.0 ** -8, 3, 4, 2
+    c = (B, H, Hk, D, S, S, 0, True, "", cap, biased)
+    q, k, v, dout, m = _case(c)
+    see = torch.ones(S, S, dtype=torch.bool, device="cuda").tril()
+    if doc:
+        ids = (torch.arange(S, device="cuda") // doc).int()
+        m["documents"], see = ids.expand(B, S).contiguous(), see & (ids[:, None] == ids[None])
+    _, _, dq, dk, _ = _run(_attention(c), q, k, v, dout, m)
+    T, back = (lambda t: t.transpose(2, 3)), (lambda t: t.transpose(1, 2))
+    Q, dO = back(q.double()), back(dout.double())
+    K, V = (back(t.double()).repeat_interleave(H // Hk, 1) for t in (k, v))
+    scale = D ** -0.5
+    z = scale * Q @ T(K)
+    t = torch.tanh(z / cap) if cap else torch.zeros_like(z)
+    s = cap * t if cap else z
+    if biased:
+        i = torch.arange(S, device="cuda")
+        s = s - m["slopes"].double()[None, :, None, None] * (i[:, None] - i[None]).abs()
+    s = s.masked_fill(~see, -float("inf"))
+    P, one = torch.softmax(s, 3), 1 - t * t
+    sums = (D + 8) * 2.0 ** -24
+    Ez = sums * (scale * Q.abs() @ T(K.abs())).masked_fill(~see, 0.0).amax()
+    E = Ez + 2.0 ** -21 * (1 + s.masked_fill(~see, 0.0).abs().amax()) + 2.0 ** -22 * cap
+    dP = dO @ T(V)
+    delta, size = (P * dP).sum(3, keepdim=True), dO.abs() @ T(V.abs())
+    dP_tol = sums * size
+    delta_tol = (P * (dP_tol + (2 * E + 200 * 2.0 ** -24) * dP.abs())).sum(3, keepdim=True)   # up to 192 keys
+    slope_tol = 0.77 * Ez / cap + 2.0 ** -20 if cap else 0.0
+    dS = P * (dP - delta) * one
+    tol = P * (delta_tol + dP_tol) + (2 * E + slope_tol) * P * (dP - delta).abs()
+    tol = (tol + BF * dS.abs()) * (1 + 2 * BF) * scale
+    group = lambda x: back(x.reshape(B, Hk, H // Hk, S, D).sum(2))
+    want = {"dq": back(scale * dS @ K), "dk": group(scale * T(dS) @ Q)}
+    tols = {"dq": back(tol @ K.abs()), "dk": group(T(tol) @ Q.abs())}
+    for got, name in ((dq, "dq"), (dk, "dk")):
+        _close(got, want[name], tols[name] + BF * want[name].abs(), name)
