@@ -202,3 +202,32 @@ def test_gradients_of_few_keys_do_not_carry_the_rounding_of_out(S, doc, cap, bia
     tols = {"dq": back(tol @ K.abs()), "dk": group(T(tol) @ Q.abs())}
     for got, name in ((dq, "dq"), (dk, "dk")):
         _close(got, want[name], tols[name] + BF * want[name].abs(), name)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_gradients_with_offsets_past_32_bits(D):
+    """Every tensor of a forward and a backward with its last tokens beyond 2^32 elements."""
+    step, S, H, Hk = 1 << 20, 4200, 2, 1
+    c = (1, H, Hk, D, S, S, 0, True, "len", 0.0, False)
+    q, k, v, dout, m = _case(c)
+    store = torch.empty(step * S, dtype=torch.bfloat16, device="cuda")
+    place = iter(range(0, step, 1024))
+
+    def strided(t):
+        return store.as_strided(t.shape, (8, step, D, 1), next(place))
+
+    far = [strided(t) for t in (q, k, v, q, dout, q, k, v)]
+    for x, t in zip(far, (q, k, v, None, dout)):
+        if t is not None:
+            x.copy_(t)
+    qf, kf, vf, of, dof, *grads = far
+    a = _attention(c)
+    ws, lse = a.workspace(backward=True), torch.empty(1, H, S, device="cuda")
+    a.forward(qf, kf, vf, of, lse, workspace=ws, **m)
+    a.backward(qf, kf, vf, of, lse, dof, *grads, workspace=ws, **m)
+    # the bits of the same call on contiguous tensors, which are tested against the definition
+    for x, t in zip((of, lse, *grads), _run(a, q, k, v, dout, m)):
+        assert torch.equal(x, t)
+    r = Reference(q[:, -200:], k, v, D ** -0.5, 0.0, None, _see((1, H, Hk, D, 200, S, S - 200, True, "len", 0.0, False), m),
+                  S - 200)
+    _close(of[:, -200:], r.out, r.out_tol, "out")
