@@ -157,8 +157,9 @@ hipError_t attention_long_bwd(const bf16_t* qkv, const bf16_t* dctx, const float
 struct RotaryArgs {
   const void* x = nullptr;
   void* out = nullptr;
-  const int32_t* positions = nullptr;   // [rows], or NULL: first + row % tokens
-  int first = 0, tokens = 0, rows = 0, heads = 0, dim = 0, rot = 0;   // rows = batch * tokens
+  const int32_t* positions = nullptr;   // [rows], or NULL: row % tokens
+  double first = 0.0;                   // added to them
+  int tokens = 0, rows = 0, heads = 0, dim = 0, rot = 0;   // rows = batch * tokens
   long xb = 0, xt = 0, xh = 0, ob = 0, ot = 0, oh = 0;                // strides: sequence, token, head
   int interleaved = 0;
   float sign = 1.0f, magnitude = 1.0f;

@@ -72,7 +72,7 @@ void run_rotary(const spectrain_rotary_desc* desc, const void* x, const int32_t*
   a.x = x;
   a.out = out;
   a.positions = positions;
-  a.first = d.first_position;
+  a.first = positions ? 0 : d.first_position;
   a.tokens = d.tokens;
   a.rows = static_cast<int>(rows);
   a.heads = d.heads;

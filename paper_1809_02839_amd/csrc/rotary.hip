@@ -64,9 +64,8 @@ __global__ __launch_bounds__(NT) void rotary_kernel(RotaryArgs a, int per_block,
   const int half = a.rot / 2, row0 = blockIdx.x * per_block, rows = min(per_block, a.rows - row0);
   for (int e = threadIdx.x; e < rows * half; e += NT) {
     const int t = e / half, i = e - t * half, row = row0 + t;
-    // a sum of two 32-bit numbers need not be one
-    const double pos = a.positions ? a.positions[row] : static_cast<double>(a.first) + row % a.tokens;
-    double turn = pos * a.turns[i];
+    const int pos = a.positions ? a.positions[row] : row % a.tokens;
+    double turn = (pos + a.first) * a.turns[i];   // the sum may pass 32 bits
     turn -= rint(turn);
     float s, c;
     sincospif(2.0f * static_cast<float>(turn), &s, &c);
