@@ -372,16 +372,21 @@ int spectrain_rotary(const spectrain_rotary_desc* desc, const void* x_dev, const
  * reach rows and keys beside its own. Scores, softmax statistics and sums
  * are float32 (a cap moves a score by at most 2^-16 up to caps of 64, by 2^-21 of
  * itself past them); probabilities and score gradients are rounded to bf16 for their
- * products, results once to bf16. Results do not depend on timing: no atomics.
+ * products, results once to bf16. The backward sums P dP of a row in float32 where
+ * 128 rows see up to 192 keys between them, and takes it from the rounded out
+ * elsewhere. Results do not depend on timing: no atomics.
  *   documents   int32 [batch, kv_len]: a document is a run of equal numbers
  *               (needs 0 <= q_offset and q_offset + q_len <= kv_len)
  *   prefix, kv_lengths  int32 [batch], taken into [0, kv_len]
  *   slopes      float32 [heads]
  *   lse         float32 [batch, heads, q_len], contiguous
+ * The sequences of a call share q_offset. Caches of unlike lengths (kv_lengths)
+ * suit one new token a sequence, placed at or past the longest of them (slopes then
+ * shift lse only); several new tokens take a call for each length.
  * head_dim: a multiple of 8 up to 128; batch * heads * ceil(length / 32) below
- * 2^23 for both lengths. 64 tokens of k and v, and 64 / group + 1 tokens by
- * the heads of a group of q and dout, span at most 2^29 elements. Strides are multiples of 8 elements and
- * tensors 16-byte aligned. out may not overlap q, k, v; the gradients may not
+ * 2^23 for both lengths. 64 tokens of k and v, and 64 / group + 1 tokens by the
+ * heads of a group of q and dout, span at most 2^29 elements. Strides are multiples
+ * of 8 elements and tensors 16-byte aligned. out may not overlap q, k, v; the gradients may not
  * overlap each other or an input, but all of them may be parts of one packed
  * tensor. */
 typedef struct {

@@ -13,8 +13,10 @@
 // lane ends with scores of one row of its own: masks, maxima and sums of a row are
 // scalars of a lane, and the registers of a group of 32 columns are already an
 // operand of the next product (attention_long.hip). Probabilities and score
-// gradients are rounded to bf16 for it, 2^-8 of each at random, as the results are
-// once more; scores, maxima, sums and results stay float32.
+// gradients are rounded to bf16 for it, 2^-8 of each at most and at random, as the
+// results are once more: the matrix instructions take no wider operand at their rate,
+// and two roundings of one size make the error of out and the gradients 1.1 to 1.4
+// times that of a result rounded once. Scores, maxima, sums and results stay float32.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -515,10 +517,11 @@ __device__ __forceinline__ float lse_of(float m, float sum) { return sum == 0.0f
 
 // A block: 128 rows, or one piece of their keys; one pass over the keys. The
 // matrix instructions are busy 53% of the time at 128 columns (16 heads, 8192
-// causal tokens, 338 us, 814 TFLOP/s; 16384 tokens with two heads to a key head
-// 1045 us, 1050 TFLOP/s); the rest waits on the exponentials between the two
+// causal tokens, 311 us, 884 TFLOP/s; 16384 tokens with two heads to a key head
+// 1087 us, 1012 TFLOP/s); the rest waits on the exponentials between the two
 // products, four instructions' time each, which the other wave of a SIMD only
-// partly covers. At 64 columns they bound the kernel (905 TFLOP/s).
+// partly covers. At 64 columns they bound the kernel (32 heads, 8192 tokens, 306 us,
+// 900 TFLOP/s).
 template <int DH, int KIND>
 __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
   using T = Tile<DH>;
@@ -578,8 +581,8 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
 // Up to 32 rows (single tokens, and what a group makes of a few): bound by reading
 // the keys and values once, so the block's waves share out the keys, each with
 // tiles of 32 of its own that no other wave waits for, and join their sums at the
-// end. 1.6 GB of 16 ragged caches in 280 us, 5.7 TB/s, where a copy of 1 GiB moves
-// 5.1; 128 rows a block would keep one wave of four busy (1225 us).
+// end. 1.6 GB of 16 ragged caches in 286 us, 5.6 TB/s, where a copy of 1 GiB moves
+// 5.1; in blocks of 128 rows, one wave of four busy, 369 us.
 template <int DH, int KIND>
 __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
   using T = Tile<DH>;
@@ -826,7 +829,10 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   // by 0.0042 of their norm with 2 tokens, 0.0030 with 16, 0.0026 with 256. A walk of
   // few tiles is made twice, first for the sum of P dP: 0.0024 with any number. Two
   // tiles stay in their buffers meanwhile (a backward of 64 x 8 heads of 64 columns, 128
-  // tokens 31.3 -> 32.9 us, 256 tokens 66.9 -> 68.8).
+  // tokens 31.3 -> 32.9 us, 256 tokens 66.9 -> 68.8). Longer walks take the rounded
+  // out: 0.0025 where many keys have weight, 0.0028 where a bias leaves a row few of
+  // them; two walks there too would be 0.0024 for a fifth of the backward (6 x 1013
+  // tokens of 12 heads of 80, capped, biased: 164 -> 199 us).
   float delta = 0.0f;
   int buf = 0;
   const int walk = (end - begin + KT - 1) / KT;
@@ -888,10 +894,10 @@ struct RowInfo {
 
 // dK and dV of WAVES * 32 keys: the wave's own 32 are keys, the walked columns
 // rows (four products). At 128 columns the two results and the fragments of K and
-// V would fill the registers of two waves a SIMD (35 spilled, 2460 us for 16384
+// V would fill the registers of two waves a SIMD (30 spilled, 2469 us for 16384
 // causal tokens of 16 heads, two to a key head); eight waves, which share a staged
-// tile and leave LDS for it, keep V there instead (2195 us; with V in registers
-// 2399). Heads that share a key head are walked by one block, so their sum needs
+// tile and leave LDS for it, keep V there instead (2183 us; with V in registers
+// 2372). Heads that share a key head are walked by one block, so their sum needs
 // no atomics and has one order.
 template <int DH, int KIND, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_masked_dkv_kernel(Args a) {
@@ -1093,11 +1099,10 @@ size_t q_rows(const AttentionArgs& a) { return static_cast<size_t>(a.batch) * a.
 size_t k_rows(const AttentionArgs& a) { return static_cast<size_t>(a.batch) * a.kv_heads * a.kv_len; }
 
 // How the walks of a kernel's blocks are cut: up to `want` blocks fill the chip,
-// and fewer of a long walk leave CUs idle (6 x 1013 rows of 4 key heads, 192
-// blocks: dK and dV 278 us whole, 95 in up to five pieces). A piece has at least
-// `least` steps, so that a partial result's write and read stay small beside its
-// products. Two pieces for the long documents of a chip that is full as it is
-// measured nothing (2.39 ms of 2.40; 1.20 of 1.10).
+// and fewer of a long walk leave CUs idle (a backward of 8 heads of 4096 causal
+// tokens, 128 columns, 327 us whole and 215 in pieces; of 6 x 1013 tokens, 12 heads
+// of 80 on 4, 157 and 109). A piece has at least `least` steps, so that a partial
+// result's write and read stay small beside its products.
 struct Cut {
   int pieces = 1, quantum = 1;   // as in Args
 };
@@ -1119,18 +1124,23 @@ Plan plan(const AttentionArgs& a) {
   const long bh = static_cast<long>(a.batch) * a.kv_heads;
   const long row_tiles = (a.rows + ROWS - 1L) / ROWS;
   // Rows of one wave go to the kernel whose waves share out the keys: 4 rows of 16
-  // x 8 key heads over 32768 keys take 371 us there and 409 in tiles of 128 rows, 8
-  // rows of 32 x 8 over 2048 keys 24 and 33; 64 rows would read the keys twice (30
-  // and 23 over 8192). One block a CU: more gain nothing and have to be joined (4 x
-  // 8 heads of 8192 keys 30 us in 256 blocks, 34 in 512, 45 in 1024).
+  // x 8 key heads over 32768 keys take 371 us there and 377 in tiles of 128 rows, of
+  // 32 x 8 over 4096 keys (one head to a row) 95 and 106, 8 rows of 32 x 8 over 2048
+  // keys 45 and 49; 64 rows would read the keys twice (4 x 8 over 8192 39 us and 34).
+  // One block a CU: more gain little and have to be joined (4 x 8 heads of 8192 keys
+  // 30 us in 256 blocks, 35 in 512, 45 in 1024; 16 x 8 of 32768 371, 368, 367).
   p.few = a.rows <= 32;
   p.fwd = p.few ? cut(bh, (a.kv_len + 31L) / 32, 256, 8)
                 : cut(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8);   // two blocks a CU
   p.dq = cut(bh * row_tiles, (a.kv_len + KT - 1L) / KT, 512, 8);
-  // Eight waves, four: 64 x 1024 tokens and heads 130 us of a backward, 137; 64 x 8
-  // of 256 tokens 116, 121; 2 x 16 of 4096 481, 541. At 128 keys half of the eight
-  // have none: 62, 56.
+  // A backward with eight waves and with four: 4 x 16 heads of 1024 causal tokens 132
+  // us and 141, 64 x 8 of 256 117 and 119, 2 x 16 of 4096 485 and 527 (2 x 8 of 1024
+  // 72 and 68). At 128 keys half of the eight have none: 63 and 56.
   p.wide = a.dim > 96 && a.kv_len > 128;
+  // Two rounds of blocks (of four waves two fit a CU, of eight one) even out walks of
+  // unlike length: 12 heads of 4096 causal tokens, 192 blocks of eight, 264 us of a
+  // backward and in one round 340, 8 heads 215 and 223; but 16 heads of 2048, 128
+  // blocks, 148 and 136.
   const long step = a.group <= KT ? KT / a.group * a.group : KT;
   p.dkv = cut(bh * (p.wide ? (a.kv_len + 255L) / 256 : (a.kv_len + 127L) / 128), (a.rows + step - 1) / step,
               p.wide ? 512 : 1024, 8);
