@@ -581,7 +581,7 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_fwd_kernel(Args a) {
 // Up to 32 rows (single tokens, and what a group makes of a few): bound by reading
 // the keys and values once, so the block's waves share out the keys, each with
 // tiles of 32 of its own that no other wave waits for, and join their sums at the
-// end. 1.6 GB of 16 ragged caches in 286 us, 5.6 TB/s, where a copy of 1 GiB moves
+// end. 1.6 GB of 16 ragged caches in 290 us, 5.6 TB/s, where a copy of 1 GiB moves
 // 5.1; in blocks of 128 rows, one wave of four busy, 369 us.
 template <int DH, int KIND>
 __global__ __launch_bounds__(NT, 1) void attention_masked_few_kernel(Args a) {
@@ -752,7 +752,7 @@ __device__ __forceinline__ float log2_sum(const Args& a, long row) {
 
 // dQ of 128 rows (or a piece of it), and delta = out . dout (the sum of P dP) of each
 // for the other kernel. Scores and dP are formed again from the tiles (three products; matrix
-// instructions busy 61% at 128 columns): 1400 us for 16384 causal tokens of 16
+// instructions busy 62% at 128 columns): 1400 us for 16384 causal tokens of 16
 // heads, two to a key head.
 template <int DH, int KIND>
 __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
@@ -830,8 +830,8 @@ __global__ __launch_bounds__(NT, 2) void attention_masked_dq_kernel(Args a) {
   // few tiles is made twice, first for the sum of P dP: 0.0024 with any number. Two
   // tiles stay in their buffers meanwhile (a backward of 64 x 8 heads of 64 columns, 128
   // tokens 31.3 -> 32.9 us, 256 tokens 66.9 -> 68.8). Longer walks take the rounded
-  // out: 0.0025 where many keys have weight, 0.0028 where a bias leaves a row few of
-  // them; two walks there too would be 0.0024 for a fifth of the backward (6 x 1013
+  // out: 0.0024 to 0.0026 where many keys have weight, 0.0028 where a bias leaves few
+  // of them; two walks there too would be 0.0024 for a fifth of the backward (6 x 1013
   // tokens of 12 heads of 80, capped, biased: 164 -> 199 us).
   float delta = 0.0f;
   int buf = 0;
