@@ -1,0 +1,471 @@
+"""Performance cases of the operators around a linear layer in 8 bits: root-mean-square
+norm (with the residual's addition, an 8-bit output, its gradients), blocks of 128 (a
+tensor as e4m3 codes with one power-of-two scale for 128 values of a row or for a tile
+of 128 x 128, in either orientation), and the product of two such tensors.
+
+With `own` false a case runs in plain form, from elementary operations in 32 bits
+rounded once at the end; with `own` true it makes the library's calls.
+
+op:  norm      forward: sum of x and residual, its norm (kept in 8 bits where out is
+               e4m3, and restored)
+     training  norm forward and backward: sum, y, dx, dweight
+     pack      a tensor packed, in one or both orientations, and restored
+     product   out = A B^T of 8-bit A [m, k] and B [n, k], with bias and ReLU
+     linear    a training step of a linear layer: x, the weight and dy packed in both
+               orientations, y = x W^T, dx = dy W (zero where relu and x is), dW = dy^T x
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+BLOCK = 128           # values that share a scale
+EPS = 1e-6
+
+
+def _norm(name, op, rows, cols, dtype, out, residual):
+    return dict(name=name, op=op, rows=rows, cols=cols, dtype=dtype, out=out, residual=residual)
+
+
+def _pack(name, rows, cols, dtype, tiles, sides):
+    return dict(name=name, op="pack", rows=rows, cols=cols, dtype=dtype, tiles=tiles, sides=sides)
+
+
+def _product(name, m, n, k, out, a_tiles=False, b_tiles=True, bias=False, relu=False):
+    return dict(name=name, op="product", m=m, n=n, k=k, out=out, a_tiles=a_tiles, b_tiles=b_tiles, bias=bias, relu=relu)
+
+
+def _linear(name, tokens, cols, rows, relu):
+    return dict(name=name, op="linear", tokens=tokens, cols=cols, rows=rows, relu=relu)
+
+
+def listed():
+    return [
+        # one new token of a few sequences: latency
+        _norm("norm_token", "norm", 3, 512, "bf16", "bf16", True),
+        # the benchmark's encoder stage: what its linear layers in 8 bits read
+        _norm("norm_stage", "norm", 8192, 512, "bf16", "e4m3", True),
+        # odd rows and columns, a float32 residual stream with a bf16 layer behind it
+        _norm("norm_train_odd", "training", 1013, 1531, "fp32", "bf16", True),
+        # a long sequence of a wide layer
+        _norm("norm_train_long", "training", 16384, 8192, "bf16", "bf16", True),
+        # predicted weights of the benchmark's encoder stage, for a product and its data gradient
+        _pack("pack_weight", 2048, 512, "fp32", True, "both"),
+        # activations of a wide layer, odd row count, for a product and its weight gradient
+        _pack("pack_tokens", 50001, 8184, "bf16", False, "both"),
+        # one new token of a few sequences through a small layer: latency
+        _product("product_token", 3, 2048, 512, "bf16"),
+        # one new token of sixteen sequences through a wide layer: bound by reading the weight
+        _product("product_decode", 16, 16384, 8192, "bf16"),
+        # a prompt chunk, nothing a multiple of anything, float32 result
+        _product("product_odd", 1013, 1531, 777, "fp32", bias=True),
+        # a large product: bound by the matrix instructions
+        _product("product_large", 8192, 8192, 8192, "bf16", bias=True, relu=True),
+        # second layer of the benchmark's feed-forward network, behind a ReLU
+        _linear("linear_stage", 8192, 2048, 512, True),
+        # a long sequence through a wide layer
+        _linear("linear_long", 16384, 4096, 8192, False),
+    ]
+
+
+def _spread(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _width(rng, lo, hi, multiple, share):
+    n = _spread(rng, lo, hi)
+    return -(-n // multiple) * multiple if rng.random() < share else n
+
+
+def draw(rng):
+    op = rng.choice(("norm", "training", "pack", "product", "product", "linear"))
+    if op in ("norm", "training"):
+        cols = _width(rng, 33, 16384, 8, 0.7)
+        rows = min(_spread(rng, 1, 60000), 16384 * 8192 // cols)
+        dtype = rng.choice(("bf16", "bf16", "fp32"))
+        out = rng.choice(("bf16", "bf16", dtype) + (("e4m3", "e4m3") if op == "norm" else ()))
+        return _norm(None, op, rows, cols, dtype, out, rng.random() < 0.7)
+    if op == "pack":
+        cols = _width(rng, 33, 16384, 8, 0.7)
+        rows = min(_spread(rng, 1, 60000), 50001 * 8184 // cols)
+        return _pack(None, rows, cols, rng.choice(("bf16", "bf16", "fp32")), rng.random() < 0.5,
+                     rng.choice(("rows", "columns", "both")))
+    if op == "product":
+        m = rng.choice((rng.randint(1, 33), _spread(rng, 1, 16384), _spread(rng, 33, 16384)))
+        n, k = _width(rng, 33, 16384, 16, 0.7), _width(rng, 33, 16384, 16, 0.7)
+        while float(m) * n * k > 8192.0 ** 3:
+            m = (m + 1) // 2
+        return _product(None, m, n, k, rng.choice(("bf16", "bf16", "fp32")), a_tiles=rng.random() < 0.2,
+                        b_tiles=rng.random() < 0.7, bias=rng.random() < 0.5, relu=rng.random() < 0.3)
+    tokens, cols, rows = _width(rng, 17, 16384, 16, 0.6), _width(rng, 64, 8192, 16, 0.8), _width(rng, 64, 8192, 16, 0.8)
+    while float(tokens) * cols * rows > 16384.0 * 4096 * 8192:
+        tokens = (tokens + 1) // 2
+    return _linear(None, tokens, cols, rows, rng.random() < 0.5)
+
+
+# ------------------------------------------------------------------ inputs ----
+def _dtype(name):
+    return torch.float32 if name == "fp32" else torch.bfloat16
+
+
+def _randn(g, *shape):
+    return torch.randn(*shape, generator=g, device=DEV)
+
+
+def _tokens(g, rows, cols):
+    """Activations: rows of unlike size, a few columns that stand out."""
+    x = _randn(g, rows, cols)
+    x.mul_(torch.exp(0.5 * _randn(g, rows, 1)))
+    return x.mul_(torch.where(torch.rand(1, cols, generator=g, device=DEV) < 0.01, 20.0, 1.0))
+
+
+def _exponents(top):
+    """Smallest e, -117 to 120, with top / 2^e <= 448 = 0.875 * 2^9."""
+    mantissa, exponent = torch.frexp(top)
+    return torch.where(mantissa <= 0.875, exponent - 9, exponent - 8).clamp(-117, 120)
+
+
+def _power(e):
+    """2^e of whole -126 <= e <= 127, exactly (a GPU's exp2 and pow are off by a step for some)."""
+    return ((e + 127).to(torch.int32) << 23).view(torch.float32)
+
+
+def _blocks(x, tiles):
+    """Float x [rows, cols] as [block rows, rows of one, block columns, 128], zeros behind its edges."""
+    R, C = x.shape
+    high = BLOCK if tiles else 1
+    return torch.nn.functional.pad(x, (0, -C % BLOCK, 0, -R % high)).reshape(-(-R // high), high, -(-C // BLOCK), BLOCK)
+
+
+def _encode(x, tiles):
+    """e4m3 values of every block, and their exponents [block rows, 1, block columns, 1]."""
+    y = _blocks(x, tiles)
+    e = _exponents(y.abs().amax((1, 3), keepdim=True))
+    return (y * _power(-e)).to(torch.float8_e4m3fn), e
+
+
+def _rounded(x, tiles):
+    """The float values that x is held as."""
+    f, e = _encode(x, tiles)
+    return (f.float() * _power(e)).flatten(2).flatten(0, 1)[:x.shape[0], :x.shape[1]].contiguous()
+
+
+def _coded(x, tiles):
+    """Codes uint8 [rows, cols], rows of a multiple of 16 bytes, and scale bytes."""
+    f, e = _encode(x, tiles)
+    R, C = x.shape
+    codes = torch.zeros(R, -(-C // 16) * 16, dtype=torch.uint8, device=x.device)[:, :C]
+    codes.copy_(f.view(torch.uint8).flatten(2).flatten(0, 1)[:R, :C])
+    return codes, (e[:, 0, :, 0] + 127).to(torch.uint8)
+
+
+def _norm_state(c, g):
+    R, C = c["rows"], c["cols"]
+    t = _dtype(c["dtype"])
+    st = {"x": _tokens(g, R, C).to(t), "weight": (1.0 + 0.2 * _randn(g, C)), "residual": None}
+    if c["residual"]:
+        st["residual"] = _randn(g, R, C).to(t)
+    y = _dtype(c["out"])
+    if c["op"] == "training":
+        st["dy"] = _randn(g, R, C).to(y)
+        st["dsum"] = _randn(g, R, C).to(t) if c["residual"] else None
+    if own:
+        from paper_1809_02839_amd import native
+        st["native"] = native
+        st["norm"] = native.RmsNorm(C, eps=EPS)
+        st["sum"] = torch.empty_like(st["x"]) if c["residual"] else None
+        st["out"] = torch.empty(R, C, dtype=y, device=DEV)
+        st["rstd"] = torch.empty(R, dtype=torch.float32, device=DEV)
+        if c["out"] == "e4m3":
+            st["codes"], st["scales"] = native.blocks_empty(R, C, device=DEV)
+        if c["op"] == "training":
+            st["dx"] = torch.empty_like(st["x"])
+            st["dweight"] = torch.empty(C, dtype=torch.float32, device=DEV)
+            st["workspace"] = st["norm"].workspace(R)
+    return st
+
+
+def _pack_state(c, g):
+    R, C = c["rows"], c["cols"]
+    st = {"x": _tokens(g, R, C).to(_dtype(c["dtype"]))}
+    if own:
+        from paper_1809_02839_amd import native
+        st["native"] = native
+        for side, shape in (("rows", (R, C)), ("columns", (C, R))):
+            if c["sides"] in (side, "both"):
+                st[side] = native.blocks_empty(*shape, tiles=c["tiles"], device=DEV)
+                st["out_" + side] = torch.empty(shape, dtype=torch.bfloat16, device=DEV)
+    return st
+
+
+def _product_state(c, g):
+    m, n, k = c["m"], c["n"], c["k"]
+    st = {"a": _coded(_tokens(g, m, k), c["a_tiles"]), "b": _coded(_randn(g, n, k).mul_(k ** -0.5), c["b_tiles"]),
+          "bias": 0.3 * _randn(g, n) if c["bias"] else None}
+    if own:
+        from paper_1809_02839_amd import native
+        st["product"] = p = native.Product(m, n, k, a_tiles=c["a_tiles"], b_tiles=c["b_tiles"], relu=c["relu"])
+        st["out"] = torch.empty(m, n, dtype=_dtype(c["out"]), device=DEV)
+        st["workspace"] = p.workspace()
+    return st
+
+
+def _linear_state(c, g):
+    T, K, N = c["tokens"], c["cols"], c["rows"]
+    bf = torch.bfloat16
+    x = _tokens(g, T, K)
+    st = {"x": (x.relu_() if c["relu"] else x).to(bf), "weight": _randn(g, N, K).mul_(K ** -0.5),
+          "dy": _tokens(g, T, N).mul_(1e-3).to(bf)}
+    if own:
+        from paper_1809_02839_amd import native
+        st["native"] = native
+        empty = native.blocks_empty
+        st["x8"], st["xt8"] = empty(T, K, device=DEV), empty(K, T, device=DEV)
+        st["w8"], st["wt8"] = empty(N, K, tiles=True, device=DEV), empty(K, N, tiles=True, device=DEV)
+        st["dy8"], st["dyt8"] = empty(T, N, device=DEV), empty(N, T, device=DEV)
+        st["forward"] = native.Product(T, N, K, b_tiles=True)
+        st["data"] = native.Product(T, K, N, b_tiles=True)
+        st["gradient"] = native.Product(N, K, T)
+        st["workspace"] = max((st[n].workspace() for n in ("forward", "data", "gradient")), key=lambda w: w.numel())
+        st["y"] = torch.empty(T, N, dtype=bf, device=DEV)
+        st["dx"] = torch.empty(T, K, dtype=bf, device=DEV)
+        st["dw"] = torch.empty(N, K, dtype=torch.float32, device=DEV)
+    return st
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    make = {"norm": _norm_state, "training": _norm_state, "pack": _pack_state, "product": _product_state,
+            "linear": _linear_state}[case["op"]]
+    st = make(case, g)
+    st["case"] = case
+    return st
+
+
+# -------------------------------------------------------------- plain forms ----
+def _plain_norm(st):
+    c, x = st["case"], st["x"]
+    h = x.float()
+    if st["residual"] is not None:
+        h = (h + st["residual"].float()).to(x.dtype).float()       # the stored sum is what is normed
+    r = torch.rsqrt((h * h).mean(1, keepdim=True) + EPS)
+    w = st["weight"]
+    y = h * r * w
+    held = _rounded(y, False).to(torch.bfloat16) if c["out"] == "e4m3" else y.to(_dtype(c["out"]))
+    out = [held] if st["residual"] is None else [h.to(x.dtype), held]
+    if c["op"] == "norm":
+        return out
+    d = st["dy"].float()
+    z = h * r
+    u = d * w
+    dx = r * (u - z * (u * z).mean(1, keepdim=True))
+    if st["dsum"] is not None:
+        dx = dx + st["dsum"].float()
+    return out + [dx.to(x.dtype), (d * z).sum(0)]
+
+
+def _plain_pack(st):
+    c, x = st["case"], st["x"].float()
+    out = []
+    if c["sides"] != "columns":
+        out.append(_rounded(x, c["tiles"]).to(torch.bfloat16))
+    if c["sides"] != "rows":
+        out.append(_rounded(x.t().contiguous(), c["tiles"]).to(torch.bfloat16))
+    return out
+
+
+def _decoded(codes, scales, tiles):
+    e = scales.to(torch.int32) - 127
+    e = e.repeat_interleave(BLOCK, 1)[:, :codes.shape[1]]
+    if tiles:
+        e = e.repeat_interleave(BLOCK, 0)[:codes.shape[0]]
+    return codes.contiguous().view(torch.float8_e4m3fn).float() * _power(e)
+
+
+def _plain_product(st):
+    c = st["case"]
+    y = torch.matmul(_decoded(*st["a"], c["a_tiles"]), _decoded(*st["b"], c["b_tiles"]).t())
+    if st["bias"] is not None:
+        y = y + st["bias"]
+    if c["relu"]:
+        y = y.clamp(min=0.0)
+    return y.to(_dtype(c["out"]))
+
+
+def _plain_linear(st):
+    x, w, dy = st["x"].float(), st["weight"], st["dy"].float()
+    w8 = _rounded(w, True)
+    y = torch.matmul(_rounded(x, False), w8.t())
+    dx = torch.matmul(_rounded(dy, False), w8)
+    if st["case"]["relu"]:
+        dx = torch.where(x > 0, dx, torch.zeros_like(dx))
+    dw = torch.matmul(_rounded(dy.t().contiguous(), False), _rounded(x.t().contiguous(), False).t())
+    return y.to(torch.bfloat16), dx.to(torch.bfloat16), dw
+
+
+# ------------------------------------------------------------ library calls ----
+def _own_norm(st):
+    c = st["case"]
+    norm, h = st["norm"], st["x"] if st["sum"] is None else st["sum"]
+    if c["out"] == "e4m3":
+        norm.forward(st["x"], st["weight"], residual=st["residual"], sum=st["sum"], codes=st["codes"], scales=st["scales"])
+        st["native"].blocks_restore(st["codes"], st["scales"], st["out"])
+    else:
+        norm.forward(st["x"], st["weight"], st["out"], residual=st["residual"], sum=st["sum"],
+                     rstd=st["rstd"] if c["op"] == "training" else None)
+    out = [st["out"]] if st["sum"] is None else [st["sum"], st["out"]]
+    if c["op"] == "norm":
+        return out
+    norm.backward(st["dy"], h, st["weight"], st["rstd"], st["dx"], st["dweight"], dsum=st["dsum"],
+                  workspace=st["workspace"])
+    return out + [st["dx"], st["dweight"]]
+
+
+def _own_pack(st):
+    c, native = st["case"], st["native"]
+    rows, columns = st.get("rows", (None, None)), st.get("columns", (None, None))
+    native.blocks_pack(st["x"], *rows, *columns, tiles=c["tiles"])
+    out = []
+    for side in ("rows", "columns"):
+        if side in st:
+            native.blocks_restore(*st[side], st["out_" + side], tiles=c["tiles"])
+            out.append(st["out_" + side])
+    return out
+
+
+def _own_product(st):
+    st["product"].apply(*st["a"], *st["b"], st["out"], bias=st["bias"], workspace=st["workspace"])
+    return st["out"]
+
+
+def _own_linear(st):
+    pack, ws = st["native"].blocks_pack, st["workspace"]
+    pack(st["x"], *st["x8"], *st["xt8"])
+    pack(st["weight"], *st["w8"], *st["wt8"], tiles=True)
+    pack(st["dy"], *st["dy8"], *st["dyt8"])
+    st["forward"].apply(*st["x8"], *st["w8"], st["y"], workspace=ws)
+    st["data"].apply(*st["dy8"], *st["wt8"], st["dx"], mask=st["x"] if st["case"]["relu"] else None, workspace=ws)
+    st["gradient"].apply(*st["dyt8"], *st["xt8"], st["dw"], workspace=ws)
+    return st["y"], st["dx"], st["dw"]
+
+
+def run(state):
+    op = state["case"]["op"]
+    if own:
+        return {"pack": _own_pack, "product": _own_product, "linear": _own_linear}.get(op, _own_norm)(state)
+    return {"pack": _plain_pack, "product": _plain_product, "linear": _plain_linear}.get(op, _plain_norm)(state)
+
+
+# --------------------------------------------------------------------- work ----
+def work(case):
+    c = case
+    if c["op"] in ("norm", "training"):
+        n, s, o = c["rows"] * c["cols"], 4 if c["dtype"] == "fp32" else 2, 4 if c["out"] == "fp32" else 2
+        size = n * s * (3 if c["residual"] else 1) + 4 * c["cols"]
+        flops = 6.0 * n
+        if c["out"] == "e4m3":
+            size += n * (1 + 1 + 2) + 2 * c["rows"] * -(-c["cols"] // BLOCK)     # written, read, restored
+        else:
+            size += n * o
+        if c["op"] == "training":     # dy, the sum, the sum's gradient; dx, dweight
+            size += n * (o + s * (3 if c["residual"] else 2)) + 8 * c["rows"] + 8 * c["cols"]
+            flops += 12.0 * n
+        return {"bytes": size, "flops": flops}
+    if c["op"] == "pack":
+        n, s = c["rows"] * c["cols"], 4 if c["dtype"] == "fp32" else 2
+        return {"bytes": n * (s + (2 if c["sides"] == "both" else 1) * (1 + 1 + 2)), "flops": 6.0 * n}
+    if c["op"] == "product":
+        m, n, k = c["m"], c["n"], c["k"]
+        return {"bytes": k * (m + n) + m * n * (4 if c["out"] == "fp32" else 2) + (4 * n if c["bias"] else 0),
+                "flops": 2.0 * m * n * k}
+    T, K, N = c["tokens"], c["cols"], c["rows"]
+    # bf16 x and dy, the float32 weight; both orientations of all three written and read; y, dx, dW
+    return {"bytes": 2 * T * (K + N) + 4 * N * K + 4 * (T * K + T * N + N * K) + 2 * T * (N + K) + 4 * N * K
+            + (2 * T * K if c["relu"] else 0), "flops": 6.0 * T * K * N}
+
+
+# -------------------------------------------------------------------- exact ----
+def _two(e):
+    """2^e of whole -300 <= e <= 300, from a table."""
+    return torch.tensor([2.0 ** i for i in range(-300, 301)], dtype=torch.float64, device=DEV)[e.long() + 300]
+
+
+def _nearest(x, tiles):
+    """64-bit x by the nearest e4m3 value of each block's scale, found by the step at each value's size."""
+    R, C = x.shape
+    out = torch.empty_like(x)
+    high = BLOCK if tiles else min(R, 8192)
+    for r in range(0, R, high):
+        for j in range(0, C, BLOCK):
+            y = x[r:r + high, j:j + BLOCK]
+            top = y.abs().amax().reshape(1, 1) if tiles else y.abs().amax(1, keepdim=True)
+            e = torch.ceil(torch.log2(top / 448.0)).clamp(-117, 120)
+            e = (e + (top > 448.0 * _two(e)).double() - (top <= 224.0 * _two(e)).double()).clamp(-117, 120)
+            z = y * _two(-e)
+            step = _two(torch.frexp(z.abs().clamp(min=2.0 ** -6))[1] - 4)
+            out[r:r + high, j:j + BLOCK] = torch.round(z / step).mul_(step) * _two(e)
+    return out
+
+
+def _table():
+    """The value of every e4m3 code, from its bits."""
+    code = torch.arange(256, device=DEV)
+    power, part = (code >> 3) & 15, (code & 7).double() / 8.0
+    size = torch.where(power == 0, part * 2.0 ** -6, (1.0 + part) * _two(power - 7))
+    return torch.where(code >= 128, -size, size)
+
+
+def _held(codes, scales, tiles):
+    R, C = codes.shape
+    row = torch.arange(R, device=DEV) // (BLOCK if tiles else 1)
+    power = _two(scales.long() - 127)
+    return _table()[codes.long()] * power[row][:, torch.arange(C, device=DEV) // BLOCK]
+
+
+def _exact_norm(st):
+    c = st["case"]
+    x = st["x"].double()
+    if st["residual"] is not None:
+        x = x + st["residual"].double()
+    h = x.to(st["x"].dtype).double()
+    train = c["op"] == "training"
+    if train and h.numel() > 1 << 27:
+        return None
+    w = st["weight"].double()
+    outs = [] if st["residual"] is None else [x]
+    if not train:
+        y = h / torch.sqrt(h.square().sum(1, keepdim=True) / h.shape[1] + EPS) * w
+        return outs + [_nearest(y, False) if c["out"] == "e4m3" else y]
+    h.requires_grad_(True)
+    w.requires_grad_(True)
+    y = h / torch.sqrt(h.square().sum(1, keepdim=True) / h.shape[1] + EPS) * w
+    dh, dw = torch.autograd.grad(y, (h, w), st["dy"].double())
+    if st["dsum"] is not None:
+        dh = dh + st["dsum"].double()
+    return outs + [y.detach(), dh, dw]
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    if case["op"] in ("norm", "training"):
+        return _exact_norm(st)
+    if case["op"] == "pack":
+        x, c = st["x"].double(), case
+        if c["tiles"] and -(-c["rows"] // BLOCK) * -(-c["cols"] // BLOCK) > 12000:
+            return None
+        sides = {"rows": (x,), "columns": (x.t(),), "both": (x, x.t())}[c["sides"]]
+        return [_nearest(s, c["tiles"]) for s in sides]
+    if case["op"] == "product":
+        y = torch.mm(_held(*st["a"], case["a_tiles"]), _held(*st["b"], case["b_tiles"]).t().contiguous())
+        if case["bias"]:
+            y += st["bias"].double()
+        return torch.relu(y) if case["relu"] else y
+    x, w, dy = st["x"].double(), st["weight"].double(), st["dy"].double()
+    w = _nearest(w, True)
+    y = torch.mm(_nearest(x, False), w.t().contiguous())
+    dx = torch.mm(_nearest(dy, False), w)
+    if case["relu"]:
+        dx = dx * (x > 0)
+    return y, dx, torch.mm(_nearest(dy.t().contiguous(), False), _nearest(x.t().contiguous(), False).t().contiguous())
