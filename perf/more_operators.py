@@ -153,12 +153,15 @@ def _rounded(x, tiles):
 
 
 def _coded(x, tiles):
-    """Codes uint8 [rows, cols], rows of a multiple of 16 bytes, and scale bytes."""
+    """Codes uint8 [rows, cols] and scale bytes [block columns, rows] (a tile's for each of its rows), lines of a
+    multiple of 16 bytes."""
     f, e = _encode(x, tiles)
     R, C = x.shape
     codes = torch.zeros(R, -(-C // 16) * 16, dtype=torch.uint8, device=x.device)[:, :C]
     codes.copy_(f.view(torch.uint8).flatten(2).flatten(0, 1)[:R, :C])
-    return codes, (e[:, 0, :, 0] + 127).to(torch.uint8)
+    scales = torch.zeros(e.shape[2], -(-R // 16) * 16, dtype=torch.uint8, device=x.device)[:, :R]
+    scales.copy_((e[:, 0, :, 0] + 127).repeat_interleave(f.shape[1], 0)[:R].t())
+    return codes, scales
 
 
 def _norm_state(c, g):
@@ -195,7 +198,7 @@ def _pack_state(c, g):
         st["native"] = native
         for side, shape in (("rows", (R, C)), ("columns", (C, R))):
             if c["sides"] in (side, "both"):
-                st[side] = native.blocks_empty(*shape, tiles=c["tiles"], device=DEV)
+                st[side] = native.blocks_empty(*shape, device=DEV)
                 st["out_" + side] = torch.empty(shape, dtype=torch.bfloat16, device=DEV)
     return st
 
@@ -206,7 +209,7 @@ def _product_state(c, g):
           "bias": 0.3 * _randn(g, n) if c["bias"] else None}
     if own:
         from paper_1809_02839_amd import native
-        st["product"] = p = native.Product(m, n, k, a_tiles=c["a_tiles"], b_tiles=c["b_tiles"], relu=c["relu"])
+        st["product"] = p = native.Product(m, n, k, relu=c["relu"])
         st["out"] = torch.empty(m, n, dtype=_dtype(c["out"]), device=DEV)
         st["workspace"] = p.workspace()
     return st
@@ -223,10 +226,10 @@ def _linear_state(c, g):
         st["native"] = native
         empty = native.blocks_empty
         st["x8"], st["xt8"] = empty(T, K, device=DEV), empty(K, T, device=DEV)
-        st["w8"], st["wt8"] = empty(N, K, tiles=True, device=DEV), empty(K, N, tiles=True, device=DEV)
+        st["w8"], st["wt8"] = empty(N, K, device=DEV), empty(K, N, device=DEV)
         st["dy8"], st["dyt8"] = empty(T, N, device=DEV), empty(N, T, device=DEV)
-        st["forward"] = native.Product(T, N, K, b_tiles=True)
-        st["data"] = native.Product(T, K, N, b_tiles=True)
+        st["forward"] = native.Product(T, N, K)
+        st["data"] = native.Product(T, K, N)
         st["gradient"] = native.Product(N, K, T)
         st["workspace"] = max((st[n].workspace() for n in ("forward", "data", "gradient")), key=lambda w: w.numel())
         st["y"] = torch.empty(T, N, dtype=bf, device=DEV)
@@ -276,17 +279,14 @@ def _plain_pack(st):
     return out
 
 
-def _decoded(codes, scales, tiles):
-    e = scales.to(torch.int32) - 127
-    e = e.repeat_interleave(BLOCK, 1)[:, :codes.shape[1]]
-    if tiles:
-        e = e.repeat_interleave(BLOCK, 0)[:codes.shape[0]]
+def _decoded(codes, scales):
+    e = (scales.to(torch.int32) - 127).t().repeat_interleave(BLOCK, 1)[:, :codes.shape[1]]
     return codes.contiguous().view(torch.float8_e4m3fn).float() * _power(e)
 
 
 def _plain_product(st):
     c = st["case"]
-    y = torch.matmul(_decoded(*st["a"], c["a_tiles"]), _decoded(*st["b"], c["b_tiles"]).t())
+    y = torch.matmul(_decoded(*st["a"]), _decoded(*st["b"]).t())
     if st["bias"] is not None:
         y = y + st["bias"]
     if c["relu"]:
@@ -330,7 +330,7 @@ def _own_pack(st):
     out = []
     for side in ("rows", "columns"):
         if side in st:
-            native.blocks_restore(*st[side], st["out_" + side], tiles=c["tiles"])
+            native.blocks_restore(*st[side], st["out_" + side])
             out.append(st["out_" + side])
     return out
 
@@ -417,11 +417,9 @@ def _table():
     return torch.where(code >= 128, -size, size)
 
 
-def _held(codes, scales, tiles):
-    R, C = codes.shape
-    row = torch.arange(R, device=DEV) // (BLOCK if tiles else 1)
-    power = _two(scales.long() - 127)
-    return _table()[codes.long()] * power[row][:, torch.arange(C, device=DEV) // BLOCK]
+def _held(codes, scales):
+    column = torch.arange(codes.shape[1], device=DEV) // BLOCK
+    return _table()[codes.long()] * _two(scales.long() - 127)[column].t()
 
 
 def _exact_norm(st):
@@ -458,7 +456,7 @@ def exact(case, seed):
         sides = {"rows": (x,), "columns": (x.t(),), "both": (x, x.t())}[c["sides"]]
         return [_nearest(s, c["tiles"]) for s in sides]
     if case["op"] == "product":
-        y = torch.mm(_held(*st["a"], case["a_tiles"]), _held(*st["b"], case["b_tiles"]).t().contiguous())
+        y = torch.mm(_held(*st["a"]).contiguous(), _held(*st["b"]).t().contiguous())
         if case["bias"]:
             y += st["bias"].double()
         return torch.relu(y) if case["relu"] else y
