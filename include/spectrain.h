@@ -442,6 +442,117 @@ int spectrain_checkpoint_pack(int32_t dtype, int64_t rows, int64_t cols, const v
 int spectrain_checkpoint_restore(int32_t dtype, int64_t rows, int64_t cols, const uint8_t* codes_dev,
                                  const uint8_t* scales_dev, void* out_dev, int64_t ld, void* hip_stream);
 
+/* ---- Linear layers in 8 bits ----
+ *
+ * A tensor [rows, cols] in blocks: e4m3 codes and, for 128 consecutive columns
+ * (the last block of a row may be shorter), the scale 2^(byte - 127). The layout
+ * of the three calls below:
+ *   codes   uint8 [rows, cols], rows codes_ld bytes apart
+ *   scales  uint8 [ceil(cols / 128), rows], lines scales_ld bytes apart: one byte
+ *           for each row and block of columns
+ * Both start at a multiple of 16 bytes and their ld are multiples of 16, codes_ld
+ * at most 2^22; a line's bytes up to the next multiple of 16 belong to it (they
+ * are read by the product, whatever they hold, and never written). Lines of a
+ * larger tensor may be given alone (a view). Alignment, errors, streams and
+ * tensors with a dimension of 0 are as for the operators above. */
+
+/* Which values share a scale: 128 of a row, or a tile of 128 rows by 128 columns
+ * (counted from the first; its byte is then written for each of its rows). */
+typedef enum { SPECTRAIN_BLOCKS_ROWS = 0, SPECTRAIN_BLOCKS_TILES = 1 } spectrain_blocks_shape;
+
+/* Pack x into blocks, transposed x (blocks of 128 consecutive rows of x), or both
+ * in one pass; codes or transposed may be NULL (its scales then too). The scale is
+ * the smallest power of two, at least 2^-117, with max |x| / scale <= 448; a value
+ * is kept as the nearest e4m3 number of x / scale, ties to even (a small one may
+ * become 0). A value that is not finite becomes NaN and is no part of the scale,
+ * and nothing finite becomes infinite: in blocks whose largest value is past
+ * 448 * 2^119 a code stays at most 240. TILES: codes and transposed hold the same
+ * numbers. */
+typedef struct {
+  uint32_t abi_version;      /* SPECTRAIN_ABI_VERSION */
+  int32_t dtype;             /* spectrain_dtype of x, or of a restore's out */
+  int32_t shape;             /* spectrain_blocks_shape; a restore does not look at it */
+  int32_t reserved;          /* 0 */
+  int64_t rows, cols;        /* below 2^31; ceil(rows / 128) * ceil(cols / 128) at most 2^23 */
+  int64_t ld;                /* elements between rows of x or out: >= cols, at most 2^40 */
+  int64_t codes_ld, scales_ld;             /* >= cols, >= rows */
+  int64_t transposed_ld, transposed_scales_ld;   /* >= rows, >= cols; looked at where transposed is given */
+} spectrain_blocks_desc;
+
+int spectrain_blocks_pack(const spectrain_blocks_desc* desc, const void* x_dev, uint8_t* codes_dev,
+                          uint8_t* scales_dev, uint8_t* transposed_dev, uint8_t* transposed_scales_dev,
+                          void* hip_stream);
+
+/* The values that codes and scales (bytes 10 .. 247) stand for. */
+int spectrain_blocks_restore(const spectrain_blocks_desc* desc, const uint8_t* codes_dev, const uint8_t* scales_dev,
+                             void* out_dev, void* hip_stream);
+
+/* Root-mean-square norm of rows, with the addition of a residual:
+ *   h = x + residual, rounded to their type (residual NULL: h = x)    sum = h
+ *   rstd = 1 / sqrt(mean(h^2) + eps)          y = h rstd weight
+ * y is written in out_dtype (y_dev), in blocks of 128 of a row (codes_dev and
+ * scales_dev, as spectrain_blocks_pack ROWS takes them from the float32 y), or
+ * both. Sums are float32: a row whose squares pass its range has rstd 0. sum
+ * (NULL: not kept) goes with a residual and may be x or the residual itself (the
+ * same ld); otherwise outputs may not overlap inputs or each other. rstd float32
+ * [rows], NULL where no backward follows.
+ * Backward, with z = h rstd and u = dy weight:
+ *   dx = rstd (u - z mean(u z)) + dsum        dweight = sum over the rows of dy z
+ * h is the forward's sum (x where there was no residual); dsum, the gradient that
+ * reaches h by its other uses, may be NULL. dx is the gradient of x and of the
+ * residual alike; it may be dsum, or dy where their types agree (the same ld).
+ * dweight float32 [cols], overwritten. No atomics: results repeat bitwise. */
+typedef struct {
+  uint32_t abi_version;      /* SPECTRAIN_ABI_VERSION */
+  int32_t dtype;             /* spectrain_dtype of x, residual, sum, dsum and dx */
+  int32_t out_dtype;         /* of y and dy: dtype, or SPECTRAIN_BF16 */
+  int32_t weight_dtype;      /* of weight [cols] */
+  float eps;                 /* finite, > 0 */
+  int32_t reserved;          /* 0 */
+  int64_t rows, cols;        /* rows below 2^31, cols 1 .. 65536 */
+  int64_t x_ld, residual_ld, sum_ld, y_ld;   /* elements between rows: >= cols, at most 2^40; */
+  int64_t codes_ld, scales_ld;               /* looked at where their tensor is given. A backward takes */
+  int64_t dy_ld, dsum_ld, dx_ld;             /* sum_ld for h */
+} spectrain_rms_norm_desc;
+
+int spectrain_rms_norm_forward(const spectrain_rms_norm_desc* desc, const void* x_dev, const void* residual_dev,
+                               const void* weight_dev, void* sum_dev, void* y_dev, uint8_t* codes_dev,
+                               uint8_t* scales_dev, float* rstd_dev, void* hip_stream);
+
+/* Bytes of 256-byte aligned workspace that a backward needs. */
+int spectrain_rms_norm_workspace(const spectrain_rms_norm_desc* desc, size_t* bytes);
+int spectrain_rms_norm_backward(const spectrain_rms_norm_desc* desc, const void* dy_dev, const void* h_dev,
+                                const void* weight_dev, const float* rstd_dev, const void* dsum_dev, void* dx_dev,
+                                float* dweight_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* Product of two tensors in blocks, both with k along their rows:
+ *   v[i, j] = sum over k of A[i, k] B[j, k]     A [m, k], B [n, k]
+ *   v += bias[j]    v = 0 where v < 0 if relu    v = 0 where not mask[i, j] > 0
+ *   out = v, or out += v if accumulate
+ * with float32 sums (bias and mask NULL: without). A linear layer's forward takes
+ * x and its weight; its data gradient dy and the transposed weight; its weight
+ * gradient transposed dy and transposed x. Results do not depend on timing: no
+ * atomics; an element's sum takes the same order whatever the other rows hold.
+ * out may not overlap an operand or the mask. */
+typedef struct {
+  uint32_t abi_version;      /* SPECTRAIN_ABI_VERSION */
+  int32_t out_dtype;         /* spectrain_dtype of out and mask */
+  int32_t bias_dtype;        /* of bias [n] */
+  int32_t relu;              /* 0 or 1 */
+  int32_t accumulate;        /* 0 or 1 (float32 out) */
+  int32_t reserved;          /* 0 */
+  int64_t m, n, k;           /* below 2^31; k at most 2^22; ceil(m / 64) * ceil(n / 64) at most 2^23 */
+  int64_t a_ld, a_scales_ld, b_ld, b_scales_ld;   /* scales_ld * ceil(k / 128) below 2^31 */
+  int64_t out_ld, mask_ld;   /* elements: >= n, at most 2^40 */
+} spectrain_product_desc;
+
+/* Bytes of 256-byte aligned workspace that the product needs (0: none). */
+int spectrain_product_workspace(const spectrain_product_desc* desc, size_t* bytes);
+int spectrain_product(const spectrain_product_desc* desc, const uint8_t* a_codes_dev, const uint8_t* a_scales_dev,
+                      const uint8_t* b_codes_dev, const uint8_t* b_scales_dev, const void* bias_dev,
+                      const void* mask_dev, void* out_dev, void* workspace_dev, size_t workspace_bytes,
+                      void* hip_stream);
+
 /* ---- A transformer stage's use of them ---- */
 
 /* Positions and masks of a TRANSFORMER stage. By default its attention has

@@ -210,6 +210,60 @@ int spectrain_checkpoint_restore(int32_t dtype, int64_t rows, int64_t cols, cons
   });
 }
 
+int spectrain_blocks_pack(const spectrain_blocks_desc* desc, const void* x_dev, uint8_t* codes_dev,
+                          uint8_t* scales_dev, uint8_t* transposed_dev, uint8_t* transposed_scales_dev,
+                          void* hip_stream) {
+  return guarded([&]() {
+    spx::run_blocks_pack(desc, x_dev, codes_dev, scales_dev, transposed_dev, transposed_scales_dev,
+                         static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int spectrain_blocks_restore(const spectrain_blocks_desc* desc, const uint8_t* codes_dev, const uint8_t* scales_dev,
+                             void* out_dev, void* hip_stream) {
+  return guarded([&]() {
+    spx::run_blocks_restore(desc, codes_dev, scales_dev, out_dev, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int spectrain_rms_norm_forward(const spectrain_rms_norm_desc* desc, const void* x_dev, const void* residual_dev,
+                               const void* weight_dev, void* sum_dev, void* y_dev, uint8_t* codes_dev,
+                               uint8_t* scales_dev, float* rstd_dev, void* hip_stream) {
+  return guarded([&]() {
+    spx::run_rms_norm_forward(desc, x_dev, residual_dev, weight_dev, sum_dev, y_dev, codes_dev, scales_dev, rstd_dev,
+                              static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int spectrain_rms_norm_workspace(const spectrain_rms_norm_desc* desc, size_t* bytes) {
+  if (!bytes) return set_error(SPECTRAIN_EINVAL, "bytes is NULL");
+  return guarded([&]() { *bytes = spx::rms_norm_workspace(desc); });
+}
+
+int spectrain_rms_norm_backward(const spectrain_rms_norm_desc* desc, const void* dy_dev, const void* h_dev,
+                                const void* weight_dev, const float* rstd_dev, const void* dsum_dev, void* dx_dev,
+                                float* dweight_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  return guarded([&]() {
+    spx::run_rms_norm_backward(desc, dy_dev, h_dev, weight_dev, rstd_dev, dsum_dev, dx_dev, dweight_dev,
+                               workspace_dev, workspace_bytes, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int spectrain_product_workspace(const spectrain_product_desc* desc, size_t* bytes) {
+  if (!bytes) return set_error(SPECTRAIN_EINVAL, "bytes is NULL");
+  return guarded([&]() { *bytes = spx::product_workspace(desc); });
+}
+
+int spectrain_product(const spectrain_product_desc* desc, const uint8_t* a_codes_dev, const uint8_t* a_scales_dev,
+                      const uint8_t* b_codes_dev, const uint8_t* b_scales_dev, const void* bias_dev,
+                      const void* mask_dev, void* out_dev, void* workspace_dev, size_t workspace_bytes,
+                      void* hip_stream) {
+  return guarded([&]() {
+    spx::run_product(desc, a_codes_dev, a_scales_dev, b_codes_dev, b_scales_dev, bias_dev, mask_dev, out_dev,
+                     workspace_dev, workspace_bytes, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
 const char* spectrain_last_error(void) { return g_last_error.c_str(); }
 
 }  // extern "C"

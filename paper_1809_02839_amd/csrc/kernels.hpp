@@ -206,6 +206,50 @@ constexpr int CHECKPOINT_MAX = 5;
 hipError_t checkpoint_pack(const CheckpointArgs* a, int n, int dtype, hipStream_t s);
 hipError_t checkpoint_restore(const CheckpointArgs* a, int n, int dtype, hipStream_t s);
 
+// Tensors in blocks (blocks.hip): e4m3 codes [rows][codes_ld] and a scale byte
+// for each row and 128 columns, [block column][scales_ld].
+constexpr int BLOCK_COLS = 128;
+struct BlocksArgs {
+  const void* x = nullptr;   // pack
+  void* out = nullptr;       // restore
+  uint8_t *codes = nullptr, *scales = nullptr, *t_codes = nullptr, *t_scales = nullptr;
+  long rows = 0, cols = 0, ld = 0, codes_ld = 0, scales_ld = 0, t_ld = 0, t_scales_ld = 0;
+  int tiles = 0;             // a scale for 128 x 128, not for 128 of a row
+};
+hipError_t blocks_pack(const BlocksArgs& a, int dtype, hipStream_t s);
+hipError_t blocks_restore(const BlocksArgs& a, int dtype, hipStream_t s);
+
+// Root-mean-square norm (norm.hip). dtype: x, residual, sum (h), dsum, dx; out_dtype: y, dy.
+struct RmsNormArgs {
+  const void *x = nullptr, *residual = nullptr, *weight = nullptr;
+  void *sum = nullptr, *y = nullptr;
+  uint8_t *codes = nullptr, *scales = nullptr;
+  float* rstd = nullptr;
+  const void *dy = nullptr, *dsum = nullptr;   // backward; x is then h
+  void* dx = nullptr;
+  float *dweight = nullptr, *ws = nullptr;
+  long rows = 0, cols = 0;
+  long x_ld = 0, residual_ld = 0, sum_ld = 0, y_ld = 0, codes_ld = 0, scales_ld = 0, dy_ld = 0, dsum_ld = 0, dx_ld = 0;
+  int dtype = 0, out_dtype = 0, weight_dtype = 0;
+  float eps = 0.0f;
+};
+constexpr long RMS_NORM_COLS = 65536;   // longest row: its block keeps it in registers
+size_t rms_norm_ws_bytes(long rows, long cols);
+hipError_t rms_norm_fwd(const RmsNormArgs& a, hipStream_t s);
+hipError_t rms_norm_bwd(const RmsNormArgs& a, hipStream_t s);
+
+// Product of tensors in blocks (product.hip): out = epilogue(A B^T).
+struct ProductArgs {
+  const uint8_t *a = nullptr, *a_scales = nullptr, *b = nullptr, *b_scales = nullptr;
+  const void *bias = nullptr, *mask = nullptr;
+  void* out = nullptr;
+  float* ws = nullptr;
+  long m = 0, n = 0, k = 0, a_ld = 0, a_scales_ld = 0, b_ld = 0, b_scales_ld = 0, out_ld = 0, mask_ld = 0;
+  int out_dtype = 0, bias_dtype = 0, relu = 0, accumulate = 0;
+};
+size_t product_ws_bytes(long m, long n, long k);
+hipError_t product(const ProductArgs& a, hipStream_t s);
+
 // Row chunking of the two-pass column reductions (column sums, layer-norm
 // parameter gradients) and the float32 workspace each pass needs.
 constexpr int COLSUM_ROWS = 64;   // rows summed per block in the first pass

@@ -310,4 +310,280 @@ void run_checkpoint(int dtype, int64_t rows, int64_t cols, const void* x, int64_
                                                                                   : "checkpoint_restore");
 }
 
+// --------------------------------------------------- linear layers in 8 bits ----
+namespace {
+
+constexpr int64_t MAX_CODES_LD = int64_t{1} << 22;   // byte offsets inside a tile of 256 rows stay below 2^30
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+void check_version(uint32_t v) {
+  if (v != SPECTRAIN_ABI_VERSION) fail("abi_version mismatch");
+}
+
+void check_dtype(int dtype, const char* what) {
+  if (dtype != SPECTRAIN_FP32 && dtype != SPECTRAIN_BF16) fail(std::string("unknown ") + what);
+}
+
+size_t bytes_of(int dtype) { return dtype == SPECTRAIN_BF16 ? 2 : 4; }
+
+// Elements between rows of a matrix.
+void check_ld(int64_t ld, int64_t cols, const char* what) {
+  if (ld < cols || ld > MAX_STRIDE) fail(std::string(what) + " must lie in [" + std::to_string(cols) + ", 2^40]");
+}
+
+void check_elements(const void* p, int dtype, const char* what) {
+  if (!aligned(p, bytes_of(dtype))) fail(std::string(what) + " is not aligned to its elements");
+}
+
+// Lines of codes or scale bytes.
+void check_lines(const void* p, int64_t ld, int64_t bytes, int64_t most, const char* what) {
+  if (ld < bytes || ld > most || ld % 16)
+    fail(std::string(what) + "_ld must be a multiple of 16 in [" + std::to_string(bytes) + ", " +
+         std::to_string(most) + "]");
+  if (!aligned(p, 16)) fail(std::string(what) + " must be 16-byte aligned");
+}
+
+void check_blocks(const void* codes, const void* scales, int64_t rows, int64_t cols, int64_t codes_ld,
+                  int64_t scales_ld, const char* what) {
+  if (!codes != !scales) fail(std::string(what) + " go with their scales");
+  if (!codes) return;
+  check_lines(codes, codes_ld, cols, MAX_CODES_LD, what);
+  check_lines(scales, scales_ld, rows, MAX_STRIDE, (std::string(what) + " scales").c_str());
+  if (codes == scales) fail(std::string(what) + " and their scales overlap");
+}
+
+BlocksArgs blocks_args(const spectrain_blocks_desc* desc) {
+  if (!desc) fail("desc is NULL");
+  const spectrain_blocks_desc& d = *desc;
+  check_version(d.abi_version);
+  check_dtype(d.dtype, "dtype");
+  if (d.reserved != 0) fail("reserved must be 0");
+  if (d.rows < 0 || d.cols < 0) fail("rows and cols must be >= 0");
+  if (d.rows >= int64_t{1} << 31 || d.cols >= int64_t{1} << 31) fail("rows and cols must be below 2^31");
+  if (ceil_div(d.rows, 128) * ceil_div(d.cols, 128) > 1 << 23)
+    fail("ceil(rows / 128) * ceil(cols / 128) must be at most 2^23");
+  check_ld(d.ld, d.cols, "ld");
+  BlocksArgs a;
+  a.rows = d.rows;
+  a.cols = d.cols;
+  a.ld = d.ld;
+  a.codes_ld = d.codes_ld;
+  a.scales_ld = d.scales_ld;
+  a.t_ld = d.transposed_ld;
+  a.t_scales_ld = d.transposed_scales_ld;
+  return a;
+}
+
+}  // namespace
+
+void run_blocks_pack(const spectrain_blocks_desc* desc, const void* x, uint8_t* codes, uint8_t* scales, uint8_t* t_codes,
+                     uint8_t* t_scales, hipStream_t s) {
+  BlocksArgs a = blocks_args(desc);
+  if (desc->shape != SPECTRAIN_BLOCKS_ROWS && desc->shape != SPECTRAIN_BLOCKS_TILES) fail("unknown shape");
+  check_blocks(codes, scales, a.rows, a.cols, a.codes_ld, a.scales_ld, "codes");
+  check_blocks(t_codes, t_scales, a.cols, a.rows, a.t_ld, a.t_scales_ld, "transposed");
+  if (a.rows == 0 || a.cols == 0) return;
+  if (!x || (!codes && !t_codes)) fail("a tensor is NULL");
+  check_elements(x, desc->dtype, "x");
+  if (codes && t_codes && (t_codes == codes || t_codes == scales || t_scales == codes || t_scales == scales))
+    fail("the outputs must not overlap");
+  for (const void* p : {static_cast<const void*>(codes), static_cast<const void*>(scales),
+                        static_cast<const void*>(t_codes), static_cast<const void*>(t_scales)})
+    if (p == x) fail("an output must not be x");
+  a.x = x;
+  a.codes = codes;
+  a.scales = scales;
+  a.t_codes = t_codes;
+  a.t_scales = t_scales;
+  a.tiles = desc->shape == SPECTRAIN_BLOCKS_TILES;
+  hip_check(blocks_pack(a, desc->dtype, s), "blocks_pack");
+}
+
+void run_blocks_restore(const spectrain_blocks_desc* desc, const uint8_t* codes, const uint8_t* scales, void* out,
+                        hipStream_t s) {
+  BlocksArgs a = blocks_args(desc);
+  check_blocks(codes, scales, a.rows, a.cols, a.codes_ld, a.scales_ld, "codes");
+  if (a.rows == 0 || a.cols == 0) return;
+  if (!codes || !out) fail("a tensor is NULL");
+  check_elements(out, desc->dtype, "out");
+  if (out == codes || out == scales) fail("out must not be an input");
+  a.codes = const_cast<uint8_t*>(codes);
+  a.scales = const_cast<uint8_t*>(scales);
+  a.out = out;
+  hip_check(blocks_restore(a, desc->dtype, s), "blocks_restore");
+}
+
+// --------------------------------------------------------------- rms norm ----
+namespace {
+
+RmsNormArgs rms_norm_args(const spectrain_rms_norm_desc* desc) {
+  if (!desc) fail("desc is NULL");
+  const spectrain_rms_norm_desc& d = *desc;
+  check_version(d.abi_version);
+  check_dtype(d.dtype, "dtype");
+  check_dtype(d.out_dtype, "out_dtype");
+  check_dtype(d.weight_dtype, "weight_dtype");
+  if (d.out_dtype != d.dtype && d.out_dtype != SPECTRAIN_BF16) fail("out_dtype must be dtype or bf16");
+  if (d.reserved != 0) fail("reserved must be 0");
+  if (!(d.eps > 0.0f) || !std::isfinite(d.eps)) fail("eps must be finite and > 0");
+  if (d.rows < 0 || d.rows >= int64_t{1} << 31) fail("rows must lie in [0, 2^31)");
+  if (d.cols < 1 || d.cols > RMS_NORM_COLS) fail("cols must lie in [1, 65536]");
+  RmsNormArgs a;
+  a.rows = d.rows;
+  a.cols = d.cols;
+  a.dtype = d.dtype;
+  a.out_dtype = d.out_dtype;
+  a.weight_dtype = d.weight_dtype;
+  a.eps = d.eps;
+  return a;
+}
+
+// A matrix that may be absent: its ld is looked at only where it is given.
+long given_ld(const void* p, int64_t ld, int64_t cols, int dtype, const char* what) {
+  if (!p) return 0;
+  check_ld(ld, cols, (std::string(what) + "_ld").c_str());
+  check_elements(p, dtype, what);
+  return ld;
+}
+
+}  // namespace
+
+void run_rms_norm_forward(const spectrain_rms_norm_desc* desc, const void* x, const void* residual, const void* weight,
+                          void* sum, void* y, uint8_t* codes, uint8_t* scales, float* rstd, hipStream_t s) {
+  RmsNormArgs a = rms_norm_args(desc);
+  const spectrain_rms_norm_desc& d = *desc;
+  a.x_ld = given_ld(x, d.x_ld, a.cols, d.dtype, "x");
+  a.residual_ld = given_ld(residual, d.residual_ld, a.cols, d.dtype, "residual");
+  a.sum_ld = given_ld(sum, d.sum_ld, a.cols, d.dtype, "sum");
+  a.y_ld = given_ld(y, d.y_ld, a.cols, d.out_dtype, "y");
+  check_elements(weight, d.weight_dtype, "weight");
+  check_blocks(codes, scales, a.rows, a.cols, d.codes_ld, d.scales_ld, "codes");
+  if (!aligned(rstd, 4)) fail("rstd must be 4-byte aligned");
+  if (sum && !residual) fail("sum goes with a residual");
+  if (a.rows == 0) return;
+  if (!x || !weight || (!y && !codes)) fail("a tensor is NULL");
+  if (sum && ((sum == x && a.sum_ld != a.x_ld) || (sum == residual && a.sum_ld != a.residual_ld)))
+    fail("in place, sum must have the same ld");
+  for (const void* o : {static_cast<const void*>(y), static_cast<const void*>(codes), static_cast<const void*>(scales),
+                        static_cast<const void*>(rstd)})
+    if (o && (o == x || o == residual || o == weight || o == sum)) fail("an output must not be an input or the sum");
+  if (sum && sum == weight) fail("an output must not be an input or the sum");
+  if (codes && (codes == y || scales == y)) fail("the outputs must not overlap");
+  a.x = x;
+  a.residual = residual;
+  a.weight = weight;
+  a.sum = sum;
+  a.y = y;
+  a.codes = codes;
+  a.scales = scales;
+  a.codes_ld = d.codes_ld;
+  a.scales_ld = d.scales_ld;
+  a.rstd = rstd;
+  hip_check(rms_norm_fwd(a, s), "rms_norm");
+}
+
+size_t rms_norm_workspace(const spectrain_rms_norm_desc* desc) {
+  const RmsNormArgs a = rms_norm_args(desc);
+  return rms_norm_ws_bytes(a.rows, a.cols);
+}
+
+void run_rms_norm_backward(const spectrain_rms_norm_desc* desc, const void* dy, const void* h, const void* weight,
+                           const float* rstd, const void* dsum, void* dx, float* dweight, void* ws, size_t ws_bytes,
+                           hipStream_t s) {
+  RmsNormArgs a = rms_norm_args(desc);
+  const spectrain_rms_norm_desc& d = *desc;
+  check_workspace(ws, ws_bytes, rms_norm_ws_bytes(a.rows, a.cols));
+  a.dy_ld = given_ld(dy, d.dy_ld, a.cols, d.out_dtype, "dy");
+  a.sum_ld = given_ld(h, d.sum_ld, a.cols, d.dtype, "sum");
+  a.dsum_ld = given_ld(dsum, d.dsum_ld, a.cols, d.dtype, "dsum");
+  a.dx_ld = given_ld(dx, d.dx_ld, a.cols, d.dtype, "dx");
+  check_elements(weight, d.weight_dtype, "weight");
+  if (!aligned(rstd, 4) || !aligned(dweight, 4)) fail("rstd and dweight must be 4-byte aligned");
+  if (!dweight) fail("dweight is NULL");
+  if (a.rows && (!dy || !h || !weight || !rstd || !dx)) fail("a tensor is NULL");
+  if (dx && (dx == h || dx == weight || dx == rstd || dx == dweight)) fail("dx must not be h, weight, rstd or dweight");
+  for (const void* p : {dy, h, weight, static_cast<const void*>(rstd), dsum})
+    if (p == dweight) fail("dweight must not be an input");
+  if (dx && dx == dsum && a.dx_ld != a.dsum_ld) fail("in place, dx must have the same ld");
+  if (dx && dx == dy && (a.dx_ld != a.dy_ld || d.dtype != d.out_dtype)) fail("in place, dx must have the same ld and type");
+  a.dy = dy;
+  a.x = h;
+  a.weight = weight;
+  a.rstd = const_cast<float*>(rstd);
+  a.dsum = dsum;
+  a.dx = dx;
+  a.dweight = dweight;
+  a.ws = static_cast<float*>(ws);
+  hip_check(rms_norm_bwd(a, s), "rms_norm_bwd");
+}
+
+// ---------------------------------------------------------------- product ----
+namespace {
+
+ProductArgs product_args(const spectrain_product_desc* desc) {
+  if (!desc) fail("desc is NULL");
+  const spectrain_product_desc& d = *desc;
+  check_version(d.abi_version);
+  check_dtype(d.out_dtype, "out_dtype");
+  check_dtype(d.bias_dtype, "bias_dtype");
+  if ((d.relu != 0 && d.relu != 1) || (d.accumulate != 0 && d.accumulate != 1)) fail("relu and accumulate must be 0 or 1");
+  if (d.accumulate && d.out_dtype != SPECTRAIN_FP32) fail("accumulate needs a float32 out");
+  if (d.reserved != 0) fail("reserved must be 0");
+  if (d.m < 0 || d.n < 0 || d.k < 0) fail("m, n and k must be >= 0");
+  if (d.m >= int64_t{1} << 31 || d.n >= int64_t{1} << 31 || d.k > MAX_CODES_LD)
+    fail("m and n must be below 2^31 and k at most 2^22");
+  if (ceil_div(d.m, 64) * ceil_div(d.n, 64) > 1 << 23) fail("ceil(m / 64) * ceil(n / 64) must be at most 2^23");
+  ProductArgs a;
+  a.m = d.m;
+  a.n = d.n;
+  a.k = d.k;
+  a.out_dtype = d.out_dtype;
+  a.bias_dtype = d.bias_dtype;
+  a.relu = d.relu;
+  a.accumulate = d.accumulate;
+  return a;
+}
+
+}  // namespace
+
+size_t product_workspace(const spectrain_product_desc* desc) {
+  const ProductArgs a = product_args(desc);
+  return product_ws_bytes(a.m, a.n, a.k);
+}
+
+void run_product(const spectrain_product_desc* desc, const uint8_t* a_codes, const uint8_t* a_scales,
+                 const uint8_t* b_codes, const uint8_t* b_scales, const void* bias, const void* mask, void* out,
+                 void* ws, size_t ws_bytes, hipStream_t s) {
+  ProductArgs a = product_args(desc);
+  const spectrain_product_desc& d = *desc;
+  check_workspace(ws, ws_bytes, product_ws_bytes(a.m, a.n, a.k));
+  check_blocks(a_codes, a_scales, a.m, a.k, d.a_ld, d.a_scales_ld, "a");
+  check_blocks(b_codes, b_scales, a.n, a.k, d.b_ld, d.b_scales_ld, "b");
+  const int64_t blocks = ceil_div(a.k, 128);
+  if (blocks && (d.a_scales_ld >= (int64_t{1} << 31) / blocks || d.b_scales_ld >= (int64_t{1} << 31) / blocks))
+    fail("scales_ld * ceil(k / 128) must be below 2^31");
+  a.out_ld = given_ld(out, d.out_ld, a.n, d.out_dtype, "out");
+  a.mask_ld = given_ld(mask, d.mask_ld, a.n, d.out_dtype, "mask");
+  check_elements(bias, d.bias_dtype, "bias");
+  if (a.m == 0 || a.n == 0) return;
+  if (!out || (a.k && (!a_codes || !b_codes))) fail("a tensor is NULL");
+  for (const void* p : {static_cast<const void*>(a_codes), static_cast<const void*>(a_scales),
+                        static_cast<const void*>(b_codes), static_cast<const void*>(b_scales), bias, mask})
+    if (out == p) fail("out must not be an input");
+  a.a = a_codes;
+  a.a_scales = a_scales;
+  a.b = b_codes;
+  a.b_scales = b_scales;
+  a.a_ld = d.a_ld;
+  a.a_scales_ld = d.a_scales_ld;
+  a.b_ld = d.b_ld;
+  a.b_scales_ld = d.b_scales_ld;
+  a.bias = bias;
+  a.mask = mask;
+  a.out = out;
+  a.ws = static_cast<float*>(ws);
+  hip_check(product(a, s), "product");
+}
+
 }  // namespace spx

@@ -31,10 +31,14 @@ EXPORTED = ("spectrain_version_difference", "spectrain_stage_create", "spectrain
             "spectrain_stage_read_stash", "spectrain_stage_destroy", "spectrain_stage_set_attention",
             "spectrain_stage_set_masks", "spectrain_stage_set_stash", "spectrain_rotary",
             "spectrain_attention_workspace", "spectrain_attention_forward", "spectrain_attention_backward",
-            "spectrain_checkpoint_pack", "spectrain_checkpoint_restore", "spectrain_last_error")
+            "spectrain_checkpoint_pack", "spectrain_checkpoint_restore", "spectrain_blocks_pack",
+            "spectrain_blocks_restore", "spectrain_rms_norm_forward", "spectrain_rms_norm_workspace",
+            "spectrain_rms_norm_backward", "spectrain_product_workspace", "spectrain_product", "spectrain_last_error")
 ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "parts": 3}
 CHECKPOINT_GROUP = 32
+BLOCK_COLS = 128
+BLOCKS_ROWS, BLOCKS_TILES = 0, 1
 STASH_FORMATS = {"bf16": 0, "e4m3": 1}
 
 
@@ -71,6 +75,25 @@ class AttentionDesc(ctypes.Structure):
 
 class AttentionMasks(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("documents", "prefix", "kv_lengths", "slopes")]
+
+
+class BlocksDesc(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in ("dtype", "shape", "reserved")] + [
+        (n, ctypes.c_int64) for n in ("rows", "cols", "ld", "codes_ld", "scales_ld", "transposed_ld",
+                                      "transposed_scales_ld")]
+
+
+class RmsNormDesc(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in (
+        "dtype", "out_dtype", "weight_dtype")] + [("eps", ctypes.c_float), ("reserved", ctypes.c_int32)] + [
+        (n, ctypes.c_int64) for n in ("rows", "cols", "x_ld", "residual_ld", "sum_ld", "y_ld", "codes_ld", "scales_ld",
+                                      "dy_ld", "dsum_ld", "dx_ld")]
+
+
+class ProductDesc(ctypes.Structure):
+    _fields_ = [("abi_version", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in (
+        "out_dtype", "bias_dtype", "relu", "accumulate", "reserved")] + [(n, ctypes.c_int64) for n in (
+            "m", "n", "k", "a_ld", "a_scales_ld", "b_ld", "b_scales_ld", "out_ld", "mask_ld")]
 
 
 class StageAttention(ctypes.Structure):
@@ -127,6 +150,13 @@ def lib():
                                                             ctypes.POINTER(AttentionMasks)] + [vp] * 10 + [sz, vp]),
             "spectrain_checkpoint_pack": (ctypes.c_int, [i32, i64, i64, vp, i64, vp, vp, vp]),
             "spectrain_checkpoint_restore": (ctypes.c_int, [i32, i64, i64, vp, vp, vp, i64, vp]),
+            "spectrain_blocks_pack": (ctypes.c_int, [ctypes.POINTER(BlocksDesc)] + [vp] * 6),
+            "spectrain_blocks_restore": (ctypes.c_int, [ctypes.POINTER(BlocksDesc)] + [vp] * 4),
+            "spectrain_rms_norm_forward": (ctypes.c_int, [ctypes.POINTER(RmsNormDesc)] + [vp] * 9),
+            "spectrain_rms_norm_workspace": (ctypes.c_int, [ctypes.POINTER(RmsNormDesc), ctypes.POINTER(sz)]),
+            "spectrain_rms_norm_backward": (ctypes.c_int, [ctypes.POINTER(RmsNormDesc)] + [vp] * 8 + [sz, vp]),
+            "spectrain_product_workspace": (ctypes.c_int, [ctypes.POINTER(ProductDesc), ctypes.POINTER(sz)]),
+            "spectrain_product": (ctypes.c_int, [ctypes.POINTER(ProductDesc)] + [vp] * 8 + [sz, vp]),
             "spectrain_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -395,6 +425,12 @@ def _side(t, shape, dtype, device, what):
     return t.data_ptr()
 
 
+def _scratch(workspace, device):
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on {device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 class Rotary:
     """Rotary positions of heads of one width (spectrain_rotary): layout "half"
     or "interleaved"; scaling "none", "linear", "ntk" or "parts"."""
@@ -481,11 +517,6 @@ class Attention:
                               _side(kv_lengths, (d.batch,), "torch.int32", device, "kv_lengths"),
                               _side(slopes, (d.heads,), "torch.float32", device, "slopes"))
 
-    def _scratch(self, workspace, device):
-        if workspace.device != device or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be contiguous and on {device}")
-        return workspace.data_ptr(), workspace.numel() * workspace.element_size()
-
     def forward(self, q, k, v, out, lse=None, *, workspace, documents=None, prefix=None, kv_lengths=None, slopes=None,
                 stream=None):
         """out = attention(q, k, v); lse float32 [batch, heads, q_len] as the backward takes it (None: not wanted)."""
@@ -494,7 +525,7 @@ class Attention:
                                              ("out", out, self._qs)), q)
         lp = _side(lse, (d.batch, d.heads, d.q_len), "torch.float32", dev, "lse")
         m = self._masks(dev, documents, prefix, kv_lengths, slopes)
-        wp, wn = self._scratch(workspace, dev)
+        wp, wn = _scratch(workspace, dev)
         _on(dev, stream, lib().spectrain_attention_forward, ctypes.byref(d), ctypes.byref(m), *ptr, lp, wp, wn)
 
     def backward(self, q, k, v, out, lse, dout, dq, dk, dv, *, workspace, documents=None, prefix=None, kv_lengths=None,
@@ -506,7 +537,7 @@ class Attention:
             ("dk", dk, ks), ("dv", dv, ks)), q)
         lp = _side(lse, (d.batch, d.heads, d.q_len), "torch.float32", dev, "lse")
         m = self._masks(dev, documents, prefix, kv_lengths, slopes)
-        wp, wn = self._scratch(workspace, dev)
+        wp, wn = _scratch(workspace, dev)
         _on(dev, stream, lib().spectrain_attention_backward, ctypes.byref(d), ctypes.byref(m), *ptr[:4], lp,
             *ptr[4:], wp, wn)
 
@@ -534,3 +565,172 @@ def checkpoint_restore(codes, scales, out, stream=None):
     dt, rows, cols, cp, sp, ld = _checkpoint_args(out, codes, scales, "out")
     op = out.data_ptr()
     _on(out.device, stream, lib().spectrain_checkpoint_restore, dt, rows, cols, cp, sp, op, ld)
+
+
+# ---- linear layers in 8 bits ----
+
+def _matrix(t, shape, dtype, device, what):
+    """Pointer and ld of a [rows, cols] tensor with a contiguous last dimension (None: absent)."""
+    if t is None:
+        return None, 0
+    if t.device != device:
+        raise ValueError(f"{what} must be on {device}, got {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    rows, cols = shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what} must be contiguous in its last dimension")
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, 1)
+
+
+def _lines(t, shape, device, what):
+    """Pointer and ld of codes or scale bytes; one line's ld, which torch may have lost, is its length rounded up."""
+    import torch
+    p, ld = _matrix(t, shape, torch.uint8, device, what)
+    return p, -(-shape[1] // 16) * 16 if shape[0] <= 1 else ld
+
+
+def _blocks(codes, scales, rows, cols, device, what):
+    """Pointers and ld of codes [rows, cols] and scales [ceil(cols / 128), rows] (both None: absent)."""
+    if (codes is None) != (scales is None):
+        raise ValueError(f"{what} and their scales go together")
+    if codes is None:
+        return None, 0, None, 0
+    return (*_lines(codes, (rows, cols), device, what),
+            *_lines(scales, (-(-cols // BLOCK_COLS), rows), device, what + " scales"))
+
+
+def blocks_empty(rows, cols, device="cuda"):
+    """Codes uint8 [rows, cols] and scales uint8 [ceil(cols / 128), rows] of a tensor in blocks, not filled."""
+    import torch
+
+    def lines(n, length):
+        return torch.empty(n, -(-length // 16) * 16, dtype=torch.uint8, device=device)[:, :length]
+
+    return lines(rows, cols), lines(-(-cols // BLOCK_COLS), rows)
+
+
+def blocks_pack(x, codes=None, scales=None, transposed=None, transposed_scales=None, tiles=False, stream=None):
+    """x [rows, cols] to blocks (codes, scales), to blocks of its transpose, or to both; a scale for 128 values of a
+    row, or (tiles) for 128 x 128."""
+    if x.dim() != 2:
+        raise ValueError(f"x must be [rows, cols], got {tuple(x.shape)}")
+    rows, cols = x.shape
+    xp, ld = _matrix(x, x.shape, x.dtype, x.device, "x")
+    cp, cl, sp, sl = _blocks(codes, scales, rows, cols, x.device, "codes")
+    tp, tl, up, ul = _blocks(transposed, transposed_scales, cols, rows, x.device, "transposed")
+    d = BlocksDesc(ABI_VERSION, _dtype_code(x, "x"), BLOCKS_TILES if tiles else BLOCKS_ROWS, 0, rows, cols, ld, cl, sl,
+                   tl, ul)
+    _on(x.device, stream, lib().spectrain_blocks_pack, ctypes.byref(d), xp, cp, sp, tp, up)
+
+
+def blocks_restore(codes, scales, out, stream=None):
+    """The values that codes and scales stand for, into out [rows, cols]."""
+    if out.dim() != 2:
+        raise ValueError(f"out must be [rows, cols], got {tuple(out.shape)}")
+    rows, cols = out.shape
+    op, ld = _matrix(out, out.shape, out.dtype, out.device, "out")
+    cp, cl, sp, sl = _blocks(codes, scales, rows, cols, out.device, "codes")
+    d = BlocksDesc(ABI_VERSION, _dtype_code(out, "out"), BLOCKS_ROWS, 0, rows, cols, ld, cl, sl, 0, 0)
+    _on(out.device, stream, lib().spectrain_blocks_restore, ctypes.byref(d), cp, sp, op)
+
+
+class RmsNorm:
+    """Root-mean-square norm of rows of `cols` values (spectrain_rms_norm_forward
+    and _backward). Tensors are [rows, cols], bf16 or float32, contiguous in their
+    last dimension; y and dy may be bf16 beside float32 others."""
+
+    def __init__(self, cols, eps=1e-6):
+        self.cols, self.eps = cols, eps
+
+    def _desc(self, rows, dtype, out_dtype, weight_dtype):
+        d = RmsNormDesc(ABI_VERSION, dtype, out_dtype, weight_dtype, self.eps, 0, rows, self.cols)
+        return d
+
+    def workspace_bytes(self, rows):
+        n = ctypes.c_size_t()
+        _check(lib().spectrain_rms_norm_workspace(ctypes.byref(self._desc(rows, FP32, FP32, FP32)), ctypes.byref(n)))
+        return n.value
+
+    def workspace(self, rows, device="cuda"):
+        """A workspace for backwards of `rows` rows: one for calls that follow each other on a stream."""
+        import torch
+        return torch.empty(max(256, self.workspace_bytes(rows)), dtype=torch.uint8, device=device)
+
+    def _checked(self, x, weight, what):
+        if x.dim() != 2 or x.shape[1] != self.cols:
+            raise ValueError(f"{what} must be [rows, {self.cols}], got {tuple(x.shape)}")
+        if tuple(weight.shape) != (self.cols,) or not weight.is_contiguous() or weight.device != x.device:
+            raise ValueError(f"weight must be contiguous ({self.cols},) on {x.device}, got {tuple(weight.shape)} on "
+                             f"{weight.device}")
+        return _dtype_code(x, what), _dtype_code(weight, "weight")
+
+    def forward(self, x, weight, y=None, *, residual=None, sum=None, codes=None, scales=None, rstd=None, stream=None):
+        """sum = x + residual (rounded to their type); its norm to y, to blocks of 128 (codes, scales), or both; rstd
+        float32 [rows] as the backward takes it (None: not wanted)."""
+        dt, wt = self._checked(x, weight, "x")
+        shape, dev = x.shape, x.device
+        d = self._desc(shape[0], dt, dt if y is None else _dtype_code(y, "y"), wt)
+        xp, d.x_ld = _matrix(x, shape, x.dtype, dev, "x")
+        rp, d.residual_ld = _matrix(residual, shape, x.dtype, dev, "residual")
+        sp, d.sum_ld = _matrix(sum, shape, x.dtype, dev, "sum")
+        yp, d.y_ld = _matrix(y, shape, None if y is None else y.dtype, dev, "y")
+        cp, d.codes_ld, lp, d.scales_ld = _blocks(codes, scales, *shape, dev, "codes")
+        qp = _side(rstd, (shape[0],), "torch.float32", dev, "rstd")
+        _on(dev, stream, lib().spectrain_rms_norm_forward, ctypes.byref(d), xp, rp, weight.data_ptr(), sp, yp, cp, lp, qp)
+
+    def backward(self, dy, h, weight, rstd, dx, dweight, *, dsum=None, workspace, stream=None):
+        """dx (of x and of the residual alike) and dweight float32 [cols], overwritten, from dy, the forward's sum h
+        and rstd, and the gradient dsum that reaches h elsewhere."""
+        dt, wt = self._checked(h, weight, "h")
+        shape, dev = h.shape, h.device
+        d = self._desc(shape[0], dt, _dtype_code(dy, "dy"), wt)
+        gp, d.dy_ld = _matrix(dy, shape, dy.dtype, dev, "dy")
+        hp, d.sum_ld = _matrix(h, shape, h.dtype, dev, "h")
+        sp, d.dsum_ld = _matrix(dsum, shape, h.dtype, dev, "dsum")
+        xp, d.dx_ld = _matrix(dx, shape, h.dtype, dev, "dx")
+        rp = _side(rstd, (shape[0],), "torch.float32", dev, "rstd")
+        wp = _side(dweight, (self.cols,), "torch.float32", dev, "dweight")
+        kp, kn = _scratch(workspace, dev)
+        _on(dev, stream, lib().spectrain_rms_norm_backward, ctypes.byref(d), gp, hp, weight.data_ptr(), rp, sp, xp, wp,
+            kp, kn)
+
+
+class Product:
+    """out [m, n] = A B^T of tensors in blocks, A [m, k] and B [n, k]
+    (spectrain_product): + bias [n], ReLU, zero where mask [m, n] is not positive."""
+
+    def __init__(self, m, n, k, relu=False, accumulate=False):
+        self.m, self.n, self.k = m, n, k
+        self.relu, self.accumulate = int(bool(relu)), int(bool(accumulate))
+
+    def _desc(self, out_dtype):
+        return ProductDesc(ABI_VERSION, out_dtype, FP32, self.relu, self.accumulate, 0, self.m, self.n, self.k)
+
+    def workspace_bytes(self):
+        n = ctypes.c_size_t()
+        _check(lib().spectrain_product_workspace(ctypes.byref(self._desc(FP32)), ctypes.byref(n)))
+        return n.value
+
+    def workspace(self, device="cuda"):
+        """A workspace for this shape's calls: one for calls that follow each other on a stream."""
+        import torch
+        return torch.empty(max(256, self.workspace_bytes()), dtype=torch.uint8, device=device)
+
+    def apply(self, a, a_scales, b, b_scales, out, *, bias=None, mask=None, workspace, stream=None):
+        """out = A B^T (out += with accumulate). Returns out."""
+        dev, m, n, k = out.device, self.m, self.n, self.k
+        d = self._desc(_dtype_code(out, "out"))
+        op, d.out_ld = _matrix(out, (m, n), out.dtype, dev, "out")
+        mp, d.mask_ld = _matrix(mask, (m, n), out.dtype, dev, "mask")
+        ap, d.a_ld, sp, d.a_scales_ld = _blocks(a, a_scales, m, k, dev, "a")
+        bp, d.b_ld, tp, d.b_scales_ld = _blocks(b, b_scales, n, k, dev, "b")
+        bias_p = None
+        if bias is not None:
+            d.bias_dtype = _dtype_code(bias, "bias")
+            bias_p = _side(bias, (n,), str(bias.dtype), dev, "bias")
+        wp, wn = _scratch(workspace, dev)
+        _on(dev, stream, lib().spectrain_product, ctypes.byref(d), ap, sp, bp, tp, bias_p, mp, op, wp, wn)
+        return out
