@@ -16,7 +16,7 @@ namespace {
 constexpr int NT = 256, TILE = BLOCK_COLS;
 constexpr int PITCH = TILE + 16;   // bytes between transposed lines in LDS
 
-template <typename T, bool WIDE>
+template <typename T>
 __global__ __launch_bounds__(NT) void blocks_pack_kernel(BlocksArgs a, uint32_t tiles_n) {
   __shared__ uint32_t tops[16][TILE];          // per row group: the columns' largest
   __shared__ uint8_t turned[TILE * PITCH];
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(NT) void blocks_pack_kernel(BlocksArgs a, uint32_t 
   const T* x = static_cast<const T*>(a.x) + (row0 + 8 * g) * a.ld + col0 + 8 * c;
   float v[8][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) load8<T, WIDE>(x + i * a.ld, 8 * g + i < rows ? nc : 0, v[i]);
+  for (int i = 0; i < 8; ++i) load8<T>(x + i * a.ld, 8 * g + i < rows ? nc : 0, v[i]);
 
   uint32_t row_top[8];
 #pragma unroll
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(NT) void blocks_pack_kernel(BlocksArgs a, uint32_t 
   if (t < cols) a.t_scales[static_cast<long>(tm) * a.t_scales_ld + col0 + t] = static_cast<uint8_t>(col_e[t] + 127);
 }
 
-template <typename T, bool WIDE>
+template <typename T>
 __global__ __launch_bounds__(NT) void blocks_restore_kernel(BlocksArgs a, uint32_t tiles_n) {
   const int t = threadIdx.x, c = t & 15, g = t >> 4;
   const uint32_t tm = blockIdx.x / tiles_n, tn = blockIdx.x - tm * tiles_n;
@@ -148,13 +148,8 @@ __global__ __launch_bounds__(NT) void blocks_restore_kernel(BlocksArgs a, uint32
       const f32x2_t hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[q]), true);
       v[4 * q] = lo[0] * scale, v[4 * q + 1] = lo[1] * scale, v[4 * q + 2] = hi[0] * scale, v[4 * q + 3] = hi[1] * scale;
     }
-    store8<T, WIDE>(static_cast<T*>(a.out) + r * a.ld + col, n, v);
+    store8<T>(static_cast<T*>(a.out) + r * a.ld + col, n, v);
   }
-}
-
-// Whether eight consecutive values of a row can be loaded or stored at once.
-bool wide(const BlocksArgs& a, const void* t) {
-  return a.cols % 8 == 0 && a.ld % 8 == 0 && reinterpret_cast<uintptr_t>(t) % 16 == 0;
 }
 
 template <typename K>
@@ -168,15 +163,11 @@ hipError_t launch(K* kernel, const BlocksArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t blocks_pack(const BlocksArgs& a, int dtype, hipStream_t s) {
-  const bool w = wide(a, a.x);
-  if (dtype) return launch(w ? blocks_pack_kernel<bf16_t, true> : blocks_pack_kernel<bf16_t, false>, a, s);
-  return launch(w ? blocks_pack_kernel<float, true> : blocks_pack_kernel<float, false>, a, s);
+  return dtype ? launch(blocks_pack_kernel<bf16_t>, a, s) : launch(blocks_pack_kernel<float>, a, s);
 }
 
 hipError_t blocks_restore(const BlocksArgs& a, int dtype, hipStream_t s) {
-  const bool w = wide(a, a.out);
-  if (dtype) return launch(w ? blocks_restore_kernel<bf16_t, true> : blocks_restore_kernel<bf16_t, false>, a, s);
-  return launch(w ? blocks_restore_kernel<float, true> : blocks_restore_kernel<float, false>, a, s);
+  return dtype ? launch(blocks_restore_kernel<bf16_t>, a, s) : launch(blocks_restore_kernel<float>, a, s);
 }
 
 }  // namespace spx

@@ -49,45 +49,50 @@ __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
 }
 
-// Eight consecutive values of a row of bf16 or float32, n of them there.
-template <typename T, bool WIDE>
+// Vectors at any element's address: rows need not start at multiples of 16 bytes.
+typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint16_t u16x8u_t __attribute__((ext_vector_type(8), aligned(2)));
+
+// Eight consecutive values of a row of bf16 or float32, n of them there (the others 0).
+template <typename T>
 __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-  if (WIDE) {
-    if (n <= 0) return;
+  if (n >= 8) {
     if constexpr (sizeof(T) == 2) {
-      const u16x8_t u = *reinterpret_cast<const u16x8_t*>(p);
+      const u16x8_t u = *reinterpret_cast<const u16x8u_t*>(p);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = bf16_to_f32(u[i]);
     } else {
-      const float4 u = *reinterpret_cast<const float4*>(p), w = *reinterpret_cast<const float4*>(p + 4);
-      v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w, v[4] = w.x, v[5] = w.y, v[6] = w.z, v[7] = w.w;
+      const f32x4_t u = *reinterpret_cast<const f32x4u_t*>(p), w = *reinterpret_cast<const f32x4u_t*>(p + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = u[i], v[4 + i] = w[i];
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 8; ++i) {
+      v[i] = 0.0f;
       if (i < n) {
         if constexpr (sizeof(T) == 2) v[i] = bf16_to_f32(p[i]);
         else v[i] = p[i];
       }
+    }
   }
 }
 
-template <typename T, bool WIDE>
+template <typename T>
 __device__ __forceinline__ void store8(T* p, int n, const float (&v)[8]) {
-  if (WIDE) {
-    if (n <= 0) return;
+  if (n >= 8) {
     if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                                pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+      typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+      typedef uint32_t u32x4u_t __attribute__((ext_vector_type(4), aligned(2)));
+      const u32x4_t u = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+      *reinterpret_cast<u32x4u_t*>(p) = u;
     } else {
-      *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      *reinterpret_cast<f32x4u_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4u_t*>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < 7; ++i)
       if (i < n) {
         if constexpr (sizeof(T) == 2) p[i] = f32_to_bf16(v[i]);
         else p[i] = v[i];

@@ -32,10 +32,9 @@ __device__ __forceinline__ float row_sum(float v, float* part) {
   return v;
 }
 
-template <bool WIDE>
 __device__ __forceinline__ void load_weight(const RmsNormArgs& a, long col, int n, float (&w)[8]) {
-  if (a.weight_dtype) load8<bf16_t, WIDE>(static_cast<const bf16_t*>(a.weight) + col, n, w);
-  else load8<float, WIDE>(static_cast<const float*>(a.weight) + col, n, w);
+  if (a.weight_dtype) load8<bf16_t>(static_cast<const bf16_t*>(a.weight) + col, n, w);
+  else load8<float>(static_cast<const float*>(a.weight) + col, n, w);
 }
 
 template <typename T>
@@ -44,7 +43,7 @@ __device__ __forceinline__ float rounded(float v) {
   else return v;
 }
 
-template <typename T, typename Y, int TPR, int V, bool WIDE>
+template <typename T, typename Y, int TPR, int V>
 __global__ __launch_bounds__(TPR > NT ? TPR : NT) void rms_norm_fwd_kernel(RmsNormArgs a) {
   __shared__ float part[16];
   constexpr int ROWS = TPR < NT ? NT / TPR : 1;   // of a block
@@ -57,13 +56,13 @@ __global__ __launch_bounds__(TPR > NT ? TPR : NT) void rms_norm_fwd_kernel(RmsNo
     for (int v = 0; v < V; ++v) {
       const long col = 8L * (v * TPR + t);
       const int n = static_cast<int>(min(max(a.cols - col, 0L), 8L));
-      load8<T, WIDE>(static_cast<const T*>(a.x) + row * a.x_ld + col, n, h[v]);
+      load8<T>(static_cast<const T*>(a.x) + row * a.x_ld + col, n, h[v]);
       if (a.residual) {
         float r[8];
-        load8<T, WIDE>(static_cast<const T*>(a.residual) + row * a.residual_ld + col, n, r);
+        load8<T>(static_cast<const T*>(a.residual) + row * a.residual_ld + col, n, r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[v][i] = rounded<T>(h[v][i] + r[i]);
-        if (a.sum) store8<T, WIDE>(static_cast<T*>(a.sum) + row * a.sum_ld + col, n, h[v]);
+        if (a.sum) store8<T>(static_cast<T*>(a.sum) + row * a.sum_ld + col, n, h[v]);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum = fmaf(h[v][i], h[v][i], sum);
@@ -76,10 +75,10 @@ __global__ __launch_bounds__(TPR > NT ? TPR : NT) void rms_norm_fwd_kernel(RmsNo
       const long col = 8L * (v * TPR + t);
       const int n = static_cast<int>(min(max(a.cols - col, 0L), 8L));
       float w[8];
-      load_weight<WIDE>(a, col, n, w);
+      load_weight(a, col, n, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) h[v][i] = h[v][i] * r * w[i];
-      if (a.y) store8<Y, WIDE>(static_cast<Y*>(a.y) + row * a.y_ld + col, n, h[v]);
+      if (a.y) store8<Y>(static_cast<Y*>(a.y) + row * a.y_ld + col, n, h[v]);
       if (a.codes) {   // 16 threads hold a block
         uint32_t top = 0;
 #pragma unroll
@@ -96,7 +95,7 @@ __global__ __launch_bounds__(TPR > NT ? TPR : NT) void rms_norm_fwd_kernel(RmsNo
   }
 }
 
-template <typename T, typename Y, int TPR, int V, bool WIDE>
+template <typename T, typename Y, int TPR, int V>
 __global__ __launch_bounds__(TPR > NT ? TPR : NT) void rms_norm_bwd_kernel(RmsNormArgs a) {
   __shared__ float part[16];
   constexpr int ROWS = TPR < NT ? NT / TPR : 1;
@@ -117,9 +116,9 @@ __global__ __launch_bounds__(TPR > NT ? TPR : NT) void rms_norm_bwd_kernel(RmsNo
       const long col = 8L * (v * TPR + t);
       const int n = static_cast<int>(min(max(a.cols - col, 0L), 8L));
       float w[8];
-      load8<T, WIDE>(static_cast<const T*>(a.x) + row * a.sum_ld + col, n, z[v]);
-      load8<Y, WIDE>(static_cast<const Y*>(a.dy) + row * a.dy_ld + col, n, u[v]);
-      load_weight<WIDE>(a, col, n, w);
+      load8<T>(static_cast<const T*>(a.x) + row * a.sum_ld + col, n, z[v]);
+      load8<Y>(static_cast<const Y*>(a.dy) + row * a.dy_ld + col, n, u[v]);
+      load_weight(a, col, n, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         z[v][i] *= r;
@@ -136,10 +135,10 @@ __global__ __launch_bounds__(TPR > NT ? TPR : NT) void rms_norm_bwd_kernel(RmsNo
       float d[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) d[i] = 0.0f;
-      if (a.dsum) load8<T, WIDE>(static_cast<const T*>(a.dsum) + row * a.dsum_ld + col, n, d);
+      if (a.dsum) load8<T>(static_cast<const T*>(a.dsum) + row * a.dsum_ld + col, n, d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) d[i] = fmaf(r, fmaf(-z[v][i], mean, u[v][i]), d[i]);
-      store8<T, WIDE>(static_cast<T*>(a.dx) + row * a.dx_ld + col, n, d);
+      store8<T>(static_cast<T*>(a.dx) + row * a.dx_ld + col, n, d);
     }
   }
   // partial row of this row group: [block * ROWS + group][cols]
@@ -148,7 +147,7 @@ __global__ __launch_bounds__(TPR > NT ? TPR : NT) void rms_norm_bwd_kernel(RmsNo
   for (int v = 0; v < V; ++v) {
     const long col = 8L * (v * TPR + t);
     const int n = static_cast<int>(min(max(a.cols - col, 0L), 8L));
-    store8<float, WIDE>(ws + col, n, dw[v]);
+    store8<float>(ws + col, n, dw[v]);
   }
 }
 
@@ -194,16 +193,12 @@ long bwd_blocks(long rows, const Shape& s) {
   return std::max(1L, std::min(need, BWD_BLOCKS / rows_of_block(s)));
 }
 
-bool wide_row(const void* p, long ld, int dtype) {
-  return !p || (ld % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0) || (dtype == 0 && ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0);
-}
-
-template <typename T, typename Y, bool WIDE, bool BWD>
+template <typename T, typename Y, bool BWD>
 hipError_t launch(const RmsNormArgs& a, const Shape& sh, unsigned blocks, hipStream_t s) {
 #define SPX_CASE(TPR, V)                                                                                          \
   if (sh.tpr == TPR && sh.v == V) {                                                                               \
-    if (BWD) hipLaunchKernelGGL((rms_norm_bwd_kernel<T, Y, TPR, V, WIDE>), dim3(blocks), dim3(TPR > NT ? TPR : NT), 0, s, a); \
-    else hipLaunchKernelGGL((rms_norm_fwd_kernel<T, Y, TPR, V, WIDE>), dim3(blocks), dim3(TPR > NT ? TPR : NT), 0, s, a);     \
+    if (BWD) hipLaunchKernelGGL((rms_norm_bwd_kernel<T, Y, TPR, V>), dim3(blocks), dim3(TPR > NT ? TPR : NT), 0, s, a); \
+    else hipLaunchKernelGGL((rms_norm_fwd_kernel<T, Y, TPR, V>), dim3(blocks), dim3(TPR > NT ? TPR : NT), 0, s, a);     \
     return hipGetLastError();                                                                                     \
   }
   SPX_CASE(64, 1)
@@ -219,12 +214,9 @@ hipError_t launch(const RmsNormArgs& a, const Shape& sh, unsigned blocks, hipStr
 }
 
 template <bool BWD>
-hipError_t dispatch(const RmsNormArgs& a, bool wide, const Shape& sh, unsigned blocks, hipStream_t s) {
-  if (a.dtype && wide) return launch<bf16_t, bf16_t, true, BWD>(a, sh, blocks, s);
-  if (a.dtype) return launch<bf16_t, bf16_t, false, BWD>(a, sh, blocks, s);
-  if (a.out_dtype && wide) return launch<float, bf16_t, true, BWD>(a, sh, blocks, s);
-  if (a.out_dtype) return launch<float, bf16_t, false, BWD>(a, sh, blocks, s);
-  return wide ? launch<float, float, true, BWD>(a, sh, blocks, s) : launch<float, float, false, BWD>(a, sh, blocks, s);
+hipError_t dispatch(const RmsNormArgs& a, const Shape& sh, unsigned blocks, hipStream_t s) {
+  if (a.dtype) return launch<bf16_t, bf16_t, BWD>(a, sh, blocks, s);
+  return a.out_dtype ? launch<float, bf16_t, BWD>(a, sh, blocks, s) : launch<float, float, BWD>(a, sh, blocks, s);
 }
 
 }  // namespace
@@ -236,20 +228,14 @@ size_t rms_norm_ws_bytes(long rows, long cols) {
 
 hipError_t rms_norm_fwd(const RmsNormArgs& a, hipStream_t s) {
   const Shape sh = shape_of(a.cols);
-  const bool wide = a.cols % 8 == 0 && wide_row(a.x, a.x_ld, a.dtype) && wide_row(a.residual, a.residual_ld, a.dtype) &&
-                    wide_row(a.sum, a.sum_ld, a.dtype) && wide_row(a.y, a.y_ld, a.out_dtype) &&
-                    reinterpret_cast<uintptr_t>(a.weight) % 16 == 0;
   const long blocks = std::min((a.rows + rows_of_block(sh) - 1) / rows_of_block(sh), 1L << 16);
-  return dispatch<false>(a, wide, sh, static_cast<unsigned>(blocks), s);
+  return dispatch<false>(a, sh, static_cast<unsigned>(blocks), s);
 }
 
 hipError_t rms_norm_bwd(const RmsNormArgs& a, hipStream_t s) {
   const Shape sh = shape_of(a.cols);
-  const bool wide = a.cols % 8 == 0 && wide_row(a.x, a.sum_ld, a.dtype) && wide_row(a.dy, a.dy_ld, a.out_dtype) &&
-                    wide_row(a.dsum, a.dsum_ld, a.dtype) && wide_row(a.dx, a.dx_ld, a.dtype) &&
-                    reinterpret_cast<uintptr_t>(a.weight) % 16 == 0;
   const long blocks = bwd_blocks(a.rows, sh);
-  if (hipError_t e = dispatch<true>(a, wide, sh, static_cast<unsigned>(blocks), s); e != hipSuccess) return e;
+  if (hipError_t e = dispatch<true>(a, sh, static_cast<unsigned>(blocks), s); e != hipSuccess) return e;
   const unsigned sums = static_cast<unsigned>((a.cols + SUM_COLS - 1) / SUM_COLS);
   hipLaunchKernelGGL(rms_norm_sum_kernel, dim3(sums), dim3(NT), 0, s, a.ws, a.dweight, a.cols,
                      static_cast<int>(blocks * rows_of_block(sh)));

@@ -10,6 +10,7 @@
 // turned to bf16 (exact, scale included) for v_mfma_f32_32x32x16_bf16 at half the
 // rate.
 #include <algorithm>
+#include <iterator>
 #include <type_traits>
 #include <utility>
 
@@ -74,96 +75,90 @@ __device__ __forceinline__ bf16x8_t widened(const i32x8_t& v, int q, float scale
 
 struct TileArgs : ProductArgs {
   uint32_t tiles_m = 0, tiles_n = 0, total = 0;   // total: tiles by slices of k
-  int k_blocks = 0, per_split = 0, splits = 1;    // blocks of 128, and of a slice
+  int k_blocks = 0, per_split = 0, splits = 1;    // blocks of 128 (1 at least), and of a slice
   float* partial = nullptr;                       // splits > 1: [slice][m][n]
-  int wide = 0;                                   // rows of out and mask allow a thread's columns at once
 };
 
+// W values of a row at any element's address, as float32 and as raw bf16.
 template <int W>
-__device__ __forceinline__ void store_whole(const ProductArgs& a, long at, const float (&v)[W]) {
-  typedef float fW __attribute__((ext_vector_type(W)));
-  typedef uint16_t hW __attribute__((ext_vector_type(W)));
-  if (a.out_dtype) {
-    if constexpr (W == 4) {
-      *reinterpret_cast<uint2*>(static_cast<bf16_t*>(a.out) + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-    } else if constexpr (W == 2) {
-      *reinterpret_cast<uint32_t*>(static_cast<bf16_t*>(a.out) + at) = pack_bf16x2(v[0], v[1]);
-    } else {
-      static_cast<bf16_t*>(a.out)[at] = f32_to_bf16(v[0]);
-    }
-  } else {
-    fW u;
+using Floats = float __attribute__((ext_vector_type(W), aligned(4)));
+template <int W>
+using Halves = uint16_t __attribute__((ext_vector_type(W), aligned(2)));
+
+template <int W>
+__device__ __forceinline__ void store_whole(float* p, const float (&v)[W]) {
+  Floats<W> u;
 #pragma unroll
-    for (int q = 0; q < W; ++q) u[q] = v[q];
-    *reinterpret_cast<fW*>(static_cast<float*>(a.out) + at) = u;
+  for (int q = 0; q < W; ++q) u[q] = v[q];
+  *reinterpret_cast<Floats<W>*>(p) = u;
+}
+template <int W>
+__device__ __forceinline__ void store_whole(bf16_t* p, const float (&v)[W]) {
+  if constexpr (W == 4) {
+    typedef uint32_t pair_t __attribute__((ext_vector_type(2), aligned(2)));
+    *reinterpret_cast<pair_t*>(p) = pair_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  } else if constexpr (W == 2) {
+    typedef uint32_t word_t __attribute__((aligned(2)));
+    *reinterpret_cast<word_t*>(p) = pack_bf16x2(v[0], v[1]);
+  } else {
+    *p = f32_to_bf16(v[0]);
+  }
+}
+__device__ __forceinline__ float value(float v) { return v; }
+__device__ __forceinline__ float value(bf16_t v) { return bf16_to_f32(v); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(bf16_t* p, float v) { *p = f32_to_bf16(v); }
+
+// n (of W) values of a row, the others 0.
+template <int W, typename T>
+__device__ __forceinline__ void load_part(const T* p, int n, float (&v)[W]) {
+  if (n >= W) {
+    typedef T vec_t __attribute__((ext_vector_type(W), aligned(sizeof(T))));
+    const vec_t u = *reinterpret_cast<const vec_t*>(p);
+#pragma unroll
+    for (int q = 0; q < W; ++q) v[q] = value(u[q]);
+  } else {
+#pragma unroll
+    for (int q = 0; q < W; ++q) v[q] = q < n ? value(p[q]) : 0.0f;
   }
 }
 
-// What becomes of W consecutive columns j .. j + W - 1 of row i, n of them there.
 template <int W>
-__device__ __forceinline__ void finish(const ProductArgs& a, bool wide, long i, long j, int n, float (&v)[W]) {
-  if (n <= 0) return;
-  const bool all = wide && n >= W;
-  typedef float fW __attribute__((ext_vector_type(W)));
-  typedef bf16_t hW __attribute__((ext_vector_type(W)));
-  const auto load = [&](const void* base, int dtype, long at, bool whole, float (&x)[W]) {
+__device__ __forceinline__ void load_bias(const ProductArgs& a, long j, int n, float (&v)[W]) {
 #pragma unroll
-    for (int q = 0; q < W; ++q) x[q] = 0.0f;
-    if (dtype) {
-      const bf16_t* p = static_cast<const bf16_t*>(base) + at;
-      if (whole) {
-        const hW u = *reinterpret_cast<const hW*>(p);
+  for (int q = 0; q < W; ++q) v[q] = 0.0f;
+  if (!a.bias) return;
+  if (a.bias_dtype) load_part<W>(static_cast<const bf16_t*>(a.bias) + j, n, v);
+  else load_part<W>(static_cast<const float*>(a.bias) + j, n, v);
+}
+
+// What becomes of the sums v of n (of W) columns, at p in out and at gate in the mask.
+template <int W, typename T>
+__device__ __forceinline__ void finish(const ProductArgs& a, const float (&bias)[W], T* p, const T* gate, int n, float (&v)[W]) {
+  const float least = a.relu ? 0.0f : -INFINITY;   // a NaN stays
 #pragma unroll
-        for (int q = 0; q < W; ++q) x[q] = bf16_to_f32(u[q]);
-      } else {
-#pragma unroll
-        for (int q = 0; q < W; ++q)
-          if (q < n) x[q] = bf16_to_f32(p[q]);
-      }
-    } else {
-      const float* p = static_cast<const float*>(base) + at;
-      if (whole) {
-        const fW u = *reinterpret_cast<const fW*>(p);
-#pragma unroll
-        for (int q = 0; q < W; ++q) x[q] = u[q];
-      } else {
-#pragma unroll
-        for (int q = 0; q < W; ++q)
-          if (q < n) x[q] = p[q];
-      }
-    }
-  };
+  for (int q = 0; q < W; ++q) {
+    v[q] += bias[q];
+    v[q] = v[q] < least ? least : v[q];
+  }
   float x[W];
-  if (a.bias) {
-    load(a.bias, a.bias_dtype, j, false, x);
-#pragma unroll
-    for (int q = 0; q < W; ++q) v[q] += x[q];
-  }
-  if (a.relu) {
-#pragma unroll
-    for (int q = 0; q < W; ++q) v[q] = v[q] < 0.0f ? 0.0f : v[q];
-  }
   if (a.mask) {
-    load(a.mask, a.out_dtype, i * a.mask_ld + j, all, x);
+    load_part<W>(gate, n, x);
 #pragma unroll
     for (int q = 0; q < W; ++q) v[q] = x[q] > 0.0f ? v[q] : 0.0f;
   }
-  const long at = i * a.out_ld + j;
   if (a.accumulate) {
-    load(a.out, 0, at, all, x);
+    load_part<W>(p, n, x);
 #pragma unroll
     for (int q = 0; q < W; ++q) v[q] += x[q];
   }
-  if (all) {
-    store_whole<W>(a, at, v);
-    return;
-  }
+  if (n >= W) {
+    store_whole<W>(p, v);
+  } else {
 #pragma unroll
-  for (int q = 0; q < W; ++q)
-    if (q < n) {
-      if (a.out_dtype) static_cast<bf16_t*>(a.out)[at + q] = f32_to_bf16(v[q]);
-      else static_cast<float*>(a.out)[at + q] = v[q];
-    }
+    for (int q = 0; q < W; ++q)
+      if (q < n) put(p + q, v[q]);
+  }
 }
 
 // One operand's part of a block tile: T * 64 rows, of which wave half w takes
@@ -175,20 +170,18 @@ __device__ __forceinline__ void finish(const ProductArgs& a, bool wide, long i, 
 template <int T>
 struct Side {
   static constexpr int ROWS = 64 * T, LOADS = 2 * T, CODES = ROWS * BK, BYTES = CODES + 256;   // scales: one load
-  __amdgpu_buffer_rsrc_t codes, scales;
+  __amdgpu_buffer_rsrc_t codes;
   int off;          // of the first direct load's row, and the lane's chunk in it
   int chunk;        // byte of that chunk in the k block
   int ld;
 
-  __device__ void init(const uint8_t* c, const uint8_t* s, long ld, long s_ld, long row0, long rows, long k, int k_blocks,
-                       int wave, int lane) {
+  __device__ __forceinline__ void init(const uint8_t* c, long ld, long row0, long rows, long k, int wave, int lane) {
     const int here = static_cast<int>(min(rows - row0, static_cast<long>(ROWS)));
     const long line = (k + 15) / 16 * 16;   // a line's bytes that are there
-    codes = make_rsrc(c + row0 * ld, (here - 1) * ld + line);
+    codes = make_rsrc(c + row0 * ld, k ? (here - 1) * ld + line : 0);
     chunk = ((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)) * 16;
     off = (8 * wave + (lane >> 3)) * T * static_cast<int>(ld) + chunk;
     this->ld = static_cast<int>(ld);
-    scales = make_rsrc(s + row0, (k_blocks - 1) * s_ld + (rows + 15) / 16 * 16 - row0);
   }
   // Load q of a k block into the stage at `lds`; from: off in that block. Rows behind the last become zeros.
   __device__ __forceinline__ void load(int q, uint32_t lds, int from, int wave) {
@@ -196,19 +189,31 @@ struct Side {
   }
 };
 
+// Blocks that share a CU's LDS, 160 KiB.
+constexpr int blocks_of_cu(int ti, int tj, int stages) {
+  return 160 * 1024 / (stages * (64 * (ti + tj) * BK + 512));
+}
+
 // 64 TI x 64 TJ of the output by four waves of 32 TI x 32 TJ.
 //
-// k goes by blocks of 128, two of them in LDS, filled by direct loads; a wave
+// k goes by blocks of 128, STAGES of them in LDS, filled by direct loads; a wave
 // multiplies one half of a block from registers while the next half comes from
 // LDS. The barrier in the middle of a block stands for both: its second half has
-// been read, so the block after next may be loaded over it, and the next block has
+// been read, so a later block may be loaded over it, and the next block has
 // arrived.
-template <int TI, int TJ, bool EXACT, int BLOCKS>
-__global__ __launch_bounds__(NT, BLOCKS) void product_tile_kernel(TileArgs a) {
+enum Epilogue : int {
+  EPI_PLAIN,   // bias and ReLU
+  EPI_READS,   // also a mask, or sums to add to
+  EPI_SLICE    // a slice's sums, as they are, to its plane
+};
+template <int TI, int TJ, bool EXACT, int STAGES, int EPILOGUE>
+__global__ __launch_bounds__(NT, blocks_of_cu(TI, TJ, STAGES)) void product_tile_kernel(TileArgs a) {
   typedef Side<TI> SA;
   typedef Side<TJ> SB;
   constexpr int STAGE = SA::BYTES + SB::BYTES;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[STAGES * STAGE];
+  static_assert((STAGES & (STAGES - 1)) == 0 && (STAGES - 1) * (SA::LOADS + SB::LOADS + 1) < 64, "counted by vmcnt");
+  const auto stage_of = [](int kb) { return (kb & (STAGES - 1)) * STAGE; };
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1, r = lane & 31, half = lane >> 5;
 
@@ -223,20 +228,24 @@ __global__ __launch_bounds__(NT, BLOCKS) void product_tile_kernel(TileArgs a) {
 
   SA sa;
   SB sb;
-  sa.init(a.a, a.a_scales, a.a_ld, a.a_scales_ld, row0, a.m, a.k, a.k_blocks, wave, lane);
-  sb.init(a.b, a.b_scales, a.b_ld, a.b_scales_ld, col0, a.n, a.k, a.k_blocks, wave, lane);
+  sa.init(a.a, a.a_ld, row0, a.m, a.k, wave, lane);
+  sb.init(a.b, a.b_ld, col0, a.n, a.k, wave, lane);
   const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)&lds[0]));
   const int line = static_cast<int>((a.k + 15) / 16 * 16);
   const auto from = [&](int off, int chunk, int kb) { return off + (kb < kb1 && kb * BK + chunk < line ? kb * BK : OOB); };
   // waves of even number load A's scale bytes, the others B's: twice the same bytes, and no branch in the loop
-  const __amdgpu_buffer_rsrc_t scales = wave & 1 ? sb.scales : sa.scales;
-  const int scales_ld = static_cast<int>(wave & 1 ? a.b_scales_ld : a.a_scales_ld);
-  const uint32_t scales_at = wave & 1 ? SA::BYTES + SB::CODES : SA::CODES;
+  const bool second = wave & 1;
+  const int scales_ld = static_cast<int>(second ? a.b_scales_ld : a.a_scales_ld);
+  const uint32_t scales_at = second ? SA::BYTES + SB::CODES : SA::CODES;
+  const long line0 = second ? col0 : row0, lines = second ? a.n : a.m;
+  const __amdgpu_buffer_rsrc_t scales =
+      make_rsrc((second ? a.b_scales : a.a_scales) + line0,
+                a.k ? (a.k_blocks - 1L) * scales_ld + (lines + 15) / 16 * 16 - line0 : 0);
   const auto load_scales = [&](int kb, uint32_t stage) {
     dma4(scales, stage + scales_at, kb < kb1 ? 4 * lane + kb * scales_ld : 0x7ffffff0);
   };
   const auto load_block = [&](int kb) {
-    const uint32_t stage = base + static_cast<uint32_t>(kb & 1) * STAGE;
+    const uint32_t stage = base + static_cast<uint32_t>(stage_of(kb));
     load_scales(kb, stage);
     const int fa0 = from(sa.off, sa.chunk, kb), fb0 = from(sb.off, sb.chunk, kb);
 #pragma unroll
@@ -254,8 +263,8 @@ __global__ __launch_bounds__(NT, BLOCKS) void product_tile_kernel(TileArgs a) {
     const i32x4_t hi = *reinterpret_cast<const i32x4_t*>(p + (low ^ (h << 6) ^ 16));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   };
-  const auto read_a = [&](int i, int kb, int h) { fa[h][i] = read(wm * TI + i, lds + (kb & 1) * STAGE, h); };
-  const auto read_b = [&](int j, int kb, int h) { fb[h][j] = read(wn * TJ + j, lds + (kb & 1) * STAGE + SA::BYTES, h); };
+  const auto read_a = [&](int i, int kb, int h) { fa[h][i] = read(wm * TI + i, lds + stage_of(kb), h); };
+  const auto read_b = [&](int j, int kb, int h) { fb[h][j] = read(wn * TJ + j, lds + stage_of(kb) + SA::BYTES, h); };
   // a lane's T scale bytes side by side
   const auto scale_bytes = [&](const uint8_t* s, auto width) {
     if constexpr (decltype(width)::value == 4) return *reinterpret_cast<const uint32_t*>(s);
@@ -264,7 +273,7 @@ __global__ __launch_bounds__(NT, BLOCKS) void product_tile_kernel(TileArgs a) {
   };
   uint32_t ea = 0, eb = 0;
   const auto read_scales = [&](int kb, uint32_t& na, uint32_t& nb) {
-    const uint8_t* s = lds + (kb & 1) * STAGE;
+    const uint8_t* s = lds + stage_of(kb);
     na = scale_bytes(s + SA::CODES + wm * 32 * TI + r * TI, std::integral_constant<int, TI>{});
     nb = scale_bytes(s + SA::BYTES + SB::CODES + wn * 32 * TJ + r * TJ, std::integral_constant<int, TJ>{});
   };
@@ -328,99 +337,99 @@ __global__ __launch_bounds__(NT, BLOCKS) void product_tile_kernel(TileArgs a) {
     constexpr int w = decltype(wc)::value, n = decltype(total)::value, per = (READS + n - 1) / n;
     each<per>([&](auto u) { read_item(std::integral_constant<int, w * per + decltype(u)::value>{}, kb, h); });
   };
-  if (kb0 < kb1) {
-    load_block(kb0);
-    load_block(kb0 + 1);
-    dma_wait<LOADS>();
-    __syncthreads();
-    each<READS>([&](auto w) { read_item(w, kb0, 0); });
-    read_scales(kb0, ea, eb);
-    for (int kb = kb0; kb + 1 < kb1; ++kb) {
-      multiply(std::integral_constant<int, 0>{}, [&](auto w, auto total) {
-        read_some(w, total, kb, 1);
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      dma_wait<0>();
-      __syncthreads();
-      const uint32_t stage = base + static_cast<uint32_t>(kb & 1) * STAGE;
-      load_scales(kb + 2, stage);
-      uint32_t na, nb;
-      read_scales(kb + 1, na, nb);
-      const int fa0 = from(sa.off, sa.chunk, kb + 2), fb0 = from(sb.off, sb.chunk, kb + 2);
-      multiply(std::integral_constant<int, 1>{}, [&](auto wc, auto total) {
-        constexpr int w = decltype(wc)::value, n = decltype(total)::value, per = (LOADS + n - 1) / n;
-        read_some(wc, total, kb + 1, 0);
-        each<per>([&](auto u) {
-          constexpr int item = w * per + decltype(u)::value;
-          if constexpr (item < SA::LOADS) sa.load(item, stage, fa0, wave);
-          else if constexpr (item < LOADS) sb.load(item - SA::LOADS, stage + SA::BYTES, fb0, wave);
-        });
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      ea = na;
-      eb = nb;
-    }
-    const int n = static_cast<int>(min(a.k - (kb1 - 1L) * BK, static_cast<long>(BK)));
-    each<READS>([&](auto w) { read_item(w, kb1 - 1, 1); });
-    if (n < BK) {
-      cut(n, 0);
-      cut(n, 1);
-    }
-    multiply(std::integral_constant<int, 0>{}, [](auto, auto) {});
-    multiply(std::integral_constant<int, 1>{}, [](auto, auto) {});
-  }
-  dma_wait<0>();   // the block's LDS may be another's when it ends
-
-  ProductArgs e = a;   // a slice's sums go to its plane as they are
-  if (a.partial) {
-    e.out = a.partial + split * a.m * a.n;
-    e.out_ld = a.n;
-    e.out_dtype = e.relu = e.accumulate = 0;
-    e.bias = e.mask = nullptr;
-  }
-  const long j = col0 + wn * 32 * TJ + r * TJ;
-  const int n = static_cast<int>(min(a.n - j, static_cast<long>(TJ)));
-  const long row_first = row0 + wm * 32 * TI + 4 * half * TI;
-  if (a.wide && col0 + SB::ROWS <= a.n && !e.mask && !e.accumulate) {   // straight stores of whole columns
-    float bias[TJ];
 #pragma unroll
-    for (int q = 0; q < TJ; ++q)
-      bias[q] = !e.bias ? 0.0f : e.bias_dtype ? bf16_to_f32(static_cast<const bf16_t*>(e.bias)[j + q])
-                                               : static_cast<const float*>(e.bias)[j + q];
-    const float least = e.relu ? 0.0f : -INFINITY;
-#pragma unroll
-    for (int i = 0; i < TI; ++i) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const long row = row_first + (8 * (v >> 2) + (v & 3)) * TI + i;
-        float x[TJ];
-#pragma unroll
-        for (int q = 0; q < TJ; ++q) {
-          x[q] = acc[i][q][v] + bias[q];
-          x[q] = x[q] < least ? least : x[q];
-        }
-        if (row < a.m) store_whole<TJ>(e, row * e.out_ld + j, x);
-      }
-    }
-    return;
-  }
-  // the general epilogue is long: a loop over rows, which pass through LDS for an index of their own
+  for (int q = 0; q < STAGES; ++q) load_block(kb0 + q);
+  dma_wait<(STAGES - 1) * (LOADS + 1)>();
   __syncthreads();
-  float* own = reinterpret_cast<float*>(lds) + wave * (16 * 64 * TJ) + lane * TJ;
-  static_assert(4 * 16 * 64 * TJ * 4 <= 2 * STAGE, "a tile row of every wave fits");
+  each<READS>([&](auto w) { read_item(w, kb0, 0); });
+  read_scales(kb0, ea, eb);
+  for (int kb = kb0; kb + 1 < kb1; ++kb) {
+    multiply(std::integral_constant<int, 0>{}, [&](auto w, auto total) {
+      read_some(w, total, kb, 1);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    dma_wait<(STAGES - 2) * (LOADS + 1)>();
+    __syncthreads();
+    const uint32_t stage = base + static_cast<uint32_t>(stage_of(kb));
+    load_scales(kb + STAGES, stage);
+    uint32_t na, nb;
+    read_scales(kb + 1, na, nb);
+    const int fa0 = from(sa.off, sa.chunk, kb + STAGES), fb0 = from(sb.off, sb.chunk, kb + STAGES);
+    multiply(std::integral_constant<int, 1>{}, [&](auto wc, auto total) {
+      constexpr int w = decltype(wc)::value, n = decltype(total)::value, per = (LOADS + n - 1) / n;
+      read_some(wc, total, kb + 1, 0);
+      each<per>([&](auto u) {
+        constexpr int item = w * per + decltype(u)::value;
+        if constexpr (item < SA::LOADS) sa.load(item, stage, fa0, wave);
+        else if constexpr (item < LOADS) sb.load(item - SA::LOADS, stage + SA::BYTES, fb0, wave);
+      });
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    ea = na;
+    eb = nb;
+  }
+  const int left = static_cast<int>(min(a.k - (kb1 - 1L) * BK, static_cast<long>(BK)));
+  each<READS>([&](auto w) { read_item(w, kb1 - 1, 1); });
+  if (left < BK) {
+    cut(left, 0);
+    cut(left, 1);
+  }
+  multiply(std::integral_constant<int, 0>{}, [](auto, auto) {});
+  multiply(std::integral_constant<int, 1>{}, [](auto, auto) {});
+  dma_wait<0>();   // the block's LDS may be another's when it ends
+  // lane: columns j .. of the rows first + (8 (v / 4) + v % 4) TI + i, `rows` of them there
+  const long j = col0 + wn * 32 * TJ + r * TJ, first = row0 + wm * 32 * TI + 4 * half * TI;
+  const int n = static_cast<int>(min(a.n - j, static_cast<long>(TJ)));
+  const int rows = static_cast<int>(min(a.m - first, 64L * TI));
+  if (n <= 0 || rows <= 0) return;
+  typedef typename std::conditional<EXACT || EPILOGUE == EPI_SLICE, float, bf16_t>::type T;
+  const long ld = EPILOGUE == EPI_SLICE ? a.n : a.out_ld;
+  T* const out = (EPILOGUE == EPI_SLICE ? reinterpret_cast<T*>(a.partial) + split * a.m * a.n : static_cast<T*>(a.out)) + first * ld + j;
+  const T* const gates = static_cast<const T*>(a.mask) + first * a.mask_ld + j;
+  float bias[TJ];
+  if constexpr (EPILOGUE != EPI_SLICE) load_bias<TJ>(a, j, n, bias);
+  const float least = a.relu ? 0.0f : -INFINITY;   // a NaN stays
   each<TI>([&](auto ic) {
     constexpr int i = decltype(ic)::value;
 #pragma unroll
-    for (int v = 0; v < 16; ++v)
+    for (int v0 = 0; v0 < 16; v0 += 4) {   // four rows, TI apart
+      const int d0 = 2 * v0 * TI + i;
+      T* const p = out + d0 * ld;
+      const T* const g = gates + d0 * a.mask_ld;
+      float gate[4][TJ], old[4][TJ];
+      if constexpr (EPILOGUE == EPI_READS) {
 #pragma unroll
-      for (int q = 0; q < TJ; ++q) own[v * 64 * TJ + q] = acc[i][q][v];
-#pragma unroll 1
-    for (int v = 0; v < 16; ++v) {
-      const long row = row_first + (8 * (v >> 2) + (v & 3)) * TI + i;
-      float x[TJ];
+        for (int v = 0; v < 4; ++v) {
+          if (d0 + v * TI >= rows) continue;
+          if (a.mask) load_part<TJ>(g + v * TI * a.mask_ld, n, gate[v]);
+          if (EXACT && a.accumulate) load_part<TJ>(p + v * TI * ld, n, old[v]);
+        }
+      }
 #pragma unroll
-      for (int q = 0; q < TJ; ++q) x[q] = own[v * 64 * TJ + q];
-      if (row < a.m) finish<TJ>(e, a.wide, row, j, n, x);
+      for (int v = 0; v < 4; ++v) {
+        if (d0 + v * TI >= rows) continue;
+        float x[TJ];
+#pragma unroll
+        for (int q = 0; q < TJ; ++q) {
+          x[q] = acc[i][q][v0 + v];
+          if constexpr (EPILOGUE != EPI_SLICE) {
+            x[q] += bias[q];
+            x[q] = x[q] < least ? least : x[q];
+          }
+          if constexpr (EPILOGUE == EPI_READS) {
+            if (a.mask) x[q] = gate[v][q] > 0.0f ? x[q] : 0.0f;
+            if (EXACT && a.accumulate) x[q] += old[v][q];
+          }
+        }
+        T* const at = p + v * TI * ld;
+        if (n >= TJ) {
+          store_whole<TJ>(at, x);
+        } else {
+#pragma unroll
+          for (int q = 0; q < TJ; ++q)
+            if (q < n) put(at + q, x[q]);
+        }
+      }
     }
   });
 }
@@ -433,56 +442,245 @@ __global__ __launch_bounds__(NT) void product_join_kernel(TileArgs a) {
   const int n = static_cast<int>(min(a.n - j, 4L));
   float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   const float* p = a.partial + i * a.n + j;
-  for (int s = 0; s < a.splits; ++s)
+  const long plane = a.m * a.n;
+  if (a.n % 4 == 0) {
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+      const float4 u = *reinterpret_cast<const float4*>(p + s * plane);
+      v[0] += u.x, v[1] += u.y, v[2] += u.z, v[3] += u.w;
+    }
+  } else {
+    for (int s = 0; s < a.splits; ++s)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (q < n) v[q] += p[static_cast<long>(s) * a.m * a.n + q];
-  finish<4>(a, a.wide, i, j, n, v);
+      for (int q = 0; q < 4; ++q)
+        if (q < n) v[q] += p[s * plane + q];
+  }
+  float bias[4];
+  load_bias<4>(a, j, n, bias);
+  const long o = i * a.out_ld + j, gate = i * a.mask_ld + j;
+  if (a.out_dtype) finish<4>(a, bias, static_cast<bf16_t*>(a.out) + o, static_cast<const bf16_t*>(a.mask) + gate, n, v);
+  else finish<4>(a, bias, static_cast<float*>(a.out) + o, static_cast<const float*>(a.mask) + gate, n, v);
 }
 
-struct Plan {
-  int ti, tj, splits, per;
+// Few rows of A (tokens): B, the weight, is read once and bounds the time. A wave
+// takes 16 RT rows of B and every W-th block of k, its codes straight from memory
+// into the registers of v_mfma_scale_f32_16x16x128_f8f6f4 (lane 16 c + r: 32
+// codes of row r), the next block's under way while it multiplies; the waves'
+// sums are added in order over LDS.
+struct Fragment {
+  i32x8_t codes;
+  int scale;
 };
 
+template <int RT, int MT, bool EXACT>
+__global__ __launch_bounds__(RT == 1 ? 1024 : 512) void product_rows_kernel(ProductArgs a, int k_blocks) {
+  extern __shared__ __attribute__((aligned(16))) float sums[];   // [wave][RT][MT][lane][4]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int r = lane & 15, c = lane >> 4;
+  const long j0 = static_cast<long>(blockIdx.x) * 16 * RT;
+  const uint8_t *pb[RT], *pa[MT];
+  long rb[RT], ra[MT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    rb[i] = min(j0 + 16 * i + r, a.n - 1);
+    pb[i] = a.b + rb[i] * a.b_ld + 32 * c;
+  }
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    ra[i] = min(16L * i + r, a.m - 1);
+    pa[i] = a.a + ra[i] * a.a_ld + 32 * c;
+  }
+  struct Block {
+    Fragment b[RT], a[MT];
+  };
+  const auto load = [&](Block& f, int kb) {
+    const long at = static_cast<long>(kb) * BK, left = a.k - at - 32 * c;   // codes from the lane's first on
+#pragma unroll
+    for (int i = 0; i < RT + MT; ++i) {
+      Fragment& t = i < RT ? f.b[i] : f.a[i - RT];
+      const uint8_t* p = (i < RT ? pb[i] : pa[i - RT]) + at;
+      i32x4_t h[2] = {};
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        if (left > 16 * q) h[q] = *reinterpret_cast<const i32x4_t*>(p + 16 * q);
+      }
+      t.codes = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      t.scale = i < RT ? a.b_scales[kb * a.b_scales_ld + rb[i]] : a.a_scales[kb * a.a_scales_ld + ra[i - RT]];
+    }
+  };
+  const auto cut = [&](Block& f, int kb) {   // bytes behind k are not the tensor's
+    const long left = a.k - static_cast<long>(kb) * BK - 32 * c;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int keep = static_cast<int>(min(max(left - 4 * q, 0L), 4L));
+      const int mask = static_cast<int>(keep == 4 ? 0xffffffffu : (1u << (8 * keep)) - 1u);
+#pragma unroll
+      for (int i = 0; i < RT; ++i) f.b[i].codes[q] &= mask;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) f.a[i].codes[q] &= mask;
+    }
+  };
+  f32x4_t acc[RT][MT] = {};
+  const auto multiply = [&](const Block& f) {
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        if constexpr (EXACT) {
+          const float sb = __uint_as_float(static_cast<uint32_t>(f.b[i].scale) << 23);
+          const float sa = __uint_as_float(static_cast<uint32_t>(f.a[m].scale) << 23);
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            acc[i][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(f.b[i].codes, q, sb), widened(f.a[m].codes, q, sa),
+                                                                acc[i][m], 0, 0, 0);
+        } else {
+          acc[i][m] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f.b[i].codes, f.a[m].codes, acc[i][m], 0, 0, 0,
+                                                                       f.b[i].scale, 0, f.a[m].scale);
+        }
+      }
+  };
+  Block now, next;
+  if (wave < k_blocks) load(now, wave);
+  for (int kb = wave; kb < k_blocks; kb += waves) {
+    if (kb + waves < k_blocks) load(next, kb + waves);
+    if ((kb + 1L) * BK > a.k) cut(now, kb);
+    multiply(now);
+    now = next;
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) *reinterpret_cast<f32x4_t*>(sums + (((wave * RT + i) * MT + m) * 64 + lane) * 4) = acc[i][m];
+  __syncthreads();
+  // lane 16 c + r of tile (i, m) holds columns j0 + 16 i + 4 c .. + 3 of row 16 m + r
+  for (int t = threadIdx.x; t < RT * MT * 64; t += blockDim.x) {
+    const int l = t & 63, m = (t >> 6) % MT, i = (t >> 6) / MT;
+    const long row = 16 * m + (l & 15), j = j0 + 16 * i + 4 * (l >> 4);
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int w = 0; w < waves; ++w) {
+      const f32x4_t u = *reinterpret_cast<const f32x4_t*>(sums + (w * RT * MT * 64 + t) * 4);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] += u[q];
+    }
+    const int n = static_cast<int>(min(a.n - j, 4L));
+    if (row >= a.m || n <= 0) continue;
+    float bias[4];
+    load_bias<4>(a, j, n, bias);
+    typedef typename std::conditional<EXACT, float, bf16_t>::type T;
+    finish<4>(a, bias, static_cast<T*>(a.out) + row * a.out_ld + j, static_cast<const T*>(a.mask) + row * a.mask_ld + j, n, v);
+  }
+}
+
+constexpr long ROWS_MAX = 32;   // rows of A that this kernel takes
+
+template <int MT, bool EXACT>
+hipError_t launch_rows(const ProductArgs& a, hipStream_t s) {
+  const int k_blocks = static_cast<int>((a.k + BK - 1) / BK);
+  // 16 RT rows a block: a block for each CU at least where there are so many rows
+  const int rt = a.n >= 256 * 64 ? 4 : a.n >= 256 * 32 ? 2 : 1;
+  const int waves = k_blocks <= 4 ? 4 : rt == 1 && k_blocks > 8 ? 16 : 8;
+  const unsigned blocks = static_cast<unsigned>((a.n + 16 * rt - 1) / (16 * rt));
+  const size_t lds = static_cast<size_t>(waves) * rt * MT * 1024;
+  if (rt == 4) hipLaunchKernelGGL((product_rows_kernel<4, MT, EXACT>), dim3(blocks), dim3(64 * waves), lds, s, a, k_blocks);
+  else if (rt == 2) hipLaunchKernelGGL((product_rows_kernel<2, MT, EXACT>), dim3(blocks), dim3(64 * waves), lds, s, a, k_blocks);
+  else hipLaunchKernelGGL((product_rows_kernel<1, MT, EXACT>), dim3(blocks), dim3(64 * waves), lds, s, a, k_blocks);
+  return hipGetLastError();
+}
+
+// Kernels of square block tiles: 64 t rows and columns, stages of k in LDS, and
+// what they cost by measurement (us): fixed for a block's start and end, and a k
+// block with one, or as many as fit, blocks of the kind on a CU.
+struct Variant {
+  int t, stages, per_cu;
+  double fixed, step_alone, step_full;
+};
+constexpr Variant VARIANTS[] = {{4, 2, 1, 10.3, 1.43, 1.43}, {2, 2, 2, 4.5, 0.62, 0.93}, {2, 4, 1, 3.9, 0.50, 0.50},
+                                {1, 4, 2, 2.2, 0.22, 0.375}};
+constexpr Variant VARIANTS_EXACT[] = {{4, 2, 1, 12.5, 2.70, 2.70}, {2, 2, 2, 4.6, 0.84, 1.54}, {1, 4, 2, 2.5, 0.385, 0.575}};
+
+struct Plan {
+  int variant = 0, splits = 1, per_split = 1;
+};
+
+constexpr int MAX_SPLITS = 16;
+
+// The kernel and the slices of k of the least modelled time: rounds of blocks over
+// the 256 CUs, and for slices a second launch that reads their planes.
 Plan plan_of(long m, long n, long k, bool exact) {
-  const auto tiles = [&](int ti, int tj) { return ((m + 64 * ti - 1) / (64 * ti)) * ((n + 64 * tj - 1) / (64 * tj)); };
-  const int blocks = static_cast<int>((k + BK - 1) / BK);
-  Plan p{2, 2, 1, std::max(blocks, 1)};
-  if (!exact && tiles(4, 4) >= 192) p.ti = p.tj = 4;
-  else if (tiles(2, 2) < 256) p.ti = p.tj = 1;
-  return p;
+  const int k_blocks = static_cast<int>(std::max((k + BK - 1) / BK, 1L));
+  Plan best;
+  double least = 1e300;
+  const int variants = exact ? std::size(VARIANTS_EXACT) : std::size(VARIANTS);
+  for (int i = 0; i < variants; ++i) {
+    const Variant& v = exact ? VARIANTS_EXACT[i] : VARIANTS[i];
+    const long tiles = ((m + 64 * v.t - 1) / (64 * v.t)) * ((n + 64 * v.t - 1) / (64 * v.t));
+    for (int splits : {1, 2, 3, 4, 6, 8, 12, MAX_SPLITS}) {
+      if (splits > 1 && 2 * splits > k_blocks) break;
+      const int per = (k_blocks + splits - 1) / splits, used = (k_blocks + per - 1) / per;
+      const long slots = 256L * v.per_cu, work = tiles * used, rounds = work / slots, rest = work - rounds * slots;
+      const double full = v.fixed + per * v.step_full;
+      double t = rounds * full;
+      if (rest > 256) t += full;
+      else if (rest) t += v.fixed + per * v.step_alone;
+      if (used > 1) t += 2.0 + 2.0 * used * m * n * 4 / 5e6;
+      if (t < least) {
+        least = t;
+        best.variant = i;
+        best.splits = used;
+        best.per_split = per;
+      }
+    }
+  }
+  return best;
 }
 
-bool wide(const void* p, long ld, int dtype, int w) {
-  return !p || (ld % w == 0 && reinterpret_cast<uintptr_t>(p) % ((dtype ? 2 : 4) * w) == 0);
-}
-
-template <int TI, int TJ, bool EXACT, int BLOCKS>
+template <int TI, int TJ, bool EXACT, int STAGES>
 hipError_t launch(TileArgs a, hipStream_t s) {
   a.tiles_m = static_cast<uint32_t>((a.m + 64 * TI - 1) / (64 * TI));
   a.tiles_n = static_cast<uint32_t>((a.n + 64 * TJ - 1) / (64 * TJ));
   a.total = a.tiles_m * a.tiles_n * a.splits;
-  const int w = a.splits > 1 ? 4 : TJ;
-  a.wide = wide(a.out, a.out_ld, a.out_dtype, w) && wide(a.mask, a.mask_ld, a.out_dtype, w);
-  hipLaunchKernelGGL((product_tile_kernel<TI, TJ, EXACT, BLOCKS>), dim3((a.total + 7) / 8 * 8), dim3(NT), 0, s, a);
+  const dim3 grid((a.total + 7) / 8 * 8);
+  if (a.partial) hipLaunchKernelGGL((product_tile_kernel<TI, TJ, EXACT, STAGES, EPI_SLICE>), grid, dim3(NT), 0, s, a);
+  else if (a.mask || a.accumulate) hipLaunchKernelGGL((product_tile_kernel<TI, TJ, EXACT, STAGES, EPI_READS>), grid, dim3(NT), 0, s, a);
+  else hipLaunchKernelGGL((product_tile_kernel<TI, TJ, EXACT, STAGES, EPI_PLAIN>), grid, dim3(NT), 0, s, a);
+  return hipGetLastError();
+}
+
+template <bool EXACT>
+hipError_t product_of(const ProductArgs& args, hipStream_t s) {
+  if (args.m <= 16) return launch_rows<1, EXACT>(args, s);
+  if (args.m <= ROWS_MAX) return launch_rows<2, EXACT>(args, s);
+  const Plan p = plan_of(args.m, args.n, args.k, EXACT);
+  TileArgs a;
+  static_cast<ProductArgs&>(a) = args;
+  a.k_blocks = static_cast<int>(std::max((args.k + BK - 1) / BK, 1L));
+  a.splits = p.splits;
+  a.per_split = p.per_split;
+  if (p.splits > 1) a.partial = args.ws;
+  const Variant& v = EXACT ? VARIANTS_EXACT[p.variant] : VARIANTS[p.variant];
+  hipError_t e;
+  if (v.t == 4) e = launch<4, 4, EXACT, 2>(a, s);
+  else if (v.t == 1) e = launch<1, 1, EXACT, 4>(a, s);
+  else if (EXACT || v.stages == 2) e = launch<2, 2, EXACT, 2>(a, s);
+  else e = launch<2, 2, EXACT, EXACT ? 2 : 4>(a, s);
+  if (e != hipSuccess || p.splits == 1) return e;
+  const long threads = a.m * ((a.n + 3) / 4);
+  hipLaunchKernelGGL(product_join_kernel, dim3(static_cast<unsigned>((threads + NT - 1) / NT)), dim3(NT), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t product_ws_bytes(long, long, long) { return 0; }
-
-hipError_t product(const ProductArgs& args, hipStream_t s) {
-  const bool exact = args.out_dtype == 0;
-  const Plan p = plan_of(args.m, args.n, args.k, exact);
-  TileArgs a;
-  static_cast<ProductArgs&>(a) = args;
-  a.k_blocks = static_cast<int>((args.k + BK - 1) / BK);
-  a.splits = p.splits;
-  a.per_split = p.per;
-  if (exact) return p.ti == 2 ? launch<2, 2, true, 2>(a, s) : launch<1, 1, true, 4>(a, s);
-  if (p.ti == 4) return launch<4, 4, false, 1>(a, s);
-  return p.ti == 2 ? launch<2, 2, false, 2>(a, s) : launch<1, 1, false, 4>(a, s);
+size_t product_ws_bytes(long m, long n, long k) {
+  if (m <= ROWS_MAX || n == 0) return 0;
+  size_t planes = 0;
+  for (bool exact : {false, true}) {
+    const int splits = plan_of(m, n, k, exact).splits;
+    if (splits > 1) planes = std::max(planes, static_cast<size_t>(splits));
+  }
+  return planes * m * n * sizeof(float);
 }
+
+hipError_t product(const ProductArgs& a, hipStream_t s) { return a.out_dtype ? product_of<false>(a, s) : product_of<true>(a, s); }
 
 }  // namespace spx
