@@ -509,7 +509,7 @@ typedef struct {
   int32_t weight_dtype;      /* of weight [cols] */
   float eps;                 /* finite, > 0 */
   int32_t reserved;          /* 0 */
-  int64_t rows, cols;        /* rows below 2^31, cols 1 .. 65536 */
+  int64_t rows, cols;        /* rows below 2^31, cols 1 .. 32768 */
   int64_t x_ld, residual_ld, sum_ld, y_ld;   /* elements between rows: >= cols, at most 2^40; */
   int64_t codes_ld, scales_ld;               /* looked at where their tensor is given. A backward takes */
   int64_t dy_ld, dsum_ld, dx_ld;             /* sum_ld for h */

@@ -233,7 +233,7 @@ struct RmsNormArgs {
   int dtype = 0, out_dtype = 0, weight_dtype = 0;
   float eps = 0.0f;
 };
-constexpr long RMS_NORM_COLS = 65536;   // longest row: its block keeps it in registers
+constexpr long RMS_NORM_COLS = 32768;   // longest row: its block keeps it in registers
 size_t rms_norm_ws_bytes(long rows, long cols);
 hipError_t rms_norm_fwd(const RmsNormArgs& a, hipStream_t s);
 hipError_t rms_norm_bwd(const RmsNormArgs& a, hipStream_t s);

@@ -428,7 +428,7 @@ RmsNormArgs rms_norm_args(const spectrain_rms_norm_desc* desc) {
   if (d.reserved != 0) fail("reserved must be 0");
   if (!(d.eps > 0.0f) || !std::isfinite(d.eps)) fail("eps must be finite and > 0");
   if (d.rows < 0 || d.rows >= int64_t{1} << 31) fail("rows must lie in [0, 2^31)");
-  if (d.cols < 1 || d.cols > RMS_NORM_COLS) fail("cols must lie in [1, 65536]");
+  if (d.cols < 1 || d.cols > RMS_NORM_COLS) fail("cols must lie in [1, 32768]");
   RmsNormArgs a;
   a.rows = d.rows;
   a.cols = d.cols;

@@ -5,6 +5,7 @@ Device buffers are passed as torch tensors (their data pointers) and streams
 as torch.cuda.Stream objects; host arrays as float32 NumPy arrays.
 """
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -568,38 +569,79 @@ def checkpoint_restore(codes, scales, out, stream=None):
 
 
 # ---- linear layers in 8 bits ----
+#
+# A small call is host time before anything else, so a call's descriptor is made
+# once for its sizes, types and strides and then only read (by any thread).
+
+_codes = {}   # torch dtype: code
+
+
+def _code(t, what):
+    c = _codes.get(t.dtype)
+    if c is None:
+        c = _codes[t.dtype] = _dtype_code(t, what)
+    return c
+
+
+def _wrong(t, shape, dtype, device, what):
+    if t.device != device:
+        raise ValueError(f"{what} must be on {device}, got {t.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
+    raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
 
 def _matrix(t, shape, dtype, device, what):
     """Pointer and ld of a [rows, cols] tensor with a contiguous last dimension (None: absent)."""
     if t is None:
         return None, 0
-    if t.device != device:
-        raise ValueError(f"{what} must be on {device}, got {t.device}")
-    if t.dtype != dtype:
-        raise ValueError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    rows, cols = shape
-    if cols > 1 and t.stride(1) != 1:
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        _wrong(t, shape, dtype, device, what)
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
         raise ValueError(f"{what} must be contiguous in its last dimension")
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(cols, 1)
+    return t.data_ptr(), ld if shape[0] > 1 else max(shape[1], 1)
 
 
-def _lines(t, shape, device, what):
+def _vector(t, n, device, what):
+    """Pointer and dtype code of a contiguous [n] tensor of bf16 or float32."""
+    if t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what} must be contiguous ({n},) on {device}, got {tuple(t.shape)} on {t.device}")
+    return t.data_ptr(), _code(t, what)
+
+
+def _floats(t, n, device, what):
+    """Pointer of a contiguous float32 [n] tensor (None: absent)."""
+    if t is None:
+        return None
+    p, code = _vector(t, n, device, what)
+    if code != FP32:
+        raise ValueError(f"{what} must be torch.float32, got {t.dtype}")
+    return p
+
+
+def _lines(t, lines, length, device, what):
     """Pointer and ld of codes or scale bytes; one line's ld, which torch may have lost, is its length rounded up."""
     import torch
-    p, ld = _matrix(t, shape, torch.uint8, device, what)
-    return p, -(-shape[1] // 16) * 16 if shape[0] <= 1 else ld
+    p, ld = _matrix(t, (lines, length), torch.uint8, device, what)
+    return p, ld if lines > 1 else (length + 15) // 16 * 16
 
 
 def _blocks(codes, scales, rows, cols, device, what):
     """Pointers and ld of codes [rows, cols] and scales [ceil(cols / 128), rows] (both None: absent)."""
-    if (codes is None) != (scales is None):
-        raise ValueError(f"{what} and their scales go together")
-    if codes is None:
+    if codes is None or scales is None:
+        if codes is not scales:
+            raise ValueError(f"{what} and their scales go together")
         return None, 0, None, 0
-    return (*_lines(codes, (rows, cols), device, what),
-            *_lines(scales, (-(-cols // BLOCK_COLS), rows), device, what + " scales"))
+    return (*_lines(codes, rows, cols, device, what),
+            *_lines(scales, (cols + BLOCK_COLS - 1) // BLOCK_COLS, rows, device, what + " scales"))
+
+
+@functools.lru_cache(maxsize=512)
+def _described(struct, *fields):
+    """A descriptor of these fields, and the reference to it that calls pass."""
+    d = struct(ABI_VERSION, *fields)
+    return d, ctypes.byref(d)
 
 
 def blocks_empty(rows, cols, device="cuda"):
@@ -618,12 +660,12 @@ def blocks_pack(x, codes=None, scales=None, transposed=None, transposed_scales=N
     if x.dim() != 2:
         raise ValueError(f"x must be [rows, cols], got {tuple(x.shape)}")
     rows, cols = x.shape
-    xp, ld = _matrix(x, x.shape, x.dtype, x.device, "x")
-    cp, cl, sp, sl = _blocks(codes, scales, rows, cols, x.device, "codes")
-    tp, tl, up, ul = _blocks(transposed, transposed_scales, cols, rows, x.device, "transposed")
-    d = BlocksDesc(ABI_VERSION, _dtype_code(x, "x"), BLOCKS_TILES if tiles else BLOCKS_ROWS, 0, rows, cols, ld, cl, sl,
-                   tl, ul)
-    _on(x.device, stream, lib().spectrain_blocks_pack, ctypes.byref(d), xp, cp, sp, tp, up)
+    dev = x.device
+    xp, ld = _matrix(x, x.shape, x.dtype, dev, "x")
+    cp, cl, sp, sl = _blocks(codes, scales, rows, cols, dev, "codes")
+    tp, tl, up, ul = _blocks(transposed, transposed_scales, cols, rows, dev, "transposed")
+    _, d = _described(BlocksDesc, _code(x, "x"), BLOCKS_TILES if tiles else BLOCKS_ROWS, 0, rows, cols, ld, cl, sl, tl, ul)
+    _on(dev, stream, lib().spectrain_blocks_pack, d, xp, cp, sp, tp, up)
 
 
 def blocks_restore(codes, scales, out, stream=None):
@@ -631,10 +673,11 @@ def blocks_restore(codes, scales, out, stream=None):
     if out.dim() != 2:
         raise ValueError(f"out must be [rows, cols], got {tuple(out.shape)}")
     rows, cols = out.shape
-    op, ld = _matrix(out, out.shape, out.dtype, out.device, "out")
-    cp, cl, sp, sl = _blocks(codes, scales, rows, cols, out.device, "codes")
-    d = BlocksDesc(ABI_VERSION, _dtype_code(out, "out"), BLOCKS_ROWS, 0, rows, cols, ld, cl, sl, 0, 0)
-    _on(out.device, stream, lib().spectrain_blocks_restore, ctypes.byref(d), cp, sp, op)
+    dev = out.device
+    op, ld = _matrix(out, out.shape, out.dtype, dev, "out")
+    cp, cl, sp, sl = _blocks(codes, scales, rows, cols, dev, "codes")
+    _, d = _described(BlocksDesc, _code(out, "out"), BLOCKS_ROWS, 0, rows, cols, ld, cl, sl, 0, 0)
+    _on(dev, stream, lib().spectrain_blocks_restore, d, cp, sp, op)
 
 
 class RmsNorm:
@@ -645,13 +688,10 @@ class RmsNorm:
     def __init__(self, cols, eps=1e-6):
         self.cols, self.eps = cols, eps
 
-    def _desc(self, rows, dtype, out_dtype, weight_dtype):
-        d = RmsNormDesc(ABI_VERSION, dtype, out_dtype, weight_dtype, self.eps, 0, rows, self.cols)
-        return d
-
     def workspace_bytes(self, rows):
         n = ctypes.c_size_t()
-        _check(lib().spectrain_rms_norm_workspace(ctypes.byref(self._desc(rows, FP32, FP32, FP32)), ctypes.byref(n)))
+        _, d = _described(RmsNormDesc, FP32, FP32, FP32, self.eps, 0, rows, self.cols)
+        _check(lib().spectrain_rms_norm_workspace(d, ctypes.byref(n)))
         return n.value
 
     def workspace(self, rows, device="cuda"):
@@ -659,43 +699,40 @@ class RmsNorm:
         import torch
         return torch.empty(max(256, self.workspace_bytes(rows)), dtype=torch.uint8, device=device)
 
-    def _checked(self, x, weight, what):
+    def _rows(self, x, what):
         if x.dim() != 2 or x.shape[1] != self.cols:
             raise ValueError(f"{what} must be [rows, {self.cols}], got {tuple(x.shape)}")
-        if tuple(weight.shape) != (self.cols,) or not weight.is_contiguous() or weight.device != x.device:
-            raise ValueError(f"weight must be contiguous ({self.cols},) on {x.device}, got {tuple(weight.shape)} on "
-                             f"{weight.device}")
-        return _dtype_code(x, what), _dtype_code(weight, "weight")
+        return x.shape, x.dtype, x.device, _code(x, what)
 
     def forward(self, x, weight, y=None, *, residual=None, sum=None, codes=None, scales=None, rstd=None, stream=None):
         """sum = x + residual (rounded to their type); its norm to y, to blocks of 128 (codes, scales), or both; rstd
         float32 [rows] as the backward takes it (None: not wanted)."""
-        dt, wt = self._checked(x, weight, "x")
-        shape, dev = x.shape, x.device
-        d = self._desc(shape[0], dt, dt if y is None else _dtype_code(y, "y"), wt)
-        xp, d.x_ld = _matrix(x, shape, x.dtype, dev, "x")
-        rp, d.residual_ld = _matrix(residual, shape, x.dtype, dev, "residual")
-        sp, d.sum_ld = _matrix(sum, shape, x.dtype, dev, "sum")
-        yp, d.y_ld = _matrix(y, shape, None if y is None else y.dtype, dev, "y")
-        cp, d.codes_ld, lp, d.scales_ld = _blocks(codes, scales, *shape, dev, "codes")
-        qp = _side(rstd, (shape[0],), "torch.float32", dev, "rstd")
-        _on(dev, stream, lib().spectrain_rms_norm_forward, ctypes.byref(d), xp, rp, weight.data_ptr(), sp, yp, cp, lp, qp)
+        shape, dtype, dev, dt = self._rows(x, "x")
+        wp, wt = _vector(weight, self.cols, dev, "weight")
+        xp, xl = _matrix(x, shape, dtype, dev, "x")
+        rp, rl = _matrix(residual, shape, dtype, dev, "residual")
+        sp, sl = _matrix(sum, shape, dtype, dev, "sum")
+        yp, yl = (None, 0) if y is None else _matrix(y, shape, y.dtype, dev, "y")
+        cp, cl, lp, ll = _blocks(codes, scales, *shape, dev, "codes")
+        qp = _floats(rstd, shape[0], dev, "rstd")
+        _, d = _described(RmsNormDesc, dt, dt if y is None else _code(y, "y"), wt, self.eps, 0, *shape, xl, rl, sl, yl, cl,
+                          ll, 0, 0, 0)
+        _on(dev, stream, lib().spectrain_rms_norm_forward, d, xp, rp, wp, sp, yp, cp, lp, qp)
 
     def backward(self, dy, h, weight, rstd, dx, dweight, *, dsum=None, workspace, stream=None):
         """dx (of x and of the residual alike) and dweight float32 [cols], overwritten, from dy, the forward's sum h
         and rstd, and the gradient dsum that reaches h elsewhere."""
-        dt, wt = self._checked(h, weight, "h")
-        shape, dev = h.shape, h.device
-        d = self._desc(shape[0], dt, _dtype_code(dy, "dy"), wt)
-        gp, d.dy_ld = _matrix(dy, shape, dy.dtype, dev, "dy")
-        hp, d.sum_ld = _matrix(h, shape, h.dtype, dev, "h")
-        sp, d.dsum_ld = _matrix(dsum, shape, h.dtype, dev, "dsum")
-        xp, d.dx_ld = _matrix(dx, shape, h.dtype, dev, "dx")
-        rp = _side(rstd, (shape[0],), "torch.float32", dev, "rstd")
-        wp = _side(dweight, (self.cols,), "torch.float32", dev, "dweight")
+        shape, dtype, dev, dt = self._rows(h, "h")
+        wp, wt = _vector(weight, self.cols, dev, "weight")
+        gp, gl = _matrix(dy, shape, dy.dtype, dev, "dy")
+        hp, hl = _matrix(h, shape, dtype, dev, "h")
+        sp, sl = _matrix(dsum, shape, dtype, dev, "dsum")
+        xp, xl = _matrix(dx, shape, dtype, dev, "dx")
+        rp = _floats(rstd, shape[0], dev, "rstd")
+        vp = _floats(dweight, self.cols, dev, "dweight")
         kp, kn = _scratch(workspace, dev)
-        _on(dev, stream, lib().spectrain_rms_norm_backward, ctypes.byref(d), gp, hp, weight.data_ptr(), rp, sp, xp, wp,
-            kp, kn)
+        _, d = _described(RmsNormDesc, dt, _code(dy, "dy"), wt, self.eps, 0, *shape, 0, 0, hl, 0, 0, 0, gl, sl, xl)
+        _on(dev, stream, lib().spectrain_rms_norm_backward, d, gp, hp, wp, rp, sp, xp, vp, kp, kn)
 
 
 class Product:
@@ -706,12 +743,10 @@ class Product:
         self.m, self.n, self.k = m, n, k
         self.relu, self.accumulate = int(bool(relu)), int(bool(accumulate))
 
-    def _desc(self, out_dtype):
-        return ProductDesc(ABI_VERSION, out_dtype, FP32, self.relu, self.accumulate, 0, self.m, self.n, self.k)
-
     def workspace_bytes(self):
         n = ctypes.c_size_t()
-        _check(lib().spectrain_product_workspace(ctypes.byref(self._desc(FP32)), ctypes.byref(n)))
+        _, d = _described(ProductDesc, FP32, FP32, self.relu, self.accumulate, 0, self.m, self.n, self.k)
+        _check(lib().spectrain_product_workspace(d, ctypes.byref(n)))
         return n.value
 
     def workspace(self, device="cuda"):
@@ -722,15 +757,12 @@ class Product:
     def apply(self, a, a_scales, b, b_scales, out, *, bias=None, mask=None, workspace, stream=None):
         """out = A B^T (out += with accumulate). Returns out."""
         dev, m, n, k = out.device, self.m, self.n, self.k
-        d = self._desc(_dtype_code(out, "out"))
-        op, d.out_ld = _matrix(out, (m, n), out.dtype, dev, "out")
-        mp, d.mask_ld = _matrix(mask, (m, n), out.dtype, dev, "mask")
-        ap, d.a_ld, sp, d.a_scales_ld = _blocks(a, a_scales, m, k, dev, "a")
-        bp, d.b_ld, tp, d.b_scales_ld = _blocks(b, b_scales, n, k, dev, "b")
-        bias_p = None
-        if bias is not None:
-            d.bias_dtype = _dtype_code(bias, "bias")
-            bias_p = _side(bias, (n,), str(bias.dtype), dev, "bias")
+        op, ol = _matrix(out, (m, n), out.dtype, dev, "out")
+        mp, ml = _matrix(mask, (m, n), out.dtype, dev, "mask")
+        ap, al, sp, sl = _blocks(a, a_scales, m, k, dev, "a")
+        bp, bl, tp, tl = _blocks(b, b_scales, n, k, dev, "b")
+        vp, vt = (None, FP32) if bias is None else _vector(bias, n, dev, "bias")
         wp, wn = _scratch(workspace, dev)
-        _on(dev, stream, lib().spectrain_product, ctypes.byref(d), ap, sp, bp, tp, bias_p, mp, op, wp, wn)
+        _, d = _described(ProductDesc, _code(out, "out"), vt, self.relu, self.accumulate, 0, m, n, k, al, sl, bl, tl, ol, ml)
+        _on(dev, stream, lib().spectrain_product, d, ap, sp, bp, tp, vp, mp, op, wp, wn)
         return out

@@ -115,7 +115,7 @@ def _backward(d, dy=P, h=2 * P, w=3 * P, rstd=4 * P, dsum=5 * P, dx=6 * P, dw=7 
     (dict(rows=-1), "rows"),
     (dict(rows=1 << 31), "rows"),
     (dict(cols=0), "cols"),
-    (dict(cols=65537), "cols"),
+    (dict(cols=32769), "cols"),
     (dict(sum_ld=299), "sum_ld"),
 ])
 def test_norm_refusals(change, needle):
