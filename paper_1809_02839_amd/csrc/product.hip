@@ -389,49 +389,82 @@ __global__ __launch_bounds__(NT, blocks_of_cu(TI, TJ, STAGES)) void product_tile
   float bias[TJ];
   if constexpr (EPILOGUE != EPI_SLICE) load_bias<TJ>(a, j, n, bias);
   const float least = a.relu ? 0.0f : -INFINITY;   // a NaN stays
-  each<TI>([&](auto ic) {
-    constexpr int i = decltype(ic)::value;
+  const auto row_at = [](int i, int v) { return (8 * (v >> 2) + (v & 3)) * TI + i; };   // row v of tile i, from first
+  if (EPILOGUE != EPI_READS || n < TJ) {
+    each<TI>([&](auto ic) {
+      constexpr int i = decltype(ic)::value;
 #pragma unroll
-    for (int v0 = 0; v0 < 16; v0 += 4) {   // four rows, TI apart
-      const int d0 = 2 * v0 * TI + i;
-      T* const p = out + d0 * ld;
-      const T* const g = gates + d0 * a.mask_ld;
-      float gate[4][TJ], old[4][TJ];
-      if constexpr (EPILOGUE == EPI_READS) {
+      for (int v0 = 0; v0 < 16; v0 += 4) {   // four rows, TI apart
+        const int d0 = row_at(i, v0);
+        T* const p = out + d0 * ld;
+        const T* const g = gates + d0 * a.mask_ld;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
           if (d0 + v * TI >= rows) continue;
-          if (a.mask) load_part<TJ>(g + v * TI * a.mask_ld, n, gate[v]);
-          if (EXACT && a.accumulate) load_part<TJ>(p + v * TI * ld, n, old[v]);
+          T* const at = p + v * TI * ld;
+          float x[TJ];
+#pragma unroll
+          for (int q = 0; q < TJ; ++q) {
+            x[q] = acc[i][q][v0 + v];
+            if constexpr (EPILOGUE != EPI_SLICE) {
+              x[q] += bias[q];
+              x[q] = x[q] < least ? least : x[q];
+            }
+            if constexpr (EPILOGUE == EPI_READS) {   // columns at the edge
+              if (q >= n) continue;
+              if (a.mask) x[q] = value(g[v * TI * a.mask_ld + q]) > 0.0f ? x[q] : 0.0f;
+              if (EXACT && a.accumulate) x[q] += value(at[q]);
+            }
+          }
+          if (n >= TJ) {
+            store_whole<TJ>(at, x);
+          } else {
+#pragma unroll
+            for (int q = 0; q < TJ; ++q)
+              if (q < n) put(at + q, x[q]);
+          }
         }
       }
+    });
+    return;
+  }
+  if constexpr (EPILOGUE == EPI_READS) {   // what a group of rows reads is asked for a group before
+    constexpr int GROUP = EXACT ? 8 : 16, GROUPS = TI * 16 / GROUP;
+    typedef T vec_t __attribute__((ext_vector_type(TJ), aligned(sizeof(T))));
+    vec_t gate[2][GROUP], old[2][EXACT ? GROUP : 1];
+    const auto ask = [&](auto gc) {
+      constexpr int g = decltype(gc)::value;
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        if (d0 + v * TI >= rows) continue;
+      for (int v = 0; v < GROUP; ++v) {
+        const long d = min(row_at(g * GROUP / 16, g * GROUP % 16 + v), rows - 1);
+        if (a.mask) gate[g & 1][v] = *reinterpret_cast<const vec_t*>(gates + d * a.mask_ld);
+        if constexpr (EXACT) {
+          if (a.accumulate) old[g & 1][v] = *reinterpret_cast<const vec_t*>(out + d * ld);
+        }
+      }
+    };
+    ask(std::integral_constant<int, 0>{});
+    each<GROUPS>([&](auto gc) {
+      constexpr int g = decltype(gc)::value, i = g * GROUP / 16;
+      if constexpr (g + 1 < GROUPS) ask(std::integral_constant<int, g + 1>{});
+#pragma unroll
+      for (int v = 0; v < GROUP; ++v) {
+        const int d = row_at(i, g * GROUP % 16 + v);
+        if (d >= rows) continue;
         float x[TJ];
 #pragma unroll
         for (int q = 0; q < TJ; ++q) {
-          x[q] = acc[i][q][v0 + v];
-          if constexpr (EPILOGUE != EPI_SLICE) {
-            x[q] += bias[q];
-            x[q] = x[q] < least ? least : x[q];
-          }
-          if constexpr (EPILOGUE == EPI_READS) {
-            if (a.mask) x[q] = gate[v][q] > 0.0f ? x[q] : 0.0f;
-            if (EXACT && a.accumulate) x[q] += old[v][q];
+          x[q] = acc[i][q][g * GROUP % 16 + v] + bias[q];
+          x[q] = x[q] < least ? least : x[q];
+          if (a.mask) x[q] = value(gate[g & 1][v][q]) > 0.0f ? x[q] : 0.0f;
+          if constexpr (EXACT) {
+            if (a.accumulate) x[q] += value(old[g & 1][v][q]);
           }
         }
-        T* const at = p + v * TI * ld;
-        if (n >= TJ) {
-          store_whole<TJ>(at, x);
-        } else {
-#pragma unroll
-          for (int q = 0; q < TJ; ++q)
-            if (q < n) put(at + q, x[q]);
-        }
+        store_whole<TJ>(out + d * ld, x);
       }
-    }
-  });
+    });
+  }
 }
 
 // The slices' partial sums, added in order.
