@@ -342,13 +342,15 @@ hipError_t rms_norm_fwd(const RmsNormArgs& a, hipStream_t s) {
 }
 
 hipError_t rms_norm_bwd(const RmsNormArgs& a, hipStream_t s) {
-  const hipError_t e = a.dtype       ? launch_bwd<bf16_t, bf16_t>(a, s)
-                       : a.out_dtype ? launch_bwd<float, bf16_t>(a, s)
-                                     : launch_bwd<float, float>(a, s);
-  if (e != hipSuccess) return e;
+  if (a.rows) {   // of no rows no tensor is touched, and dweight is their sum, 0
+    const hipError_t e = a.dtype       ? launch_bwd<bf16_t, bf16_t>(a, s)
+                         : a.out_dtype ? launch_bwd<float, bf16_t>(a, s)
+                                       : launch_bwd<float, float>(a, s);
+    if (e != hipSuccess) return e;
+  }
   const unsigned sums = static_cast<unsigned>((a.cols + SUM_COLS - 1) / SUM_COLS);
   hipLaunchKernelGGL(rms_norm_sum_kernel, dim3(sums), dim3(SUM_COLS * SUM_RUNS), 0, s, a.ws, a.dweight, a.cols,
-                     static_cast<int>(bwd_blocks(a.rows, bwd_shape(a.cols))));
+                     a.rows ? static_cast<int>(bwd_blocks(a.rows, bwd_shape(a.cols))) : 0);
   return hipGetLastError();
 }
 

@@ -533,7 +533,7 @@ ProductArgs product_args(const spectrain_product_desc* desc) {
   if (d.m < 0 || d.n < 0 || d.k < 0) fail("m, n and k must be >= 0");
   if (d.m >= int64_t{1} << 31 || d.n >= int64_t{1} << 31 || d.k > MAX_CODES_LD)
     fail("m and n must be below 2^31 and k at most 2^22");
-  if (ceil_div(d.m, 64) * ceil_div(d.n, 64) > 1 << 23) fail("ceil(m / 64) * ceil(n / 64) must be at most 2^23");
+  if (ceil_div(d.m, 64) * ceil_div(d.n, 64) > 1 << 22) fail("ceil(m / 64) * ceil(n / 64) must be at most 2^22");
   ProductArgs a;
   a.m = d.m;
   a.n = d.n;

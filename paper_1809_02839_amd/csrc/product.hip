@@ -79,11 +79,9 @@ struct TileArgs : ProductArgs {
   float* partial = nullptr;                       // splits > 1: [slice][m][n]
 };
 
-// W values of a row at any element's address, as float32 and as raw bf16.
+// W values of a row, stored at any element's address.
 template <int W>
 using Floats = float __attribute__((ext_vector_type(W), aligned(4)));
-template <int W>
-using Halves = uint16_t __attribute__((ext_vector_type(W), aligned(2)));
 
 template <int W>
 __device__ __forceinline__ void store_whole(float* p, const float (&v)[W]) {
@@ -648,7 +646,7 @@ Plan plan_of(long m, long n, long k, bool exact) {
     const Variant& v = exact ? VARIANTS_EXACT[i] : VARIANTS[i];
     const long tiles = ((m + 64 * v.t - 1) / (64 * v.t)) * ((n + 64 * v.t - 1) / (64 * v.t));
     for (int splits : {1, 2, 3, 4, 6, 8, 12, MAX_SPLITS}) {
-      if (splits > 1 && 2 * splits > k_blocks) break;
+      if (splits > 1 && (2 * splits > k_blocks || tiles * splits > 1 << 16)) break;   // few tiles only: planes stay small
       const int per = (k_blocks + splits - 1) / splits, used = (k_blocks + per - 1) / per;
       const long slots = 256L * v.per_cu, work = tiles * used, rounds = work / slots, rest = work - rounds * slots;
       const double full = v.fixed + per * v.step_full;

@@ -414,7 +414,8 @@ def _operand(rows, cols, g, tiles=False, scale=1.0):
 PRODUCTS = [(1, 1, 1), (1, 40, 128), (3, 33, 7), (5, 2048, 512), (16, 1000, 1531), (17, 129, 64), (31, 500, 2049),
             (33, 300, 4096), (64, 64, 8192), (65, 127, 129), (100, 1, 777), (128, 128, 128), (130, 257, 384),
             (256, 512, 1024), (300, 16, 6000), (777, 500, 333), (1000, 130, 5000), (513, 769, 640), (256, 256, 16),
-            (2000, 1030, 2056), (1531, 3001, 272)]
+            (2000, 1030, 2056), (1531, 3001, 272), (20, 16401, 700), (32, 16384, 130),
+            (9, 9001, 1500), (16, 17000, 64), (4090, 4081, 1003), (4096, 4096, 4000)]
 
 
 def _scale(codes, scales):
@@ -649,3 +650,15 @@ def test_layer_repeats_on_another_stream_and_in_a_graph(shape):
         for layer in (a, b):
             got = [t.clone() for t in layer.outputs()]
             assert all(torch.equal(x, y) for x, y in zip(got, layer.run()))
+
+
+def test_norm_of_no_rows_takes_no_tensors():
+    """A backward of no rows reads nothing, the weight neither: its pointers may be null."""
+    import ctypes
+    native = _native()
+    d = native.RmsNormDesc(native.ABI_VERSION, native.FP32, native.FP32, native.FP32, 1e-6, 0, 0, 100)
+    dw, ws = torch.ones(100, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    rc = native.lib().spectrain_rms_norm_backward(ctypes.byref(d), None, None, None, None, None, None, dw.data_ptr(),
+                                                  ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert rc == native.OK and bool((dw == 0).all())
