@@ -331,6 +331,7 @@ __global__ __launch_bounds__(NT, blocks_of_cu(TI, TJ, STAGES)) void product_tile
   };
 
   constexpr int READS = TI + TJ, LOADS = SA::LOADS + SB::LOADS;
+  constexpr bool LATE = (EXACT ? 2 * TI : TI * TJ) >= 4;   // groups of products: the next block is waited for amid the second half's
   const auto read_some = [&](auto wc, auto total, int kb, int h) {
     constexpr int w = decltype(wc)::value, n = decltype(total)::value, per = (READS + n - 1) / n;
     each<per>([&](auto u) { read_item(std::integral_constant<int, w * per + decltype(u)::value>{}, kb, h); });
@@ -346,21 +347,27 @@ __global__ __launch_bounds__(NT, blocks_of_cu(TI, TJ, STAGES)) void product_tile
       read_some(w, total, kb, 1);
       __builtin_amdgcn_sched_barrier(0);
     });
-    dma_wait<(STAGES - 2) * (LOADS + 1)>();
+    if constexpr (!LATE) dma_wait<(STAGES - 2) * (LOADS + 1)>();
     __syncthreads();
     const uint32_t stage = base + static_cast<uint32_t>(stage_of(kb));
     load_scales(kb + STAGES, stage);
     uint32_t na, nb;
-    read_scales(kb + 1, na, nb);
+    if constexpr (!LATE) read_scales(kb + 1, na, nb);
     const int fa0 = from(sa.off, sa.chunk, kb + STAGES), fb0 = from(sb.off, sb.chunk, kb + STAGES);
     multiply(std::integral_constant<int, 1>{}, [&](auto wc, auto total) {
       constexpr int w = decltype(wc)::value, n = decltype(total)::value, per = (LOADS + n - 1) / n;
-      read_some(wc, total, kb + 1, 0);
+      if constexpr (!LATE) read_some(wc, total, kb + 1, 0);
+      else if constexpr (w >= n / 2) read_some(std::integral_constant<int, w - n / 2>{}, std::integral_constant<int, n - n / 2>{}, kb + 1, 0);
       each<per>([&](auto u) {
         constexpr int item = w * per + decltype(u)::value;
         if constexpr (item < SA::LOADS) sa.load(item, stage, fa0, wave);
         else if constexpr (item < LOADS) sb.load(item - SA::LOADS, stage + SA::BYTES, fb0, wave);
       });
+      if constexpr (LATE && w == n / 2 - 1) {
+        dma_wait<(STAGES - 2) * (LOADS + 1) + 1 + ((w + 1) * per < LOADS ? (w + 1) * per : LOADS)>();
+        __syncthreads();
+        read_scales(kb + 1, na, nb);
+      }
       __builtin_amdgcn_sched_barrier(0);
     });
     ea = na;
@@ -625,8 +632,7 @@ struct Variant {
   int t, stages, per_cu;
   double fixed, step_alone, step_full;
 };
-constexpr Variant VARIANTS[] = {{4, 2, 1, 10.3, 1.43, 1.43}, {2, 2, 2, 4.5, 0.62, 0.93}, {2, 4, 1, 3.9, 0.50, 0.50},
-                                {1, 4, 2, 2.2, 0.22, 0.375}};
+constexpr Variant VARIANTS[] = {{4, 2, 1, 10.3, 1.40, 1.40}, {2, 2, 2, 4.5, 0.44, 0.91}, {1, 4, 2, 2.2, 0.22, 0.375}};
 constexpr Variant VARIANTS_EXACT[] = {{4, 2, 1, 12.5, 2.70, 2.70}, {2, 2, 2, 4.6, 0.84, 1.54}, {1, 4, 2, 2.5, 0.385, 0.575}};
 
 struct Plan {
@@ -641,8 +647,7 @@ Plan plan_of(long m, long n, long k, bool exact) {
   const int k_blocks = static_cast<int>(std::max((k + BK - 1) / BK, 1L));
   Plan best;
   double least = 1e300;
-  const int variants = exact ? std::size(VARIANTS_EXACT) : std::size(VARIANTS);
-  for (int i = 0; i < variants; ++i) {
+  for (int i = 0; i < static_cast<int>(std::size(VARIANTS)); ++i) {
     const Variant& v = exact ? VARIANTS_EXACT[i] : VARIANTS[i];
     const long tiles = ((m + 64 * v.t - 1) / (64 * v.t)) * ((n + 64 * v.t - 1) / (64 * v.t));
     for (int splits : {1, 2, 3, 4, 6, 8, 12, MAX_SPLITS}) {
@@ -688,12 +693,9 @@ hipError_t product_of(const ProductArgs& args, hipStream_t s) {
   a.splits = p.splits;
   a.per_split = p.per_split;
   if (p.splits > 1) a.partial = args.ws;
-  const Variant& v = EXACT ? VARIANTS_EXACT[p.variant] : VARIANTS[p.variant];
-  hipError_t e;
-  if (v.t == 4) e = launch<4, 4, EXACT, 2>(a, s);
-  else if (v.t == 1) e = launch<1, 1, EXACT, 4>(a, s);
-  else if (EXACT || v.stages == 2) e = launch<2, 2, EXACT, 2>(a, s);
-  else e = launch<2, 2, EXACT, EXACT ? 2 : 4>(a, s);
+  const hipError_t e = p.variant == 0   ? launch<4, 4, EXACT, VARIANTS[0].stages>(a, s)
+                       : p.variant == 1 ? launch<2, 2, EXACT, VARIANTS[1].stages>(a, s)
+                                        : launch<1, 1, EXACT, VARIANTS[2].stages>(a, s);
   if (e != hipSuccess || p.splits == 1) return e;
   const long threads = a.m * ((a.n + 3) / 4);
   hipLaunchKernelGGL(product_join_kernel, dim3(static_cast<unsigned>((threads + NT - 1) / NT)), dim3(NT), 0, s, a);
