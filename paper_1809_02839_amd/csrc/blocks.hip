@@ -6,7 +6,11 @@
 // for both orientations. Thread (g, c) of 16 x 16 holds rows 8 g .. 8 g + 7 at
 // columns 8 c .. 8 c + 7: a row's scale needs the 16 lanes of a row group, a
 // column's the 16 threads of equal c, over LDS. The transposed codes turn in LDS
-// (8 rows of a column are 8 consecutive bytes of a transposed line).
+// (8 rows of a column are 8 consecutive bytes of a transposed line). Codes come from
+// the conversions that scale (two values an instruction, straight from bf16) and
+// maxima of bf16 pairs: with float arithmetic for each value the pass was bound by
+// vector instructions (134 million values in both orientations 205 us, now 118, 4.5
+// TB/s; 409 million restored from either in 289, 4.2).
 #include "blocks.hpp"
 #include "kernels.hpp"
 
