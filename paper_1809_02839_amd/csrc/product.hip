@@ -635,14 +635,16 @@ hipError_t launch_rows(const ProductArgs& a, hipStream_t s) {
 }
 
 // Kernels of square block tiles: 64 t rows and columns, stages of k in LDS, and
-// what they cost by measurement (us): fixed for a block's start and end, and a k
-// block with one, or as many as fit, blocks of the kind on a CU.
+// what they cost by measurement (us): fixed for a block's start and end, a k
+// block with one, or as many as fit, blocks of the kind on a CU, and a block's mask or
+// sums to add to (8192 x 2048 x 2048 in float32 that is added to: tiles of 128 70 us, of
+// 256 80; written only 62 and 59).
 struct Variant {
   int t, stages, per_cu;
-  double fixed, step_alone, step_full;
+  double fixed, step_alone, step_full, reads;
 };
-constexpr Variant VARIANTS[] = {{4, 2, 1, 10.3, 1.40, 1.40}, {2, 2, 2, 4.5, 0.44, 0.91}, {1, 4, 2, 2.2, 0.22, 0.375}};
-constexpr Variant VARIANTS_EXACT[] = {{4, 2, 1, 12.5, 2.70, 2.70}, {2, 2, 2, 4.6, 0.84, 1.54}, {1, 4, 2, 2.5, 0.385, 0.575}};
+constexpr Variant VARIANTS[] = {{4, 2, 1, 10.3, 1.40, 1.40, 3.0}, {2, 2, 2, 4.5, 0.44, 0.91, 1.0}, {1, 4, 2, 2.2, 0.22, 0.375, 0.5}};
+constexpr Variant VARIANTS_EXACT[] = {{4, 2, 1, 12.5, 2.70, 2.70, 20.0}, {2, 2, 2, 4.6, 0.84, 1.54, 6.0}, {1, 4, 2, 2.5, 0.385, 0.62, 2.0}};
 
 struct Plan {
   int variant = 0, splits = 1, per_split = 1;
@@ -654,7 +656,7 @@ constexpr int MAX_SPLITS = 16;
 // the 256 CUs, and for slices a second launch that reads their planes. Slices: 512 x
 // 2048 x 8192 18 us, with none 47. Tiles of 64 too: 8192 x 512 x 2048 14 us, in the
 // larger alone 20. Tiles of 256 for many: 8192 cubed 400 us, of 128 by these tables 500.
-Plan plan_of(long m, long n, long k, bool exact) {
+Plan plan_of(long m, long n, long k, bool exact, bool reads) {
   const int k_blocks = static_cast<int>(std::max((k + BK - 1) / BK, 1L));
   Plan best;
   double least = 1e300;
@@ -665,10 +667,10 @@ Plan plan_of(long m, long n, long k, bool exact) {
       if (splits > 1 && (2 * splits > k_blocks || tiles * splits > 1 << 16)) break;   // few tiles only: planes stay small
       const int per = (k_blocks + splits - 1) / splits, used = (k_blocks + per - 1) / per;
       const long slots = 256L * v.per_cu, work = tiles * used, rounds = work / slots, rest = work - rounds * slots;
-      const double full = v.fixed + per * v.step_full;
+      const double fixed = v.fixed + (reads && used == 1 ? v.reads : 0.0), full = fixed + per * v.step_full;
       double t = rounds * full;
       if (rest > 256) t += full;
-      else if (rest) t += v.fixed + per * v.step_alone;
+      else if (rest) t += fixed + per * v.step_alone;
       if (used > 1) t += 2.0 + 2.0 * used * m * n * 4 / 5e6;
       if (t < least) {
         least = t;
@@ -697,7 +699,7 @@ template <bool EXACT>
 hipError_t product_of(const ProductArgs& args, hipStream_t s) {
   if (args.m <= 16) return launch_rows<1, EXACT>(args, s);
   if (args.m <= ROWS_MAX) return launch_rows<2, EXACT>(args, s);
-  const Plan p = plan_of(args.m, args.n, args.k, EXACT);
+  const Plan p = plan_of(args.m, args.n, args.k, EXACT, args.mask || args.accumulate);
   TileArgs a;
   static_cast<ProductArgs&>(a) = args;
   a.k_blocks = static_cast<int>(std::max((args.k + BK - 1) / BK, 1L));
@@ -719,8 +721,10 @@ size_t product_ws_bytes(long m, long n, long k) {
   if (m <= ROWS_MAX || n == 0) return 0;
   size_t planes = 0;
   for (bool exact : {false, true}) {
-    const int splits = plan_of(m, n, k, exact).splits;
-    if (splits > 1) planes = std::max(planes, static_cast<size_t>(splits));
+    for (bool reads : {false, true}) {
+      const int splits = plan_of(m, n, k, exact, reads).splits;
+      if (splits > 1) planes = std::max(planes, static_cast<size_t>(splits));
+    }
   }
   return planes * m * n * sizeof(float);
 }
