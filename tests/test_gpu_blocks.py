@@ -415,7 +415,7 @@ PRODUCTS = [(1, 1, 1), (1, 40, 128), (3, 33, 7), (5, 2048, 512), (16, 1000, 1531
             (33, 300, 4096), (64, 64, 8192), (65, 127, 129), (100, 1, 777), (128, 128, 128), (130, 257, 384),
             (256, 512, 1024), (300, 16, 6000), (777, 500, 333), (1000, 130, 5000), (513, 769, 640), (256, 256, 16),
             (2000, 1030, 2056), (1531, 3001, 272), (20, 16401, 700), (32, 16384, 130),
-            (9, 9001, 1500), (16, 17000, 64), (4090, 4081, 1003), (4096, 4096, 4000)]
+            (9, 9001, 1500), (16, 17000, 64), (4090, 4081, 1003), (4096, 4096, 4000), (4090, 4081, 6001)]
 
 
 def _scale(codes, scales):
