@@ -10,9 +10,9 @@
 // turned to bf16 (exact, scale included) for v_mfma_f32_32x32x16_bf16 at half the
 // rate (1e-7 of the norm).
 //
-// 8192 cubed: 400 us, 2750 TFLOP/s, matrix instructions busy 70% of the time; float32 out 745 us, 1475 TFLOP/s, busy 80%. The vendor
-// library's product of the same codes without block scales: 376 us; its bf16
-// product: 1583 TFLOP/s.
+// 8192 cubed: 400 us, 2750 TFLOP/s, matrix instructions busy 79% of the time; float32
+// out 745 us, 1475 TFLOP/s, busy 80%. The vendor library multiplies such codes without
+// block scales in 376 us, and bf16 at 1574 TFLOP/s (16384 x 16384 x 8192).
 #include <algorithm>
 #include <iterator>
 #include <type_traits>
@@ -510,8 +510,8 @@ __global__ __launch_bounds__(NT) void product_join_kernel(TileArgs a) {
 // takes 16 RT rows of B and every W-th block of k, its codes straight from memory
 // into the registers of v_mfma_scale_f32_16x16x128_f8f6f4 (lane 16 c + r: 32
 // codes of row r), the next block's under way while it multiplies; the waves'
-// sums are added in order over LDS. 16 x 16384 x 8192: 29 us with the call, 4.7 TB/s
-// (56 in square tiles); half the waves' time is waiting for memory.
+// sums are added in order over LDS. 16 x 16384 x 8192: 28 us, 4.8 TB/s (in
+// tiles of 64 32); half the waves' time is waiting for memory.
 struct Fragment {
   i32x8_t codes;
   int scale;
@@ -616,8 +616,9 @@ __global__ __launch_bounds__(RT == 1 ? 1024 : 512) void product_rows_kernel(Prod
   }
 }
 
-// Rows of A that this kernel takes. 64 x 16384 x 8192 in it, 64 rows a wave, took 53
-// us, in square tiles 33.
+// Rows of A that this kernel takes. 32 x 8192 x 4096 takes 10.7 us in it, in tiles of 64
+// 10.3, in float32 11.3 and 12.3; 64 x 4096 x 4096, 64 rows a wave, would take 14.7, in tiles
+// 9.0.
 constexpr long ROWS_MAX = 32;
 
 template <int MT, bool EXACT>
@@ -653,9 +654,9 @@ struct Plan {
 constexpr int MAX_SPLITS = 16;
 
 // The kernel and the slices of k of the least modelled time: rounds of blocks over
-// the 256 CUs, and for slices a second launch that reads their planes. Slices: 512 x
-// 2048 x 8192 18 us, with none 47. Tiles of 64 too: 8192 x 512 x 2048 14 us, in the
-// larger alone 20. Tiles of 256 for many: 8192 cubed 400 us, of 128 by these tables 500.
+// the 256 CUs, and for slices a second launch that reads their planes. In us: 8192
+// cubed in tiles of 256 398, of 128 510; 8192 x 512 x 2048 of 256 28, of 128 14, of 64 21;
+// 512 x 2048 x 8192 of 128 34, of 64 19; 512 x 512 x 8192 of 64 17, in 4 slices 10.6.
 Plan plan_of(long m, long n, long k, bool exact, bool reads) {
   const int k_blocks = static_cast<int>(std::max((k + BK - 1) / BK, 1L));
   Plan best;
