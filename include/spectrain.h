@@ -494,7 +494,7 @@ int spectrain_blocks_restore(const spectrain_blocks_desc* desc, const uint8_t* c
  *   rstd = 1 / sqrt(mean(h^2) + eps)          y = h rstd weight
  * y is written in out_dtype (y_dev), in blocks of 128 of a row (codes_dev and
  * scales_dev, as spectrain_blocks_pack ROWS takes them from the float32 y), or
- * both. Sums are float32: a row whose squares pass its range has rstd 0. sum
+ * both. A row whose mean square passes float32's range has rstd 0. sum
  * (NULL: not kept) goes with a residual and may be x or the residual itself (the
  * same ld); otherwise outputs may not overlap inputs or each other. rstd float32
  * [rows], NULL where no backward follows.

@@ -13,9 +13,9 @@
 // float32 next to such a border would show; memory hides the arithmetic.
 //
 // 16384 x 8192 bf16 with a residual: forward 199 us, backward 201, 5.4 and 5.3 TB/s
-// (a copy of 1 GiB: 5.1); 8192 x 512 to 8 bits 9.4. The backward of long
-// rows runs out of registers for a row and the next: 3.9 TB/s at 16384 columns, 1.9
-// at 32768, where they spill.
+// (a copy of 1 GiB: 5.1); 8192 x 512 to 8 bits 9.4. The backward of rows
+// past 8192 columns has no registers for them and the next and reads them a second
+// time, from L2: 3.9 TB/s at 16384 columns, 1.9 at 32768, where what is left spills.
 #include <algorithm>
 #include <type_traits>
 

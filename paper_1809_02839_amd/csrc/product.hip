@@ -672,7 +672,7 @@ Plan plan_of(long m, long n, long k, bool exact, bool reads) {
       double t = rounds * full;
       if (rest > 256) t += full;
       else if (rest) t += fixed + per * v.step_alone;
-      if (used > 1) t += 2.0 + 2.0 * used * m * n * 4 / 5e6;
+      if (used > 1) t += 2.0 + 2.0 * (used + reads) * m * n * 4 / 5e6;
       if (t < least) {
         least = t;
         best.variant = i;
