@@ -2,6 +2,8 @@
 // write tensors in blocks of 128 share.
 #pragma once
 
+#include <algorithm>
+
 #include "common.hpp"
 
 namespace spx {
@@ -47,6 +49,13 @@ __device__ __forceinline__ float block_limit(int e) { return e == 120 ? 240.0f :
 __device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
   const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
+}
+
+// Bytes that a tile of `rows` rows takes of a line of `lines` scale bytes, from byte
+// `first` on: its rows', and none behind the multiple of 16 that ends the line (what
+// lies there, up to the next line, may be another tensor's).
+__host__ __device__ constexpr long tile_scale_bytes(long rows, long first, long lines) {
+  return std::min(rows, (lines + 15) / 16 * 16 - first);
 }
 
 // Vectors at any element's address: rows need not start at multiples of 16 bytes.

@@ -245,8 +245,10 @@ __global__ __launch_bounds__(NT, blocks_of_cu(TI, TJ, STAGES)) void product_tile
   const __amdgpu_buffer_rsrc_t scales =
       make_rsrc((second ? a.b_scales : a.a_scales) + line0,
                 a.k ? (a.k_blocks - 1L) * scales_ld + (lines + 15) / 16 * 16 - line0 : 0);
+  // lanes that have no byte of the tile's part of a line load its last four again
+  const int scales_off = static_cast<int>(std::min(4L * lane, tile_scale_bytes(second ? SB::ROWS : SA::ROWS, line0, lines) - 4));
   const auto load_scales = [&](int kb, uint32_t stage) {
-    dma4(scales, stage + scales_at, kb < kb1 ? 4 * lane + kb * scales_ld : 0x7ffffff0);
+    dma4(scales, stage + scales_at, kb < kb1 ? scales_off + kb * scales_ld : 0x7ffffff0);
   };
   const auto load_block = [&](int kb) {
     const uint32_t stage = base + static_cast<uint32_t>(stage_of(kb));
