@@ -79,10 +79,15 @@ struct Raw {
   }
 };
 
-// 1 / sqrt(m): float32's, and one step of Newton's iteration in 64 bits. 0 where m passes float32.
+// 1 / sqrt(m): float32's, and one step of Newton's iteration in 64 bits. 0 where m passes
+// float32. Below its normal numbers m loses bits in float32, more than one step
+// brings back (1e-44: 1.4e-4): there 2^128 m is taken, and 2^64 put back.
 __device__ __forceinline__ double inverse_root(double m) {
-  const double r = 1.0f / sqrtf(static_cast<float>(m));
-  return r == 0.0 ? 0.0 : r * (1.5 - 0.5 * m * r * r);
+  const bool small = m < 0x1p-126;
+  const double s = small ? m * 0x1p128 : m;
+  const double r = 1.0f / sqrtf(static_cast<float>(s));
+  const double q = r * (1.5 - 0.5 * s * r * r);
+  return r == 0.0 ? 0.0 : small ? q * 0x1p64 : q;
 }
 
 constexpr int threads_of(int tpr) { return tpr > NT ? tpr : NT; }
