@@ -247,6 +247,12 @@ struct ProductArgs {
   long m = 0, n = 0, k = 0, a_ld = 0, a_scales_ld = 0, b_ld = 0, b_scales_ld = 0, out_ld = 0, mask_ld = 0;
   int out_dtype = 0, bias_dtype = 0, relu = 0, accumulate = 0;
 };
+// What runs: tiles of `tile` rows and columns (0: the kernel of few rows), k in `slices` of
+// `per_slice` blocks of 128. exact: a float32 out; reads: a mask, or sums to add to.
+struct ProductPlan {
+  int tile = 0, slices = 1, per_slice = 0;
+};
+ProductPlan product_plan(long m, long n, long k, bool exact, bool reads);
 size_t product_ws_bytes(long m, long n, long k);
 hipError_t product(const ProductArgs& a, hipStream_t s);
 

@@ -720,6 +720,12 @@ hipError_t product_of(const ProductArgs& args, hipStream_t s) {
 
 }  // namespace
 
+ProductPlan product_plan(long m, long n, long k, bool exact, bool reads) {
+  if (m <= ROWS_MAX) return {};
+  const Plan p = plan_of(m, n, k, exact, reads);
+  return {64 * (exact ? VARIANTS_EXACT : VARIANTS)[p.variant].t, p.splits, p.per_split};
+}
+
 size_t product_ws_bytes(long m, long n, long k) {
   if (m <= ROWS_MAX || n == 0) return 0;
   size_t planes = 0;

@@ -1,5 +1,6 @@
 """Host checks on what the product's kernels read and which of them a call runs,
 asked from the sources and the built library."""
+from product_shapes import KINDS, SLICED
 from test_dispatch_host import _run, needs_build
 
 SCALES = r"""
@@ -32,3 +33,44 @@ int main() {
 @needs_build
 def test_a_tile_reads_no_scale_bytes_behind_a_line(tmp_path):
     _run(SCALES, tmp_path)
+
+
+PLANS = r"""
+#include <cstdio>
+#include "kernels.hpp"
+using namespace spx;
+int main() {
+  const long shapes[][3] = {%s};
+  for (const auto& s : shapes)
+    for (bool exact : {false, true})
+      for (bool reads : {false, true}) {
+        const ProductPlan p = product_plan(s[0], s[1], s[2], exact, reads);
+        const long blocks = (s[2] + 127) / 128, plane = s[0] * s[1] * 4;
+        // every slice has blocks of k, and the workspace holds a plane for each
+        if (p.slices > 1 && (p.slices * p.per_slice < blocks || (p.slices - 1) * p.per_slice >= blocks ||
+                             product_ws_bytes(s[0], s[1], s[2]) < static_cast<size_t>(p.slices * plane)))
+          return 1;
+        std::printf("%%d %%d %%d\n", p.tile, p.slices, int(p.slices * p.per_slice > blocks));
+      }
+}
+"""
+
+
+def _plans(shapes, tmp_path):
+    """(tile, slices, whether the last slice is short) of each shape, by kind."""
+    out = _run(PLANS % ", ".join("{%d, %d, %d}" % s for s in shapes), tmp_path).splitlines()
+    rows = [tuple(map(int, l.split())) for l in out]
+    return [rows[i:i + 4] for i in range(0, len(rows), 4)]
+
+
+@needs_build
+def test_the_sliced_shapes_run_the_kernels_they_are_there_for(tmp_path):
+    """The cost model may move; then the shapes have to follow, or a kernel goes untested."""
+    reached = set()
+    for (shape, tiles), plans in zip(SLICED.items(), _plans(SLICED, tmp_path)):
+        for kind, tile, plan in zip(KINDS, tiles, plans):
+            print(shape, kind, plan)
+            assert plan[0] == tile and plan[1] > 1, (shape, kind, plan)
+            reached.add((kind, tile, plan[2]))
+    for kind in KINDS:
+        assert {(t, 1) for t in (64, 128, 256)} <= {(t, short) for k, t, short in reached if k == kind}, kind
