@@ -16,6 +16,7 @@
 // (a copy of 1 GiB: 5.1); 8192 x 512 to 8 bits 9.4. The backward of rows
 // past 8192 columns has no registers for them and the next and reads them a second
 // time, from L2: 3.9 TB/s at 16384 columns, 1.9 at 32768, where what is left spills.
+// Forwards of such rows: 4.5 TB/s at 16384 columns, 3.9 at 32768, which spill too.
 #include <algorithm>
 #include <type_traits>
 
@@ -270,8 +271,10 @@ __global__ __launch_bounds__(SUM_COLS * SUM_RUNS) void rms_norm_sum_kernel(const
 
 // Threads of a row and vectors of a thread. A wave to a row up to 1024 columns (16384
 // rows of 1024: 24 us, with 256 threads 34), more threads past them (8192 of 2048: 24,
-// with a wave 25; 256 of 2048: 3.4 and 5.1). The backward holds five times a vector's
-// registers for each and takes more threads.
+// with a wave 25; 256 of 2048: 3.4 and 5.1), and further on as few threads as hold the
+// row: 8192 of 8192 in 512 threads 100 us, in 1024 161; of 4096 in 256 54, in 512 77. The
+// backward holds five times a vector's registers for each and takes more threads:
+// 4096 of 16384 in 1024 137, in 512 181.
 struct Shape {
   int tpr, v;
 };
@@ -297,6 +300,8 @@ Shape bwd_shape(long cols) {
 }
 int rows_of_block(const Shape& s) { return s.tpr < NT ? NT / s.tpr : 1; }
 
+// Blocks of a backward at most, each of which leaves a partial row: 65536 x 512 takes 53 us
+// with 512, 83 with 256 and 56 with 1024; 8192 x 8192 109, 104 and 116; 8192 x 2048 30, 40 and 27.
 constexpr long BWD_BLOCKS = 512;
 long bwd_blocks(long rows, const Shape& s) {
   return std::max(1L, std::min((rows + 2 * rows_of_block(s) - 1) / (2 * rows_of_block(s)), BWD_BLOCKS));

@@ -626,7 +626,11 @@ constexpr long ROWS_MAX = 32;
 template <int MT, bool EXACT>
 hipError_t launch_rows(const ProductArgs& a, hipStream_t s) {
   const int k_blocks = static_cast<int>((a.k + BK - 1) / BK);
-  // 16 RT rows a block: a block for each CU at least where there are so many rows
+  // 16 RT rows a block: a block for each CU at least where there are so many rows (16 x 8192 x
+  // 4096: 32 rows 9.3 us, 16 11.5, 64 12.0; 16 x 16384 x 8192: 64 rows 28.3, 32 35.2). Waves: four
+  // where k has no blocks for more (the same times as eight), sixteen for 16 rows and a long k,
+  // which a few rows of A gain by and 32 lose by (1 x 2048 x 8192 7.3 us, with eight 8.1; 16 x
+  // 2048 x 8192 10.5 and 9.8; 32 x 8176 x 2048 9.7 and 8.7)
   const int rt = a.n >= 256 * 64 ? 4 : a.n >= 256 * 32 ? 2 : 1;
   const int waves = k_blocks <= 4 ? 4 : rt == 1 && k_blocks > 8 ? 16 : 8;
   const unsigned blocks = static_cast<unsigned>((a.n + 16 * rt - 1) / (16 * rt));

@@ -58,7 +58,7 @@ def test_mean_squares_below_the_normal_numbers(cols, eps):
 
 # Rows by the thousand. The forward takes up to 65536 blocks of one row (past 1024 columns), then each
 # block another; the backward 512 blocks at most, of four waves that take rows by
-# themselves (up to 1024 columns) or one group of threads: each walks three rows and more here.
+# themselves (up to 1024 columns) or one group of threads: they walk three rows and more here.
 ROWS = [(65600, 1032, torch.bfloat16), (1700, 1531, torch.float32), (5000, 512, torch.bfloat16),
         (2600, 8192, torch.bfloat16), (1541, 8200, torch.bfloat16)]
 
