@@ -1,5 +1,6 @@
-"""GPU: products in slices of k, in every tile that takes them, and how exactly a float32
-result is summed, against a plain implementation in 64 bits.
+"""GPU: products in slices of k, in every tile that takes them, how exactly a float32
+result is summed, and everything that may become of the sums at once, against a plain
+implementation in 64 bits.
 
 Tolerances are bounds, not measured values.
   element  as for products in one piece: (k / 16 + 64 + 16 + 3) 2^-23 sum |a b|, for a
@@ -19,7 +20,7 @@ import pytest
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
-from product_shapes import KINDS, SLICED                                          # noqa: E402
+from product_shapes import KINDS, SLICED, WHOLE                                          # noqa: E402
 from test_gpu_blocks import BF, F32, HALF, STEP, _close, _expected, _gen, _native, _operand, _randn, _scale, _tolerance   # noqa: E402
 
 
@@ -77,3 +78,32 @@ def test_a_float32_result_is_summed_in_float32(shape):
     off = float((out.double() - want).norm() / want.norm())
     print(f"[float32] {shape} {off:.2e} of the norm", flush=True)
     assert off <= _norm_bound(k)
+
+
+@pytest.mark.parametrize("out_t", [F32, BF], ids=["float32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 33, 7), (31, 500, 300), *WHOLE, (300, 301, 6001), (69, 2883, 11031)])
+def test_bias_relu_mask_and_what_was_there_together(shape, out_t):
+    """A bias of the other type, ReLU, a mask in rows that start at odd elements; into float32 also added."""
+    native = _native()
+    m, n, k = shape
+    print(f"[together] {shape} {out_t}", flush=True)
+    g = _gen(m + n + 5 * k)
+    (a, sa, A), (b, sb, B) = _operand(m, k, g), _operand(n, k, g, tiles=True, scale=k ** -0.5)
+    bias = _randn((n,), g, BF if out_t == F32 else F32)
+    mask = _randn((m, n + 5), g, out_t)[:, 3:3 + n]
+    mask[0, 0], mask[-1, -1], mask[m // 2, n // 2] = float("nan"), 0.0, -0.0
+    p = native.Product(m, n, k, relu=True, accumulate=out_t == F32)
+    room = _randn((m + 2, n + 7), g, out_t)
+    before, out, ws = room.clone(), room[1:-1, 5:5 + n], p.workspace()
+    ws.fill_(255)
+    old = out.double() if out_t == F32 else torch.zeros(m, n, dtype=torch.float64, device="cuda")
+    p.apply(a, sa, b, sb, out, bias=bias, mask=mask, workspace=ws)
+    want = _expected(A, B, bias, True, mask)
+    tol = _tolerance(out_t, k, A, B, _scale(a, sa), _scale(b, sb), bias)
+    tol = torch.where(mask.double() > 0, tol, torch.zeros_like(tol))         # a masked element is 0, or what was there
+    if out_t == F32:
+        want, tol = want + old, tol + STEP * (want.abs() + old.abs() + tol)
+    _close(out, want, tol + HALF[out_t] * (want.abs() + tol) + 1e-300, "out")
+    assert torch.equal(out[~(mask > 0)].double(), old[~(mask > 0)])
+    out.copy_(before[1:-1, 5:5 + n])
+    assert torch.equal(room, before), "values around out were written"

@@ -1,6 +1,6 @@
 """Host checks on what the product's kernels read and which of them a call runs,
 asked from the sources and the built library."""
-from product_shapes import KINDS, SLICED
+from product_shapes import KINDS, SLICED, WHOLE
 from test_dispatch_host import _run, needs_build
 
 SCALES = r"""
@@ -74,3 +74,9 @@ def test_the_sliced_shapes_run_the_kernels_they_are_there_for(tmp_path):
             reached.add((kind, tile, plan[2]))
     for kind in KINDS:
         assert {(t, 1) for t in (64, 128, 256)} <= {(t, short) for k, t, short in reached if k == kind}, kind
+
+
+@needs_build
+def test_the_whole_shapes_run_the_kernels_they_are_there_for(tmp_path):
+    for (shape, tile), plans in zip(WHOLE.items(), _plans(WHOLE, tmp_path)):
+        assert all(p[:2] == (tile, 1) for p in plans), (shape, plans)
