@@ -561,7 +561,7 @@ void run_product(const spectrain_product_desc* desc, const uint8_t* a_codes, con
   check_blocks(a_codes, a_scales, a.m, a.k, d.a_ld, d.a_scales_ld, "a");
   check_blocks(b_codes, b_scales, a.n, a.k, d.b_ld, d.b_scales_ld, "b");
   const int64_t blocks = ceil_div(a.k, 128);
-  if (blocks && (d.a_scales_ld >= (int64_t{1} << 31) / blocks || d.b_scales_ld >= (int64_t{1} << 31) / blocks))
+  if (blocks && std::max(d.a_scales_ld, d.b_scales_ld) > ((int64_t{1} << 31) - 1) / blocks)
     fail("scales_ld * ceil(k / 128) must be below 2^31");
   a.out_ld = given_ld(out, d.out_ld, a.n, d.out_dtype, "out");
   a.mask_ld = given_ld(mask, d.mask_ld, a.n, d.out_dtype, "mask");

@@ -1,5 +1,8 @@
 """Host checks on what the product's kernels read and which of them a call runs,
 asked from the sources and the built library."""
+import ctypes
+
+from paper_1809_02839_amd import native
 from product_shapes import KINDS, SLICED, WHOLE
 from test_dispatch_host import _run, needs_build
 
@@ -80,3 +83,17 @@ def test_the_sliced_shapes_run_the_kernels_they_are_there_for(tmp_path):
 def test_the_whole_shapes_run_the_kernels_they_are_there_for(tmp_path):
     for (shape, tile), plans in zip(WHOLE.items(), _plans(WHOLE, tmp_path)):
         assert all(p[:2] == (tile, 1) for p in plans), (shape, plans)
+
+
+def test_scale_lines_are_taken_up_to_the_stated_size():
+    """scales_ld * ceil(k / 128) below 2^31 is accepted, also where 2^31 is no multiple of the blocks of k (a call of no
+    rows: the arguments are checked, nothing runs)."""
+    blocks, ld = 32760, 65552
+    assert blocks * ld < 1 << 31 <= blocks * (ld + 16)
+    for side in ("a_scales_ld", "b_scales_ld"):
+        for extra, code in ((0, native.OK), (16, native.EINVAL)):
+            d = native.ProductDesc(native.ABI_VERSION, native.FP32, native.FP32, 0, 0, 0, 0, 64, 128 * blocks, 1 << 22, 64,
+                                   1 << 22, 64, 64, 64)
+            setattr(d, side, ld + extra)
+            rc = native.lib().spectrain_product(ctypes.byref(d), 4096, 8192, 12288, 16384, None, None, None, None, 0, None)
+            assert rc == code, (side, extra, native.lib().spectrain_last_error())
